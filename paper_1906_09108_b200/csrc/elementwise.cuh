@@ -11,50 +11,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-#include "once_per_device.h"
+#include "kernel_common.cuh"
 
 namespace fdg {
-
-// ------------------------------------------------ programmatic dependent launch --
-// The kernels that follow one another in a module's chain (convolution, batch-norm apply, batch-norm
-// backward apply) are launched with programmatic stream serialisation: the next kernel of the stream may be
-// scheduled while this one still runs, does the part of its start-up that needs nothing from global
-// memory (barriers, tensor-memory allocation, descriptor prefetch), and then blocks in grid_dependency_wait()
-// until the preceding kernel has completed and its writes are visible.  Nothing may be read from or written
-// to global memory before that wait.  grid_dependency_release() tells the scheduler that, as far as this
-// block is concerned, the next kernel may start being scheduled (it fires once every block has called it or
-// exited).  Both are no-ops in a kernel launched the ordinary way.
-__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void grid_dependency_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
-// Launch with the attribute that allows the overlap described above.
-template <typename... KArgs, typename... Args>
-inline cudaError_t launch_chained(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
-}
-
-// Makes a setting of the current device (see OncePerDevice).  Setting a function attribute is no stream operation: a launch
-// may be a recorded one.
-template <typename Work>
-inline cudaError_t once_per_device(OncePerDevice* once, Work work) {
-  int dev = 0;
-  const cudaError_t e = cudaGetDevice(&dev);
-  return e != cudaSuccess ? e : once->run(dev, work);
-}
-template <typename Kernel>
-inline cudaError_t set_smem_limit(Kernel kernel, size_t bytes) {
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-}
-
-// SMs of a B200.  Splits whose rows need scratch are planned for this number, not for the device's own: the size of the
-// workspace is asked for without a device.
-constexpr int kSms = 148;
 
 // A batch norm with given statistics (inference) applied in the epilogue of the convolution that produces its input:
 // the convolution's output is rounded to the storage type first, as if it had been stored, so that the result is that of
@@ -76,12 +35,6 @@ template <> struct Vec<__nv_bfloat16> {
   static constexpr int N = 8;
   __nv_bfloat16 v[8];
 };
-
-__device__ __forceinline__ float to_f(float x) { return x; }
-__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <typename T> __device__ __forceinline__ T from_f(float x);
-template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
 // Loads VEC consecutive elements (VEC == 1 or a full 16-byte vector) as floats.
 template <typename T, int VEC>

@@ -1,0 +1,104 @@
+// What the kernels of the library share: programmatic dependent launch, settings made once per device, conversion between
+// storage types and fp32, and vectors of 8 channels.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "once_per_device.h"
+
+namespace fdg {
+
+// ------------------------------------------------ programmatic dependent launch --
+// The kernels that follow one another in a module's chain (convolution, batch-norm apply, batch-norm
+// backward apply) are launched with programmatic stream serialisation: the next kernel of the stream may be
+// scheduled while this one still runs, does the part of its start-up that needs nothing from global
+// memory (barriers, tensor-memory allocation, descriptor prefetch), and then blocks in grid_dependency_wait()
+// until the preceding kernel has completed and its writes are visible.  Nothing may be read from or written
+// to global memory before that wait.  grid_dependency_release() tells the scheduler that, as far as this
+// block is concerned, the next kernel may start being scheduled (it fires once every block has called it or
+// exited).  Both are no-ops in a kernel launched the ordinary way.
+__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_dependency_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// Launch with the attribute that allows the overlap described above.
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_chained(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+// Makes a setting of the current device (see OncePerDevice).  Setting a function attribute is no stream operation: a launch
+// may be a recorded one.
+template <typename Work>
+inline cudaError_t once_per_device(OncePerDevice* once, Work work) {
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  return e != cudaSuccess ? e : once->run(dev, work);
+}
+template <typename Kernel>
+inline cudaError_t set_smem_limit(Kernel kernel, size_t bytes) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+// SMs of a B200.  Splits whose rows need scratch are planned for this number, not for the device's own: the size of the
+// workspace is asked for without a device.
+constexpr int kSms = 148;
+
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T> __device__ __forceinline__ T from_f(float x);
+template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// Eight consecutive values of a row in the storage type (16 or 32 bytes), as the kernels on columns of 8 channels move them.
+// VEC: the row is a whole number of such vectors and 16-byte aligned; otherwise the first `left` values exist, one by one,
+// and the rest read as zero.
+template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };
+template <typename T, bool VEC> __device__ __forceinline__ Raw8<T> raw8_load(const T* __restrict__ p, int left) {
+  Raw8<T> r;
+  if constexpr (VEC) {
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) r.q[j] = reinterpret_cast<const uint4*>(p)[j];
+  } else {
+    T* e = reinterpret_cast<T*>(&r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = i < left ? p[i] : from_f<T>(0.f);
+  }
+  return r;
+}
+template <typename T> __device__ __forceinline__ void raw8_to_f(const Raw8<T>& r, float (&v)[8]) {
+  const T* e = reinterpret_cast<const T*>(&r);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = to_f(e[i]);
+}
+template <typename T> __device__ __forceinline__ Raw8<T> raw8_of(const float (&v)[8]) {
+  Raw8<T> r;
+  T* e = reinterpret_cast<T*>(&r);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e[i] = from_f<T>(v[i]);
+  return r;
+}
+template <typename T, bool VEC> __device__ __forceinline__ void raw8_put(T* __restrict__ p, int left, const Raw8<T>& r) {
+  if constexpr (VEC) {
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(p)[j] = r.q[j];
+  } else {
+    const T* e = reinterpret_cast<const T*>(&r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) p[i] = e[i];
+  }
+}
+template <typename T, bool VEC> __device__ __forceinline__ void raw8_store(T* __restrict__ p, int left, const float (&v)[8]) {
+  raw8_put<T, VEC>(p, left, raw8_of<T>(v));
+}
+
+}  // namespace fdg
