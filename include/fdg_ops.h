@@ -165,6 +165,56 @@ fdg_status fdg_bn_backward(int precision, const void* dy, const void* mask, cons
                            void* dx, void* dx2, float* dgamma, float* dbeta, float* dgamma2, float* dbeta2, size_t rows,
                            int C, const float* partial, int nparts, int block_cap, void* scratch, size_t scratch_bytes,
                            fdg_stream stream);
+/* ---- tensors held in 8 bits ("checkpoints": activations kept for the backward pass in about half of bf16's bytes) ----
+ * No counterpart in the paper; its 2(K-k) batches in flight are what makes activations the largest part of a module's memory.
+ * A tensor [rows][C] is held as codes[rows][C] (signed bytes) and scales[rows][ceil(C/32)] (bytes): each block of
+ * FDG_CKPT_BLOCK consecutive channels of a row (the last of a row may be shorter) has a step 2^e, e the smallest integer
+ * >= -126 for which the block's largest magnitude rounds to at most 127 steps; code = x / step rounded to nearest even,
+ * scale byte = e + 127, value held = code * step, which is exact in bf16 and fp32: an error of at most half a step.
+ * A block with an infinity or NaN: scale byte 255, codes 0, reads back as NaN throughout.  Largest magnitudes of
+ * 127.5/128 * 2^128 and more keep e = 121 and codes of at most 127, so that finite values stay finite.
+ * A decoded bf16 checkpoint is the checkpoint, with no further rounding: fdg_conv_wgrad takes it as its x.
+ * The tensors of one call do not overlap.  Asynchronous on `stream`. */
+#define FDG_CKPT_BLOCK 32
+fdg_status fdg_ckpt_encode(int precision, const void* x, size_t rows, int C, int8_t* codes, uint8_t* scales, fdg_stream stream);
+fdg_status fdg_ckpt_decode(int precision, const int8_t* codes, const uint8_t* scales, size_t rows, int C, void* x, fdg_stream stream);
+
+/* ---- group normalisation with an activation -------------------------------------------------------------------------
+ * The normalisation that does not depend on which images share a batch.  x [N][HW][C]; group g of an image is channels
+ * [g*C/groups, (g+1)*C/groups) at all of its pixels (groups = 1: layer norm over an image, groups = C: instance norm).
+ * `groups` divides C; any C, any alignment that the storage type has (multiples of 8 channels on 16-byte aligned tensors are
+ * fastest).  gamma, beta, dgamma, dbeta [C], stats [2][N][groups] (mean, then 1/sqrt(var + eps), biased variance) are fp32.
+ * `scratch`: fdg_gn_scratch_bytes bytes of device memory, 256-byte aligned, any contents; it serves both calls, and is not
+ * to be shared by calls that may run at the same time.  The result of a call does not depend on scheduling.  No output
+ * overlaps an input or another output.  Errors: FDG_ERR_INVALID_ARG (null pointer, bad shape, precision or activation, a
+ * combination named below), FDG_ERR_WORKSPACE_TOO_SMALL, FDG_ERR_CUDA; nothing is launched after the first two. */
+typedef struct {
+  int N;        /* images */
+  int HW;       /* pixels of an image */
+  int C;        /* channels */
+  int groups;
+} fdg_gn_shape;
+enum { FDG_ACT_NONE = 0, FDG_ACT_RELU = 1, FDG_ACT_SILU = 2 };       /* z, max(z, 0), z/(1 + exp(-z)) */
+fdg_status fdg_gn_scratch_bytes(int precision, const fdg_gn_shape* shape, size_t* bytes);
+/* y = act(gamma*(x - mean)*rstd + beta [+ res]), and the statistics.  Optional outputs:
+ *   gate            [N][HW][ceil(C/8)] bytes, FDG_ACT_RELU only: bit i of byte j = [y > 0] at channel 8j + i (unused bits 0)
+ *   codes, scales   x held in 8 bits (both or neither), formed in the same pass over x where blocks fall on whole columns
+ *                   (ceil(C/8) a multiple of 4, or at most 2), else by a pass of its own
+ * `res` (nullable) is not to be combined with FDG_ACT_SILU, whose backward recomputes z from x alone. */
+fdg_status fdg_gn_forward(int precision, const fdg_gn_shape* shape, const void* x, const float* gamma, const float* beta,
+                          const void* res, int act, float eps, void* y, float* stats, uint8_t* gate, int8_t* codes,
+                          uint8_t* scales, void* scratch, size_t scratch_bytes, fdg_stream stream);
+/* With dz = dy * act'(z):  dbeta = sum dz, dgamma = sum dz*xhat over images and pixels,
+ *   dx = rstd*(gamma*dz - mean_group(gamma*dz) - xhat*mean_group(gamma*dz*xhat)) [+ res].
+ * xhat = (x - mean)*rstd from `stats` and either `x` or the checkpoint (`codes`, `scales`); exactly one of the two is given.
+ * FDG_ACT_RELU: dz = dy * [y > 0] from exactly one of `mask` (y, or any tensor that is positive where y is) and `gate`; the other
+ * activations take neither.  FDG_ACT_SILU recomputes z from xhat, gamma and beta (beta nullable otherwise).  Where the
+ * forward added `res`, the gradient of that summand is dz. */
+fdg_status fdg_gn_backward(int precision, const fdg_gn_shape* shape, const void* dy, const void* x, const int8_t* codes,
+                           const uint8_t* scales, const float* stats, const float* gamma, const float* beta, int act,
+                           const void* mask, const uint8_t* gate, const void* res, void* dx, float* dgamma, float* dbeta,
+                           void* scratch, size_t scratch_bytes, fdg_stream stream);
+
 /* out = beta * in: the shrinking of the received delayed gradient (Eq. 15). */
 fdg_status fdg_shrink(int precision, const void* in, void* out, float beta, size_t n, fdg_stream stream);
 /* The update of Eq. 11 with the optimiser of the experiments section: g' = grad + wd*theta;

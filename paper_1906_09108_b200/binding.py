@@ -20,6 +20,8 @@ FDG_SHORTCUT_PROJECTION, FDG_SHORTCUT_ZERO_PAD = 0, 1
 FDG_BACKWARD_FIRST, FDG_FORWARD_FIRST = 0, 1
 FDG_STASHED, FDG_CURRENT = 0, 1
 FDG_FP32_CUDACORE, FDG_BF16_TC = 0, 1
+FDG_ACT_NONE, FDG_ACT_RELU, FDG_ACT_SILU = 0, 1, 2
+FDG_CKPT_BLOCK = 32
 PARAM_KINDS = {0: "conv", 1: "bn_gamma", 2: "bn_beta", 3: "fc_w", 4: "fc_b"}
 
 EXPORTS = ["fdg_workspace_bytes", "fdg_create", "fdg_destroy", "fdg_param_count", "fdg_param_layout",
@@ -33,7 +35,7 @@ EXPORTS = ["fdg_workspace_bytes", "fdg_create", "fdg_destroy", "fdg_param_count"
            "fdg_ingest", "fdg_head", "fdg_debug_raise_flag", "fdg_debug_wait_probe", "fdg_debug_guard_count", "fdg_debug_guard_offset",
            "fdg_debug_check_guards", "fdg_probe_mma_rate", "fdg_bn_stats_from_partials", "fdg_lr_at", "fdg_set_lr_schedule", "fdg_bn_running_count",
            "fdg_get_bn_running", "fdg_set_bn_running", "fdg_eval", "fdg_drain", "fdg_state_bytes", "fdg_save_state",
-           "fdg_load_state"]
+           "fdg_load_state", "fdg_ckpt_encode", "fdg_ckpt_decode", "fdg_gn_scratch_bytes", "fdg_gn_forward", "fdg_gn_backward"]
 
 
 class fdg_arch(C.Structure):
@@ -61,6 +63,10 @@ class fdg_sched_entry(C.Structure):
 class fdg_conv_shape(C.Structure):
     _fields_ = [("N", C.c_int), ("H", C.c_int), ("W", C.c_int), ("Ci", C.c_int), ("Co", C.c_int), ("R", C.c_int),
                 ("stride", C.c_int), ("pad", C.c_int)]
+
+
+class fdg_gn_shape(C.Structure):
+    _fields_ = [("N", C.c_int), ("HW", C.c_int), ("C", C.c_int), ("groups", C.c_int)]
 
 
 class fdg_lr_schedule(C.Structure):
@@ -154,6 +160,11 @@ def load_library(path=LIB_PATH):
                          C.c_int, vp],
         "fdg_bn_backward": [C.c_int, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, C.c_int, vp,
                             C.c_int, C.c_int, vp, sz, vp],
+        "fdg_ckpt_encode": [C.c_int, vp, sz, C.c_int, vp, vp, vp],
+        "fdg_ckpt_decode": [C.c_int, vp, vp, sz, C.c_int, vp, vp],
+        "fdg_gn_scratch_bytes": [C.c_int, P(fdg_gn_shape), P(sz)],
+        "fdg_gn_forward": [C.c_int, P(fdg_gn_shape), vp, vp, vp, vp, C.c_int, C.c_float, vp, vp, vp, vp, vp, vp, sz, vp],
+        "fdg_gn_backward": [C.c_int, P(fdg_gn_shape), vp, vp, vp, vp, vp, vp, vp, C.c_int, vp, vp, vp, vp, vp, vp, vp, sz, vp],
         "fdg_shrink": [C.c_int, vp, vp, C.c_float, sz, vp],
         "fdg_sgd_update": [vp, vp, vp, vp, vp, sz, C.c_float, C.c_float, C.c_float, vp],
         "fdg_ingest": [C.c_int, vp, vp, sz, C.c_int, C.c_int, vp, vp, C.c_int, vp],
@@ -535,7 +546,7 @@ class ConvOps:
 
 
 class EwOps:
-    """The memory-bound operator-level calls (fdg_bn_*, fdg_shrink, fdg_sgd_update, fdg_ingest, fdg_head) on
+    """The memory-bound operator-level calls (fdg_bn_*, fdg_gn_*, fdg_ckpt_*, fdg_shrink, fdg_sgd_update, fdg_ingest, fdg_head) on
     torch CUDA tensors; activations [rows, C] (any leading shape) in the precision's storage type."""
 
     def __init__(self, precision):
@@ -544,6 +555,7 @@ class EwOps:
         self.lib = load_library()
         self.precision = precision
         self.dtype = torch.bfloat16 if precision == FDG_BF16_TC else torch.float32
+        self._gn_shapes = {}                     # (N, HW, C, groups) -> (fdg_gn_shape, scratch bytes)
 
     def _stream(self):
         return self.torch.cuda.current_stream().cuda_stream
@@ -596,6 +608,105 @@ class EwOps:
                                            _ptr(db2), rows, ch, _ptr(partial), 0 if partial is None else partial.shape[0],
                                            block_cap, _ptr(sc), nb, self._stream()))
         return (dx, dg, db, dx2, dg2, db2) if second else (dx, dg, db)
+
+    # -- group norm, and tensors held in 8 bits.  The library sees addresses only, so what it cannot check is checked here.
+    def _take(self, t, shape, dtype, what):
+        """The address of a contiguous tensor of the current device with this shape and type."""
+        if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device.index != self.torch.cuda.current_device():
+            raise FDGError(1, "%s: expected a contiguous %s tensor of shape %s on the current device, got %s %s on %s"
+                           % (what, dtype, tuple(shape), t.dtype, tuple(t.shape), t.device))
+        return t.data_ptr()
+
+    def _gn(self, t, groups):
+        """(shape structure, scratch bytes) of a group norm of tensors like t [N, pixels.., C]."""
+        if t.dim() < 2:
+            raise FDGError(1, "group norm: expected [N, pixels.., C], got %s" % (tuple(t.shape),))
+        n, ch = t.shape[0], t.shape[-1]
+        key = (n, t.numel() // max(n * ch, 1), ch, groups)
+        got = self._gn_shapes.get(key)
+        if got is None:
+            s, need = fdg_gn_shape(*key), C.c_size_t()
+            self._chk(self.lib.fdg_gn_scratch_bytes(self.precision, C.byref(s), C.byref(need)))
+            if len(self._gn_shapes) >= 4096:
+                self._gn_shapes.clear()
+            got = self._gn_shapes[key] = (s, need.value)
+        return got
+
+    @staticmethod
+    def _act(name):
+        if name not in ("none", "relu", "silu"):
+            raise FDGError(1, "activation %r: none, relu or silu" % (name,))
+        return {"none": FDG_ACT_NONE, "relu": FDG_ACT_RELU, "silu": FDG_ACT_SILU}[name]
+
+    def _held_shapes(self, shape):
+        return shape, shape[:-1] + (-(-shape[-1] // FDG_CKPT_BLOCK),)
+
+    def ckpt_encode(self, x):
+        """(codes, scales): x [.., C] held in 8 bits."""
+        torch = self.torch
+        cs, ss = self._held_shapes(x.shape)
+        px = self._take(x, x.shape, self.dtype, "x")
+        codes = torch.empty(cs, dtype=torch.int8, device=x.device)
+        scales = torch.empty(ss, dtype=torch.uint8, device=x.device)
+        self._chk(self.lib.fdg_ckpt_encode(self.precision, px, x.numel() // max(cs[-1], 1), cs[-1], codes.data_ptr(), scales.data_ptr(),
+                                           self._stream()))
+        return codes, scales
+
+    def ckpt_decode(self, held):
+        """The tensor that held = (codes, scales) stands for."""
+        torch = self.torch
+        codes, scales = held
+        cs, ss = self._held_shapes(codes.shape)
+        pc, ps = self._take(codes, cs, torch.int8, "codes"), self._take(scales, ss, torch.uint8, "scales")
+        x = torch.empty(cs, dtype=self.dtype, device=codes.device)
+        self._chk(self.lib.fdg_ckpt_decode(self.precision, pc, ps, codes.numel() // max(cs[-1], 1), cs[-1], x.data_ptr(), self._stream()))
+        return x
+
+    def gn_forward(self, x, groups, gamma, beta, act="none", res=None, eps=1e-5, gate=False, checkpoint=False):
+        """y = act(group norm of x [N, pixels.., C] [+ res]).  Returns (y, stats [2, N, groups], gate, (codes, scales)); the last
+        two are None unless asked for: the bits of [y > 0] (relu only), and x held in 8 bits, for gn_backward."""
+        torch = self.torch
+        s, need = self._gn(x, groups)
+        vec = (s.C,)
+        args = [self._take(x, x.shape, self.dtype, "x"), self._take(gamma, vec, torch.float32, "gamma"),
+                self._take(beta, vec, torch.float32, "beta"), None if res is None else self._take(res, x.shape, self.dtype, "res")]
+        y = torch.empty_like(x)
+        stats = torch.empty((2, s.N, groups), dtype=torch.float32, device=x.device)
+        bits = torch.empty(x.shape[:-1] + ((s.C + 7) // 8,), dtype=torch.uint8, device=x.device) if gate else None
+        held = None
+        if checkpoint:
+            cs, ss = self._held_shapes(x.shape)
+            held = torch.empty(cs, dtype=torch.int8, device=x.device), torch.empty(ss, dtype=torch.uint8, device=x.device)
+        sc = torch.empty(need, dtype=torch.uint8, device=x.device)
+        self._chk(self.lib.fdg_gn_forward(self.precision, C.byref(s), *args, self._act(act), eps, y.data_ptr(), stats.data_ptr(),
+                                          _ptr(bits), *((None, None) if held is None else (held[0].data_ptr(), held[1].data_ptr())),
+                                          sc.data_ptr(), need, self._stream()))
+        return y, stats, bits, held
+
+    def gn_backward(self, dy, x, stats, groups, gamma, beta=None, act="none", mask=None, gate=None, res=None):
+        """(dx, dgamma, dbeta).  `x`: the input of gn_forward, or (codes, scales) as it left them; relu: `mask` = y or `gate` = its
+        bits; silu: `beta`; `res` is added to dx."""
+        torch = self.torch
+        s, need = self._gn(dy, groups)
+        vec = (s.C,)
+        pdy = self._take(dy, dy.shape, self.dtype, "dy")
+        if isinstance(x, (tuple, list)):
+            cs, ss = self._held_shapes(dy.shape)
+            px, pc, ps = None, self._take(x[0], cs, torch.int8, "codes"), self._take(x[1], ss, torch.uint8, "scales")
+        else:
+            px, pc, ps = self._take(x, dy.shape, self.dtype, "x"), None, None
+        args = [self._take(stats, (2, s.N, groups), torch.float32, "stats"), self._take(gamma, vec, torch.float32, "gamma"),
+                None if beta is None else self._take(beta, vec, torch.float32, "beta")]
+        masks = [None if mask is None else self._take(mask, dy.shape, self.dtype, "mask"),
+                 None if gate is None else self._take(gate, dy.shape[:-1] + ((s.C + 7) // 8,), torch.uint8, "gate"),
+                 None if res is None else self._take(res, dy.shape, self.dtype, "res")]
+        dx = torch.empty_like(dy)
+        dparam = torch.empty((2, s.C), dtype=torch.float32, device=dy.device)
+        dg = dparam.data_ptr()
+        sc = torch.empty(need, dtype=torch.uint8, device=dy.device)
+        self._chk(self.lib.fdg_gn_backward(self.precision, C.byref(s), pdy, px, pc, ps, *args, self._act(act), *masks, dx.data_ptr(),
+                                           dg, dg + 4 * s.C, sc.data_ptr(), need, self._stream()))
+        return dx, dparam[0], dparam[1]
 
     def shrink(self, x, beta):
         out = self.torch.empty_like(x)

@@ -2,11 +2,12 @@
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfdg.so")
-SOURCES = ["fdg.cu"]
+SOURCES = ["fdg.cu", "norm_ops.cu"]
 
 
 def _newest_source():
@@ -22,17 +23,23 @@ def build(force=False, verbose=False):
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "--shared", "-Xcompiler", "-fPIC", "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES] + \
-          []
+    flags = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-Xcompiler", "-fPIC"]
     if verbose:
-        cmd.insert(1, "-Xptxas=-v")
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("nvcc failed building libfdg.so")
-    if verbose:
-        sys.stderr.write(res.stderr)
+        flags.insert(0, "-Xptxas=-v")
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        runs = [subprocess.Popen([nvcc] + flags + ["-c", "-o", o, os.path.join(CSRC, s)], stdout=subprocess.PIPE,
+                                 stderr=subprocess.STDOUT, text=True) for s, o in zip(SOURCES, objects)]
+        said = [r.communicate()[0] for r in runs]                     # one process per source, side by side
+        if any(r.returncode for r in runs):
+            sys.stderr.write("".join(said))
+            raise RuntimeError("nvcc failed building libfdg.so")
+        if verbose:
+            sys.stderr.write("".join(said))
+        res = subprocess.run([nvcc] + flags + ["--shared", "-o", LIB] + objects, capture_output=True, text=True)
+        if res.returncode != 0:
+            sys.stderr.write(res.stdout + res.stderr)
+            raise RuntimeError("nvcc failed linking libfdg.so")
     return LIB
 
 

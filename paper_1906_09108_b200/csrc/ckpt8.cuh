@@ -1,0 +1,233 @@
+// Activations held in 8 bits between the forward and the backward pass ("checkpoints").
+//
+// A tensor [rows][C] is held as one signed byte per value and one scale byte per block of 32 consecutive channels of a row
+// (the last block of a row may be shorter):
+//   step  = 2^e with e the smallest integer >= -126 for which the block's largest magnitude rounds to at most 127 steps,
+//   code  = x / step rounded to the nearest integer, ties to even;   value held = code * step;   scale byte = e + 127.
+// A step that is a power of two makes the division and the product exact, so a value is rounded once (by at most half a
+// step), every reader forms the same number, and that number has 7 significant bits: a bf16 tensor decoded from a
+// checkpoint is the checkpoint, and the tensor-core weight gradients multiply it without a further rounding.  The step is
+// up to twice amax/127; blocks as short as 32 (1/32 byte per value for the scale) give most of that back against one fp32
+// scale per row.  Two borders: a block that holds an infinity or a NaN gets scale byte 255 and codes 0 and reads back as NaN
+// throughout; where e would be 122 (magnitudes from 127.5/128 * 2^128 on, bf16's largest among them) e stays 121, so that
+// every value held is finite, and codes stop at +-127.
+#pragma once
+#include "kernel_common.cuh"
+
+namespace fdg {
+
+constexpr int kCkptBlock = 32;
+constexpr int kCkptThreads = 256;
+
+// ---- one block's scale, 8 values at a time --------------------------------------------------------
+// `top`: the largest magnitude of the block as its bit pattern (the order of the patterns is that of the magnitudes, with
+// infinity and then NaN above them).  Adding 2^16 carries into the exponent exactly when the mantissa is 255/128 or more,
+// i.e. when the magnitude is 127.5 steps of the lower exponent or more (127.5 itself rounds to 128).
+struct CkptScale {
+  uint32_t byte;        // e + 127
+  float inv_step;       // 2^-e; 0 for a block that is not finite
+  bool clamp;           // codes past +-127 are possible
+};
+__device__ __forceinline__ CkptScale ckpt_scale(uint32_t top) {
+  CkptScale s;
+  s.clamp = top >= 0x7F7F0000u;
+  const uint32_t e = min((top + 0x10000u) >> 23, 254u);
+  const uint32_t k = max(e, 7u) - 6u;
+  s.byte = top >= 0x7F800000u ? 255u : k;
+  s.inv_step = top >= 0x7F800000u ? 0.f : __uint_as_float((254u - k) << 23);
+  return s;
+}
+__device__ __forceinline__ uint32_t ckpt_top(const float (&v)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  return m;
+}
+// x / step rounded to the nearest even integer, in the low byte: the product is exact, and adding 1.5 * 2^23 rounds it.
+__device__ __forceinline__ uint32_t ckpt_code(float x, const CkptScale& s) {
+  float t = x * s.inv_step;
+  if (s.clamp) {
+    if (s.byte == 255u) return 0;
+    t = fminf(fmaxf(t, -127.f), 127.f);
+  }
+  return __float_as_uint(t + 12582912.f);
+}
+__device__ __forceinline__ uint2 ckpt_codes(const float (&v)[8], const CkptScale& s) {
+  uint32_t q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = ckpt_code(v[i], s);
+  uint2 r;
+  r.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+  r.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+  return r;
+}
+__device__ __forceinline__ float ckpt_step(uint32_t byte) {
+  return byte == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(byte << 23);
+}
+// code + 128 in the mantissa of 2^23, then the offset off: an integer conversion on the fp32 pipe.
+__device__ __forceinline__ void ckpt_values(uint2 codes, float step, float (&v)[8]) {
+  const uint32_t lo = codes.x ^ 0x80808080u, hi = codes.y ^ 0x80808080u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = (__uint_as_float(__byte_perm(lo, 0x4B000000u, 0x7540u + i)) - 8388736.f) * step;
+    v[4 + i] = (__uint_as_float(__byte_perm(hi, 0x4B000000u, 0x7540u + i)) - 8388736.f) * step;
+  }
+}
+
+// Bytes of 8 codes at element offset `off`; VEC: one 8-byte access, else the first `left`.
+template <bool VEC> __device__ __forceinline__ uint2 load_codes(const int8_t* codes, size_t off, int left) {
+  if constexpr (VEC) {
+    return *reinterpret_cast<const uint2*>(codes + off);
+  } else {
+    uint32_t w[2] = {0, 0};
+    for (int i = 0; i < 8; ++i)
+      if (i < left) w[i >> 2] |= (uint32_t)(uint8_t)codes[off + i] << (8 * (i & 3));
+    return make_uint2(w[0], w[1]);
+  }
+}
+template <bool VEC> __device__ __forceinline__ void store_codes(int8_t* codes, size_t off, int left, uint2 q) {
+  if constexpr (VEC) {
+    *reinterpret_cast<uint2*>(codes + off) = q;
+  } else {
+    for (int i = 0; i < 8; ++i)
+      if (i < left) codes[off + i] = (int8_t)((i < 4 ? q.x : q.y) >> (8 * (i & 3)));
+  }
+}
+
+// Lanes that share a block when consecutive lanes hold consecutive vectors of 8 channels, 0 if blocks do not fall on
+// aligned groups of lanes: rows of whole groups of four vectors, or of one or two vectors (one block).
+inline int ckpt_block_lanes(int C) {
+  const int cols = (C + 7) / 8;
+  return cols % 4 == 0 ? 4 : (cols <= 2 ? cols : 0);
+}
+__device__ __forceinline__ uint32_t ckpt_top_of_lanes(uint32_t top, int lanes) {
+  if (lanes >= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  if (lanes >= 4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  return top;
+}
+
+// ---- whole tensors -----------------------------------------------------------------------------------
+// Encode, rows of whole vectors on aligned lane groups: a thread takes vectors of 8 values, consecutive lanes consecutive
+// vectors, kCkptUnroll of them in flight.  Nothing is shared but the shuffles of a block's maximum.
+constexpr int kCkptUnroll = 4;
+template <typename T>
+__global__ void __launch_bounds__(kCkptThreads) ckpt_encode_kernel(const T* __restrict__ x, size_t vecs, int lanes, int8_t* __restrict__ codes,
+                                                                   uint8_t* __restrict__ scales) {
+  const int shift = lanes >> 1;                       // 1, 2, 4 lanes
+  grid_dependency_wait();
+  const size_t first = (size_t)blockIdx.x * (kCkptThreads * kCkptUnroll) + threadIdx.x;
+  Raw8<T> raw[kCkptUnroll];
+#pragma unroll
+  for (int u = 0; u < kCkptUnroll; ++u) {
+    const size_t i = first + (size_t)u * kCkptThreads;
+    raw[u] = i < vecs ? raw8_load<T, true>(x + i * 8, 8) : Raw8<T>{};
+  }
+#pragma unroll
+  for (int u = 0; u < kCkptUnroll; ++u) {
+    const size_t i = first + (size_t)u * kCkptThreads;
+    float v[8];
+    raw8_to_f(raw[u], v);
+    const CkptScale s = ckpt_scale(ckpt_top_of_lanes(ckpt_top(v), lanes));
+    if (i < vecs) {
+      *reinterpret_cast<uint2*>(codes + i * 8) = ckpt_codes(v, s);
+      if ((i & (unsigned)(lanes - 1)) == 0) scales[i >> shift] = (uint8_t)s.byte;
+    }
+  }
+}
+
+// Encode, any row length and alignment: a warp takes a block, a lane a value.
+template <typename T>
+__global__ void __launch_bounds__(kCkptThreads) ckpt_encode_any_kernel(const T* __restrict__ x, size_t blocks, int C, int per_row,
+                                                                       int8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  grid_dependency_wait();
+  const int lane = threadIdx.x & 31;
+  const size_t stride = (size_t)gridDim.x * (kCkptThreads / 32);
+  for (size_t b = (size_t)blockIdx.x * (kCkptThreads / 32) + (threadIdx.x >> 5); b < blocks; b += stride) {
+    const size_t row = b / (unsigned)per_row;
+    const int c = (int)(b - row * (unsigned)per_row) * kCkptBlock + lane;
+    const size_t off = row * C + c;
+    const float v = c < C ? to_f(x[off]) : 0.f;
+    const CkptScale s = ckpt_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7FFFFFFFu));
+    if (c < C) codes[off] = (int8_t)ckpt_code(v, s);
+    if (lane == 0) scales[b] = (uint8_t)s.byte;
+  }
+}
+
+// Decode, rows of whole vectors (C a multiple of 8): a thread takes vectors of 8 values.  `lanes` as in the encoder; 0: the
+// place of a vector in its row is found by one division and then by steps (step_rows rows and step_cols columns are
+// kCkptThreads vectors).
+template <typename T>
+__global__ void __launch_bounds__(kCkptThreads) ckpt_decode_kernel(const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                                   size_t vecs, int lanes, int cols, int per_row, int step_rows, int step_cols,
+                                                                   T* __restrict__ x) {
+  grid_dependency_wait();
+  const size_t first = (size_t)blockIdx.x * (kCkptThreads * kCkptUnroll) + threadIdx.x;
+  const int shift = lanes >> 1;
+  size_t row = 0;
+  int col = 0;
+  if (lanes == 0) { row = first / (unsigned)cols; col = (int)(first - row * (unsigned)cols); }
+  uint2 q[kCkptUnroll];
+  uint32_t k[kCkptUnroll];
+#pragma unroll
+  for (int u = 0; u < kCkptUnroll; ++u) {
+    const size_t i = first + (size_t)u * kCkptThreads;
+    if (i < vecs) {
+      q[u] = *reinterpret_cast<const uint2*>(codes + i * 8);
+      k[u] = scales[lanes ? i >> shift : row * (unsigned)per_row + (unsigned)col / 4];
+    }
+    if (lanes == 0) {
+      row += (unsigned)step_rows; col += step_cols;
+      if (col >= cols) { col -= cols; ++row; }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kCkptUnroll; ++u) {
+    const size_t i = first + (size_t)u * kCkptThreads;
+    if (i >= vecs) break;
+    float v[8];
+    ckpt_values(q[u], ckpt_step(k[u]), v);
+    raw8_store<T, true>(x + i * 8, 8, v);
+  }
+}
+// Decode, any row length and alignment: a thread takes values.
+template <typename T>
+__global__ void __launch_bounds__(kCkptThreads) ckpt_decode_any_kernel(const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                                       size_t elems, int C, int per_row, T* __restrict__ x) {
+  grid_dependency_wait();
+  const size_t stride = (size_t)gridDim.x * kCkptThreads;
+  for (size_t i = (size_t)blockIdx.x * kCkptThreads + threadIdx.x; i < elems; i += stride) {
+    const size_t row = i / (unsigned)C;
+    const int c = (int)(i - row * C);
+    x[i] = from_f<T>((float)codes[i] * ckpt_step(scales[row * per_row + c / kCkptBlock]));
+  }
+}
+
+// ---- host side -----------------------------------------------------------------------------------------
+inline bool aligned_to(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+constexpr size_t kCkptMaxGrid = (size_t)1 << 30;
+
+template <typename T>
+inline cudaError_t launch_ckpt_encode(cudaStream_t st, const T* x, size_t rows, int C, int8_t* codes, uint8_t* scales) {
+  const int lanes = C % 8 == 0 ? ckpt_block_lanes(C) : 0, per_row = (C + kCkptBlock - 1) / kCkptBlock;
+  if (lanes && aligned_to(x, 16) && aligned_to(codes, 8)) {
+    const size_t vecs = rows * (size_t)(C / 8), per = kCkptThreads * kCkptUnroll, grid = (vecs + per - 1) / per;
+    if (grid <= kCkptMaxGrid)
+      return launch_chained(ckpt_encode_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, x, vecs, lanes, codes, scales);
+  }
+  const size_t blocks = rows * (size_t)per_row, grid = std::min<size_t>((blocks + 7) / 8, (size_t)kSms * 64);
+  return launch_chained(ckpt_encode_any_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, x, blocks, C, per_row, codes, scales);
+}
+template <typename T>
+inline cudaError_t launch_ckpt_decode(cudaStream_t st, const int8_t* codes, const uint8_t* scales, size_t rows, int C, T* x) {
+  const int per_row = (C + kCkptBlock - 1) / kCkptBlock;
+  if (C % 8 == 0 && aligned_to(x, 16) && aligned_to(codes, 8)) {
+    const size_t vecs = rows * (size_t)(C / 8), per = kCkptThreads * kCkptUnroll, grid = (vecs + per - 1) / per;
+    if (grid <= kCkptMaxGrid)
+      return launch_chained(ckpt_decode_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, codes, scales, vecs, ckpt_block_lanes(C), C / 8, per_row,
+                            kCkptThreads / (C / 8), kCkptThreads % (C / 8), x);
+  }
+  const size_t elems = rows * (size_t)C, grid = std::min<size_t>((elems + kCkptThreads - 1) / kCkptThreads, (size_t)kSms * 64);
+  return launch_chained(ckpt_decode_any_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, codes, scales, elems, C, per_row, x);
+}
+
+}  // namespace fdg

@@ -1,0 +1,112 @@
+// Operator-level entry points of the C ABI (declared in include/fdg_ops.h): group normalisation with an activation, and tensors
+// held in 8 bits.
+#include "../../include/fdg.h"
+#include "../../include/fdg_ops.h"
+#include "group_norm.cuh"
+
+namespace fdg {
+typedef __nv_bfloat16 bf16;
+
+static bool precision_ok(int precision) { return precision == FDG_FP32_CUDACORE || precision == FDG_BF16_TC; }
+static unsigned elem_bytes(int precision) { return precision == FDG_BF16_TC ? 2 : 4; }
+static fdg_status status_of(cudaError_t e) { return e == cudaSuccess ? FDG_OK : FDG_ERR_CUDA; }
+
+// rows * C values whose bytes can be counted, and grids that can be given.
+static bool rows_ok(size_t rows, int C) { return C >= 1 && rows >= 1 && rows <= ((size_t)1 << 40) / (size_t)C; }
+static bool gn_shape_ok(int precision, const fdg_gn_shape* s) {
+  if (!s || !precision_ok(precision) || s->N < 1 || s->HW < 1 || s->C < 1 || s->groups < 1 || s->C % s->groups) return false;
+  if (s->C > 1 << 24 || !rows_ok((size_t)s->N * (size_t)s->HW, s->C)) return false;
+  const int b = (int)elem_bytes(precision);
+  return gn::grid_ok(gn::plan_forward(b, s->N, s->HW, s->C, s->groups)) && gn::grid_ok(gn::plan_backward(b, s->N, s->HW, s->C, s->groups, false)) &&
+         gn::grid_ok(gn::plan_backward(b, s->N, s->HW, s->C, s->groups, true));
+}
+static size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Scratch: the backward pass's per-image totals [N][2][C], then the streamed forms' rows of sums.
+static size_t totals_bytes(const fdg_gn_shape* s) { return align256((size_t)s->N * 2 * s->C * sizeof(float)); }
+static size_t gn_scratch_need(int precision, const fdg_gn_shape* s) {
+  const int b = (int)elem_bytes(precision);
+  const size_t rows = std::max({gn::partial_floats(gn::plan_forward(b, s->N, s->HW, s->C, s->groups)),
+                                gn::partial_floats(gn::plan_backward(b, s->N, s->HW, s->C, s->groups, false)),
+                                gn::partial_floats(gn::plan_backward(b, s->N, s->HW, s->C, s->groups, true))});
+  return totals_bytes(s) + align256(rows * sizeof(float));
+}
+
+template <typename T>
+static cudaError_t gn_forward_as(const fdg_gn_shape* s, const void* x, const float* gamma, const float* beta, const void* res, int act, float eps,
+                                 void* y, float* stats, uint8_t* gate, int8_t* codes, uint8_t* scales, void* scratch, cudaStream_t st) {
+  gn::Forward<T> p{};
+  p.x = (const T*)x; p.gamma = gamma; p.beta = beta; p.res = (const T*)res; p.y = (T*)y; p.stats = stats; p.gate = gate;
+  p.codes = codes; p.scales = scales; p.eps = eps; p.act = act;
+  p.partial = reinterpret_cast<float*>(static_cast<char*>(scratch) + totals_bytes(s));
+  return gn::launch_forward<T>(st, gn::plan_forward(sizeof(T), s->N, s->HW, s->C, s->groups), p);
+}
+template <typename T>
+static cudaError_t gn_backward_as(const fdg_gn_shape* s, const void* dy, const void* x, const int8_t* codes, const uint8_t* scales,
+                                  const float* stats, const float* gamma, const float* beta, int act, const void* mask, const uint8_t* gate,
+                                  const void* res, void* dx, float* dgamma, float* dbeta, void* scratch, cudaStream_t st) {
+  gn::Backward<T> p{};
+  p.dy = (const T*)dy; p.x = (const T*)x; p.codes = codes; p.scales = scales; p.stats = stats; p.gamma = gamma; p.beta = beta;
+  p.mask = (const T*)mask; p.gate = gate; p.res = (const T*)res; p.dx = (T*)dx; p.act = act;
+  p.totals = static_cast<float*>(scratch);
+  p.partial = reinterpret_cast<float*>(static_cast<char*>(scratch) + totals_bytes(s));
+  return gn::launch_backward<T>(st, gn::plan_backward(sizeof(T), s->N, s->HW, s->C, s->groups, codes != nullptr), p, dgamma, dbeta);
+}
+}  // namespace fdg
+
+using namespace fdg;
+
+extern "C" {
+
+fdg_status fdg_ckpt_encode(int precision, const void* x, size_t rows, int C, int8_t* codes, uint8_t* scales, fdg_stream stream) {
+  if (!x || !codes || !scales || !precision_ok(precision) || !rows_ok(rows, C) || !aligned_to(x, elem_bytes(precision))) return FDG_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return status_of(precision == FDG_BF16_TC ? launch_ckpt_encode<bf16>(st, (const bf16*)x, rows, C, codes, scales)
+                                            : launch_ckpt_encode<float>(st, (const float*)x, rows, C, codes, scales));
+}
+
+fdg_status fdg_ckpt_decode(int precision, const int8_t* codes, const uint8_t* scales, size_t rows, int C, void* x, fdg_stream stream) {
+  if (!x || !codes || !scales || !precision_ok(precision) || !rows_ok(rows, C) || !aligned_to(x, elem_bytes(precision))) return FDG_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return status_of(precision == FDG_BF16_TC ? launch_ckpt_decode<bf16>(st, codes, scales, rows, C, (bf16*)x)
+                                            : launch_ckpt_decode<float>(st, codes, scales, rows, C, (float*)x));
+}
+
+fdg_status fdg_gn_scratch_bytes(int precision, const fdg_gn_shape* s, size_t* bytes) {
+  if (!bytes || !gn_shape_ok(precision, s)) return FDG_ERR_INVALID_ARG;
+  *bytes = gn_scratch_need(precision, s);
+  return FDG_OK;
+}
+
+fdg_status fdg_gn_forward(int precision, const fdg_gn_shape* s, const void* x, const float* gamma, const float* beta, const void* res, int act,
+                          float eps, void* y, float* stats, uint8_t* gate, int8_t* codes, uint8_t* scales, void* scratch, size_t scratch_bytes,
+                          fdg_stream stream) {
+  if (!gn_shape_ok(precision, s) || !x || !gamma || !beta || !y || !stats || !(eps > 0.f)) return FDG_ERR_INVALID_ARG;
+  if (act != FDG_ACT_NONE && act != FDG_ACT_RELU && act != FDG_ACT_SILU) return FDG_ERR_INVALID_ARG;
+  if ((act == FDG_ACT_SILU && res) || (gate && act != FDG_ACT_RELU) || (codes != nullptr) != (scales != nullptr)) return FDG_ERR_INVALID_ARG;
+  const unsigned b = elem_bytes(precision);
+  if (!aligned_to(x, b) || !aligned_to(y, b) || !aligned_to(res, b) || !aligned_to(scratch, 256)) return FDG_ERR_INVALID_ARG;
+  if (!scratch || scratch_bytes < gn_scratch_need(precision, s)) return FDG_ERR_WORKSPACE_TOO_SMALL;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return status_of(precision == FDG_BF16_TC ? gn_forward_as<bf16>(s, x, gamma, beta, res, act, eps, y, stats, gate, codes, scales, scratch, st)
+                                            : gn_forward_as<float>(s, x, gamma, beta, res, act, eps, y, stats, gate, codes, scales, scratch, st));
+}
+
+fdg_status fdg_gn_backward(int precision, const fdg_gn_shape* s, const void* dy, const void* x, const int8_t* codes, const uint8_t* scales,
+                           const float* stats, const float* gamma, const float* beta, int act, const void* mask, const uint8_t* gate,
+                           const void* res, void* dx, float* dgamma, float* dbeta, void* scratch, size_t scratch_bytes, fdg_stream stream) {
+  if (!gn_shape_ok(precision, s) || !dy || !stats || !gamma || !dx || !dgamma || !dbeta) return FDG_ERR_INVALID_ARG;
+  if (act != FDG_ACT_NONE && act != FDG_ACT_RELU && act != FDG_ACT_SILU) return FDG_ERR_INVALID_ARG;
+  if ((codes != nullptr) != (scales != nullptr) || (x != nullptr) == (codes != nullptr)) return FDG_ERR_INVALID_ARG;
+  if ((mask != nullptr) + (gate != nullptr) != (act == FDG_ACT_RELU ? 1 : 0) || (act == FDG_ACT_SILU && !beta)) return FDG_ERR_INVALID_ARG;
+  const unsigned b = elem_bytes(precision);
+  if (!aligned_to(dy, b) || !aligned_to(x, b) || !aligned_to(mask, b) || !aligned_to(res, b) || !aligned_to(dx, b) || !aligned_to(scratch, 256))
+    return FDG_ERR_INVALID_ARG;
+  if (!scratch || scratch_bytes < gn_scratch_need(precision, s)) return FDG_ERR_WORKSPACE_TOO_SMALL;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return status_of(precision == FDG_BF16_TC
+                       ? gn_backward_as<bf16>(s, dy, x, codes, scales, stats, gamma, beta, act, mask, gate, res, dx, dgamma, dbeta, scratch, st)
+                       : gn_backward_as<float>(s, dy, x, codes, scales, stats, gamma, beta, act, mask, gate, res, dx, dgamma, dbeta, scratch, st));
+}
+
+}  // extern "C"

@@ -1,0 +1,452 @@
+"""Group norm with an activation and tensors held in 8 bits (fdg_gn_*, fdg_ckpt_*) through the C ABI, against their definitions in
+float64 (oracle/norms.py) on the same inputs.
+
+Tolerances, element by element.  A stored value is rounded to nearest: half a step, 2^-8 (bf16) or 2^-24 (fp32) of the value.
+Everything before is fp32 with sums whose longest chain (a thread's values, its row of threads, the lanes of a group) is
+under 256 terms, so a sum is off by less than 256 * 2^-24 of the sum of its terms' magnitudes (K below); means, spreads and the
+two group sums of the backward pass enter an output at most once each with a factor of at most 1 (SiLU's slope: 1.1), and the
+few operations around them are below that.  The magnitude that K multiplies is that of the terms, before any cancellation:
+(|x| + |mean|)*rstd stands for |xhat|.  Checkpoints have no tolerance: the format leaves no freedom."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import norms as L
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-5
+K = 256 * 2.0 ** -24
+PRECISIONS = ["fp32", "bf16"]
+
+# (N, pixels, C, groups)
+SHAPES = [
+    (1, 1, 1, 1), (3, 1, 8, 4), (2, 1, 30, 5), (5, 4, 2, 2),        # one pixel, one value, groups of a few values
+    (8, 256, 8, 4), (4, 1024, 16, 4), (3, 64, 64, 64),              # narrow layers; a group per channel
+    (2, 1024, 160, 32), (2, 64, 640, 1), (3, 49, 320, 32),          # groups of 5 channels; one group; odd maps
+    (2, 784, 30, 6), (3, 65, 33, 11), (7, 9, 24, 3), (1, 100, 7, 7),   # channels that fill no column
+    (2, 17, 2048, 16), (1, 3, 2056, 8), (2, 5, 4104, 27), (1, 2, 4112, 1),      # as wide as a CTA goes, and wider
+]
+# images that no cluster holds
+LARGE = [(1, 16384, 64, 8), (2, 9001, 160, 32), (1, 20011, 30, 1)]
+
+
+def _ops(prec_name):
+    from paper_1906_09108_b200 import binding as B
+    return B, B.EwOps(B.FDG_BF16_TC if prec_name == "bf16" else B.FDG_FP32_CUDACORE)
+
+
+def _half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def _mk(shape, seed, dtype, scale=1.0, shift=0.0):
+    a = np.random.default_rng(seed).standard_normal(shape) * scale + shift
+    t = torch.from_numpy(a.astype(np.float32)).cuda().to(dtype)
+    return t, t.double().cpu().numpy()
+
+
+def _f32(a):
+    return torch.from_numpy(np.asarray(a, np.float32)).cuda()
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _near(got, want, tol, what=""):
+    got = _np(got) if isinstance(got, torch.Tensor) else got
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (what, int(bad.sum()), float(np.abs(got - want)[bad].max()), float(np.broadcast_to(tol, want.shape)[bad].min()))
+
+
+def _params(c, seed):
+    r = np.random.default_rng(seed)
+    return ((1 + 0.3 * r.standard_normal(c)).astype(np.float32).astype(np.float64),
+            (0.2 * r.standard_normal(c)).astype(np.float32).astype(np.float64))
+
+
+
+def _channels(a, c):
+    """[N, groups] -> [N, 1, c]."""
+    return np.repeat(a, c // a.shape[1], 1)[:, None, :]
+
+
+def _size(xo, stats, c):
+    """What stands for |xhat|: (|x| + |mean|) * rstd."""
+    return (np.abs(xo) + np.abs(_channels(stats[0], c))) * _channels(stats[1], c)
+
+
+def _check_forward(ew, shape, act, with_res, seed=0, scale=1.3, shift=0.4, gate=False, ckpt=False, x=None):
+    n, p, c, groups = shape
+    if x is None:
+        x, xo = _mk((n, p, c), seed + 1, ew.dtype, scale, shift)
+    else:
+        xo = _np(x)
+    res, reso = _mk((n, p, c), seed + 2, ew.dtype) if with_res else (None, None)
+    gamma, beta = _params(c, seed + 3)
+    y, stats, bits, held = ew.gn_forward(x, groups, _f32(gamma), _f32(beta), act=act, res=res, eps=EPS, gate=gate, checkpoint=ckpt)
+    yo, z, st = L.groupnorm_forward(xo, groups, gamma, beta, EPS, act, reso)
+    # the mean: K of the mean magnitude; rstd: its square root halves the spread's error, and the CTAs' means enter squared
+    mag = np.abs(xo).reshape(n, p, groups, -1).mean((1, 3))
+    _near(stats[0], st[0], K * mag + 1e-30, "mean")
+    _near(stats[1], st[1], st[1] * (K + (K * mag * st[1]) ** 2), "rstd")
+    size = _size(xo, st, c) * np.abs(gamma) + np.abs(beta) + (0 if reso is None else np.abs(reso))
+    _near(y, yo, _half_step(ew.dtype) * np.abs(yo) + 1.1 * K * size, "y")
+    if gate:
+        b = np.unpackbits(bits.cpu().numpy(), axis=-1, bitorder="little")
+        assert (b[..., :c] == (_np(y) > 0)).all() and not b[..., c:].any()
+    if ckpt:
+        codes, scales = L.ckpt_encode(xo.reshape(-1, c))
+        assert (held[0].cpu().numpy().reshape(-1, c) == codes).all() and (held[1].cpu().numpy().reshape(n * p, -1) == scales).all()
+    return x, xo, y, stats, bits, held
+
+
+def _check_backward(ew, shape, act, seed, xo, x_arg, stats, y, bits, with_res, use_bits):
+    """x_arg is what the call is given, xo the float64 values that it stands for."""
+    n, p, c, groups = shape
+    dy, dyo = _mk((n, p, c), seed + 4, ew.dtype, 0.01)
+    res, reso = _mk((n, p, c), seed + 5, ew.dtype, 0.01) if with_res else (None, None)
+    gamma, beta = _params(c, seed + 3)
+    st = _np(stats)
+    kw = dict(mask=None, gate=None)
+    if act == "relu":
+        kw = dict(mask=None, gate=bits) if use_bits else dict(mask=y, gate=None)
+    dx, dgamma, dbeta = ew.gn_backward(dy, x_arg, stats, groups, _f32(gamma), _f32(beta), act=act, res=res, **kw)
+    xhat = L.groupnorm_xhat(xo, st, groups)
+    size = _size(xo, st, c)
+    dz = dyo * ((_np(y) > 0) if act == "relu" else L.activation_slope(gamma * xhat + beta, act))
+    # SiLU: its slope moves by at most half of what z moves
+    adz = np.abs(dz) + (0.5 * np.abs(dyo) * (size * np.abs(gamma) + np.abs(beta)) if act == "silu" else 0)
+    dxo, dgo, dbo = L.groupnorm_backward(dz, xo, st, groups, gamma, reso)
+    mean = lambda t: _channels(t.reshape(n, p, groups, -1).mean((1, 3)), c)  # noqa: E731
+    h = adz * np.abs(gamma)
+    mag = _channels(st[1], c) * (h + mean(h) + size * mean(h * size)) + (0 if reso is None else np.abs(reso))
+    _near(dx, dxo, _half_step(ew.dtype) * np.abs(dxo) + 2 * K * mag, "dx")
+    _near(dgamma, dgo, 2 * K * (adz * size).sum((0, 1)) + 1e-30, "dgamma")
+    _near(dbeta, dbo, 2 * K * adz.sum((0, 1)) + 1e-30, "dbeta")
+    return dx, dgamma, dbeta
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("shape", SHAPES + LARGE, ids=str)
+def test_forward(prec_name, shape):
+    _, ew = _ops(prec_name)
+    _check_forward(ew, shape, "none", False)
+    _check_forward(ew, shape, "relu", True, seed=10, gate=True, ckpt=shape[0] * shape[1] * shape[2] < 200000)
+    _check_forward(ew, shape, "silu", False, seed=20)
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("shape", SHAPES + LARGE, ids=str)
+def test_backward(prec_name, shape):
+    _, ew = _ops(prec_name)
+    n, p, c, groups = shape
+    for seed, act in ((30, "none"), (40, "relu"), (50, "silu")):
+        x, xo, y, stats, bits, held = _check_forward(ew, shape, act, False, seed=seed, gate=act == "relu")
+        _check_backward(ew, shape, act, seed, xo, x, stats, y, bits, act == "none", False)
+        held = ew.ckpt_encode(x)
+        heldo = L.ckpt_decode(held[0].cpu().numpy().reshape(-1, c), held[1].cpu().numpy().reshape(n * p, -1)).reshape(n, p, c)
+        _check_backward(ew, shape, act, seed, heldo, held, stats, y, bits, True, True)
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("shape", [(2, 40, 16, 4), (2, 24, 64, 2), (2, 9, 30, 5), (1, 16384, 64, 8)], ids=str)
+def test_any_alignment(prec_name, shape):
+    """Contiguous tensors that start at an element's alignment only."""
+    B, ew = _ops(prec_name)
+    n, p, c, groups = shape
+
+    def shifted(t):
+        buf = torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")
+        out = buf[1:].view(t.shape)
+        out.copy_(t)
+        return out
+
+    x = shifted(_mk((n, p, c), 61, ew.dtype)[0])
+    assert x.data_ptr() % 16
+    small = n * p * c < 200000
+    x, xo, y, stats, bits, held = _check_forward(ew, shape, "relu", False, seed=60, gate=True, ckpt=small, x=x)
+    _check_backward(ew, shape, "relu", 60, xo, x, stats, shifted(y), bits, True, False)
+    codes, scales = (shifted(t) for t in ew.ckpt_encode(x))
+    heldo = L.ckpt_decode(codes.cpu().numpy().reshape(-1, c), scales.cpu().numpy().reshape(n * p, -1)).reshape(n, p, c)
+    if small:
+        assert (codes.cpu().numpy() == held[0].cpu().numpy()).all()
+    assert (_np(ew.ckpt_decode((codes, scales))) == heldo).all()
+    _check_backward(ew, shape, "relu", 60, heldo, (codes, scales), stats, y, bits, False, True)
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("shape", [(2, 300, 40, 4), (1, 16384, 64, 8)], ids=str)
+def test_offsets_of_many_spreads(prec_name, shape):
+    """A mean of a thousand spreads: no difference of large sums.  The first pixel, where a pivot might be taken, is far off."""
+    _, ew = _ops(prec_name)
+    n, p, c, groups = shape
+    x, _ = _mk((n, p, c), 71, ew.dtype, 1.0, 1000.0)
+    x[:, 0] = 0.0
+    _check_forward(ew, shape, "none", False, seed=70, x=x)
+    x, _ = _mk((n, p, c), 72, ew.dtype, 0.0, 3.0)               # no spread at all: eps alone
+    _check_forward(ew, shape, "none", False, seed=70, x=x)
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("shape", [(3, 40, 16, 4), (3, 9001, 160, 32)], ids=str)
+def test_what_is_not_finite_stays_in_its_group(prec_name, shape):
+    _, ew = _ops(prec_name)
+    n, p, c, groups = shape
+    cg = c // groups
+    x, _ = _mk((n, p, c), 81, ew.dtype)
+    gamma, beta = (_f32(a) for a in _params(c, 82))
+    clean = ew.gn_forward(x, groups, gamma, beta, act="relu", gate=True, checkpoint=True)
+    x[1, 7, 0] = float("nan")
+    x[1, 8, cg] = float("inf")
+    y, stats, bits, held = ew.gn_forward(x, groups, gamma, beta, act="relu", gate=True, checkpoint=True)
+    assert not stats[:, 1, :2].isfinite().any()
+    assert y[1, :, :2 * cg].isnan().all()
+    keep = torch.ones_like(x, dtype=torch.bool)
+    keep[1, :, :2 * cg] = False
+    assert torch.equal(y[keep], clean[0][keep])
+    others = torch.ones_like(stats, dtype=torch.bool)
+    others[:, 1, :2] = False
+    assert torch.equal(stats[others], clean[1][others])
+    back = ew.ckpt_decode(held)
+    assert back[1, 7, :min(32, c)].isnan().all() and back[1, 8, :min(32, c)].isnan().all()
+    back[1, 7:9], ref = 0, ew.ckpt_decode(clean[3])
+    ref[1, 7:9] = 0
+    assert torch.equal(back[1, 9:], ref[1, 9:]) and torch.equal(back[0], ref[0]) and torch.equal(back[2], ref[2])
+    # the backward pass: images whose own x and dy are finite are as they were; the parameters' gradients are not finite
+    dy, _ = _mk((n, p, c), 83, ew.dtype)
+    a = ew.gn_backward(dy, x, stats, groups, gamma, act="relu", mask=clean[0])
+    b = ew.gn_backward(dy, held, stats, groups, gamma, act="relu", gate=clean[2])
+    want = ew.gn_backward(dy, clean[3], clean[1], groups, gamma, act="relu", gate=clean[2])
+    assert torch.equal(b[0][0], want[0][0]) and torch.equal(b[0][2], want[0][2])
+    assert a[0][1].isnan().any() and a[1][:2 * cg].isnan().all() and a[1][2 * cg:].isfinite().all() and a[2].isfinite().all()
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("rows, c", [(1, 1), (5, 8), (300, 16), (70, 24), (33, 30), (64, 32), (9, 33), (50, 40), (20, 160), (6, 650), (4099, 64),
+                                     (1, 1000)])
+def test_checkpoints_are_the_format(prec_name, rows, c):
+    _, ew = _ops(prec_name)
+    g = np.random.default_rng(rows * 1000 + c)
+    a = g.standard_normal((rows, c)) * 10.0 ** g.integers(-38, 38, (rows, 1))
+    a[g.random((rows, c)) < 0.1] = 0
+    x = torch.from_numpy(a.astype(np.float32)).cuda().to(ew.dtype)
+    top = torch.finfo(ew.dtype).max
+    if rows > 4:
+        x[0] = 0
+        x[1, 0] = top
+        x[2, c - 1] = float("nan")
+        x[3, 0] = -float("inf")
+        x[4] = torch.finfo(ew.dtype).tiny
+        # borders of the step: 127.5 steps and the values beside it, ties
+        edge = torch.tensor([127.5, 127.0, 0.5, 1.5, -2.5, 63.75, 126.5, -127.5], dtype=ew.dtype, device="cuda")
+        x[-1, :min(c, 8)] = edge[:min(c, 8)]
+    codes, scales = ew.ckpt_encode(x)
+    want = L.ckpt_encode(_np(x))
+    assert (codes.cpu().numpy() == want[0]).all() and (scales.cpu().numpy() == want[1]).all()
+    back = _np(ew.ckpt_decode((codes, scales)))
+    np.testing.assert_array_equal(back, L.ckpt_decode(*want))
+    again = ew.ckpt_encode(ew.ckpt_decode((codes, scales)))       # what is held is held exactly
+    np.testing.assert_array_equal(_np(ew.ckpt_decode(again)), back)
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("shape", [(3, 37, 30, 5), (3, 37, 40, 5), (1, 16390, 72, 8)], ids=str)
+def test_nothing_is_written_past_the_outputs(prec_name, shape):
+    """Every output and the scratch stand in buffers of their own with a pattern on both sides."""
+    B, ew = _ops(prec_name)
+    n, p, c, groups = shape
+    lib, prec = ew.lib, ew.precision
+    b = 2 if prec_name == "bf16" else 4
+    need, s = C.c_size_t(), B.fdg_gn_shape(n, p, c, groups)
+    assert lib.fdg_gn_scratch_bytes(prec, C.byref(s), C.byref(need)) == 0
+    sizes = dict(y=n * p * c * b, stats=2 * n * groups * 4, gate=n * p * -(-c // 8), codes=n * p * c, scales=n * p * -(-c // 32),
+                 scratch=need.value, dx=n * p * c * b, dgamma=4 * c, dbeta=4 * c)
+    pad = 512
+    bufs = {k: torch.full((v + 2 * pad,), 0x5A, dtype=torch.uint8, device="cuda") for k, v in sizes.items()}
+    at = {k: v.data_ptr() + pad for k, v in bufs.items()}
+    x, dy = _mk((n, p, c), 91, ew.dtype)[0], _mk((n, p, c), 92, ew.dtype)[0]
+    gamma, beta = (_f32(a) for a in _params(c, 93))
+    st = torch.cuda.current_stream().cuda_stream
+    assert lib.fdg_gn_forward(prec, C.byref(s), x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), None, B.FDG_ACT_RELU, EPS, at["y"],
+                              at["stats"], at["gate"], at["codes"], at["scales"], at["scratch"], need.value, st) == 0
+    for held in (False, True):
+        assert lib.fdg_gn_backward(prec, C.byref(s), dy.data_ptr(), None if held else x.data_ptr(), at["codes"] if held else None,
+                                   at["scales"] if held else None, at["stats"], gamma.data_ptr(), beta.data_ptr(), B.FDG_ACT_RELU,
+                                   None if held else at["y"], at["gate"] if held else None, None, at["dx"], at["dgamma"], at["dbeta"],
+                                   at["scratch"], need.value, st) == 0
+    torch.cuda.synchronize()
+    for k, v in bufs.items():
+        assert (v[:pad] == 0x5A).all() and (v[pad + sizes[k]:] == 0x5A).all(), k
+    y, stats, bits, kept = ew.gn_forward(x, groups, gamma, beta, act="relu", eps=EPS, gate=True, checkpoint=True)
+    for name, t in (("y", y), ("stats", stats), ("gate", bits), ("codes", kept[0]), ("scales", kept[1])):
+        assert torch.equal(bufs[name][pad:pad + sizes[name]], t.reshape(-1).view(torch.uint8)), name
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("shape", [(4, 1024, 160, 32), (2, 12000, 96, 8)], ids=str)
+def test_same_bits_again_on_streams_and_in_graphs(prec_name, shape):
+    """Two calls side by side on streams of their own, and captured and replayed on new inputs, give the bits of one call alone."""
+    _, ew = _ops(prec_name)
+    n, p, c, groups = shape
+    gamma, beta = (_f32(a) for a in _params(c, 101))
+
+    def both(x, dy):
+        y, stats, bits, held = ew.gn_forward(x, groups, gamma, beta, act="relu", gate=True, checkpoint=True)
+        return [y, stats, bits, *held, *ew.gn_backward(dy, held, stats, groups, gamma, beta, act="relu", gate=bits)]
+
+    ins = [(_mk((n, p, c), 102 + i, ew.dtype)[0], _mk((n, p, c), 112 + i, ew.dtype)[0]) for i in range(2)]
+    want = [both(*i) for i in ins]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ins]
+    for _ in range(5):
+        got = []
+        for s, i in zip(streams, ins):
+            with torch.cuda.stream(s):
+                got.append(both(*i))
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert all(torch.equal(a, b) for a, b in zip(g, w))
+    x, dy = ins[0][0].clone(), ins[0][1].clone()
+    graphs = []
+    for _ in range(2):                                   # two recorded graphs, replayed in turn
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = both(x, dy)
+        graphs.append((g, out))
+    for k in (1, 0, 1):
+        x.copy_(ins[k][0])
+        dy.copy_(ins[k][1])
+        for g, out in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for _, out in graphs:
+            assert all(torch.equal(a, b) for a, b in zip(out, want[k]))
+
+
+def test_binding_refuses_what_the_library_cannot_see():
+    B, ew = _ops("bf16")
+    x = torch.zeros((2, 4, 4, 16), dtype=torch.bfloat16, device="cuda")
+    one, zero = torch.ones(16, device="cuda"), torch.zeros(16, device="cuda")
+    y, stats, bits, held = ew.gn_forward(x, 4, one, zero, act="relu", gate=True, checkpoint=True)
+    dy = torch.zeros_like(x)
+    bad = [
+        lambda: ew.gn_forward(x.float(), 4, one, zero),
+        lambda: ew.gn_forward(x.cpu(), 4, one, zero),
+        lambda: ew.gn_forward(x.transpose(1, 3), 4, one[:4], zero[:4]),
+        lambda: ew.gn_forward(x, 3, one, zero),
+        lambda: ew.gn_forward(x, 4, one[:8], zero),
+        lambda: ew.gn_forward(x, 4, one, zero.bfloat16()),
+        lambda: ew.gn_forward(x, 4, one, zero, act="gelu"),
+        lambda: ew.gn_forward(x, 4, one, zero, act="silu", res=dy),
+        lambda: ew.gn_forward(x, 4, one, zero, act="silu", gate=True),
+        lambda: ew.gn_forward(x, 4, one, zero, res=dy[:1]),
+        lambda: ew.gn_forward(x[:0], 4, one, zero),
+        lambda: ew.gn_backward(dy, x, stats, 4, one, act="relu"),
+        lambda: ew.gn_backward(dy, x, stats, 4, one, act="relu", mask=y, gate=bits),
+        lambda: ew.gn_backward(dy, x, stats, 4, one, act="none", mask=y),
+        lambda: ew.gn_backward(dy, x, stats, 4, one, act="silu"),
+        lambda: ew.gn_backward(dy, x[:1], stats, 4, one),
+        lambda: ew.gn_backward(dy, (held[0], held[1][:1]), stats, 4, one),
+        lambda: ew.gn_backward(dy, (held[0].view(torch.uint8), held[1]), stats, 4, one),
+        lambda: ew.gn_backward(dy, x, stats[:1], 4, one),
+        lambda: ew.gn_backward(dy, x, stats, 4, one, act="relu", gate=bits[:1]),
+        lambda: ew.ckpt_encode(x.float()),
+        lambda: ew.ckpt_encode(x[..., ::2]),
+        lambda: ew.ckpt_encode(x[:0]),
+        lambda: ew.ckpt_decode((held[0], held[1].float())),
+        lambda: ew.ckpt_decode((held[0][:1], held[1])),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(B.FDGError):
+            call()
+            print("not refused:", i)
+
+
+def test_gradient_matches_differences():
+    """The fp32 calls against central differences of the float64 forward pass."""
+    _, ew = _ops("fp32")
+    n, p, c, groups, h = 2, 6, 12, 3, 1e-5
+    x, xo = _mk((n, p, c), 121, ew.dtype)
+    dy, dyo = _mk((n, p, c), 122, ew.dtype)
+    gamma, beta = _params(c, 123)
+    _, stats, _, _ = ew.gn_forward(x, groups, _f32(gamma), _f32(beta), act="silu")
+    grads = [_np(t) for t in ew.gn_backward(dy, x, stats, groups, _f32(gamma), _f32(beta), act="silu")]
+    for which, (arg, grad) in enumerate(zip((xo, gamma, beta), grads)):
+        for i in range(0, arg.size, 5):
+            side = []
+            for d in (-h, h):
+                a = arg.copy().reshape(-1)
+                a[i] += d
+                args = [xo, gamma, beta]
+                args[which] = a.reshape(arg.shape)
+                side.append((L.groupnorm_forward(args[0], groups, args[1], args[2], EPS, "silu")[0] * dyo).sum())
+            # differences are good to 1e-7 here (h^2 and 1e-16/h); fp32 to K of terms of order 10
+            assert abs((side[1] - side[0]) / (2 * h) - grad.reshape(-1)[i]) <= 1e-7 + 20 * K, (which, i)
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 values: the last image's results are those of the image alone."""
+    _, ew = _ops("bf16")
+    n, p, c, groups = 17, 1 << 20, 128, 8                         # 2.28e9 values
+    x = torch.empty((n, p, c), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for i in range(n):
+        x[i] = torch.randn((p, c), generator=g, device="cuda")
+    gamma, beta = (_f32(a) for a in _params(c, 131))
+    y, stats, bits, held = ew.gn_forward(x, groups, gamma, beta, act="relu", gate=True, checkpoint=True)
+    last = ew.gn_forward(x[-1:].clone(), groups, gamma, beta, act="relu", gate=True, checkpoint=True)
+    assert torch.equal(y[-1:], last[0]) and torch.equal(stats[:, -1:], last[1]) and torch.equal(bits[-1:], last[2])
+    assert torch.equal(held[0][-1:], last[3][0]) and torch.equal(held[1][-1:], last[3][1])
+    apart = ew.ckpt_encode(x)
+    assert torch.equal(apart[0][-1:], last[3][0]) and torch.equal(apart[1][-1:], last[3][1])
+    del apart
+    assert torch.equal(ew.ckpt_decode(held)[-1:], ew.ckpt_decode(last[3]))
+    dx = ew.gn_backward(y, held, stats, groups, gamma, act="relu", gate=bits)[0]
+    one = ew.gn_backward(y[-1:].clone(), last[3], last[1], groups, gamma, act="relu", gate=last[2])[0]
+    assert torch.equal(dx[-1:], one)
+
+
+@pytest.mark.parametrize("c, groups", [(32, 4), (160, 32)])
+def test_a_block_with_its_activations_held_in_8_bits(c, groups):
+    """The operators as a residual branch uses them: conv -> group norm + ReLU -> conv forward, keeping x and the ReLU's output
+    in 8 bits and the gate in bits, and back: data gradient, group norm from the checkpoint, weight gradients from decoded
+    checkpoints.  Each step against its float64 definition on the step's own inputs."""
+    B, ew = _ops("bf16")
+    conv = B.ConvOps(B.FDG_BF16_TC)
+    n, h, w = 4, 16, 16
+    s = B.fdg_conv_shape(n, h, w, c, c, 3, 1, 1)
+    x0 = _mk((n, h, w, c), 141, ew.dtype)[0]
+    w1, w2 = (_mk((c, 3, 3, c), 142 + i, ew.dtype, (2 / (9 * c)) ** 0.5)[0] for i in range(2))
+    gamma, beta = _params(c, 144)
+    x1 = conv.forward(s, x0, w1)
+    y1, stats, bits, held1 = ew.gn_forward(x1, groups, _f32(gamma), _f32(beta), act="relu", gate=True, checkpoint=True)
+    held_y = ew.ckpt_encode(y1)
+    dy2 = _mk((n, h, w, c), 145, ew.dtype, 0.1)[0]
+
+    yo, _, st = L.groupnorm_forward(_np(x1).reshape(n, h * w, c), groups, gamma, beta, EPS, "relu")
+    assert np.abs(_np(y1).reshape(yo.shape) - yo).max() <= _half_step(ew.dtype) * np.abs(yo).max() + 16 * K
+    # weight gradient of the second convolution: its input as held, which bf16 holds exactly
+    y1h = ew.ckpt_decode(held_y)
+    assert torch.equal(y1h.float(), held_y[0].float() * (held_y[1].int() << 23).view(torch.float32).repeat_interleave(32, -1)[..., :c])
+    dw2 = conv.wgrad(s, y1h, dy2)
+    ref = torch.nn.grad.conv2d_weight(y1h.double().permute(0, 3, 1, 2), (c, c, 3, 3), dy2.double().permute(0, 3, 1, 2), padding=1).permute(0, 2, 3, 1)
+    assert float((dw2.double() - ref).norm() / ref.norm()) <= 1e-5
+    # against the tensor itself: dy is independent of what the 8 bits left out, so the weight gradient is as far off as they are
+    full = conv.wgrad(s, y1, dy2)
+    assert float((dw2 - full).norm() / full.norm()) <= 2 * float((y1h.float() - y1.float()).norm() / y1.float().norm())
+    dy1 = conv.dgrad(s, dy2, w2, conv.flip_weights(s, w2))
+    dx1, dgamma, dbeta = ew.gn_backward(dy1, held1, stats, groups, _f32(gamma), act="relu", gate=bits)
+    heldo = L.ckpt_decode(held1[0].cpu().numpy().reshape(-1, c), held1[1].cpu().numpy().reshape(n * h * w, -1)).reshape(n, h * w, c)
+    dz = _np(dy1).reshape(n, h * w, c) * (_np(y1).reshape(n, h * w, c) > 0)
+    dxo, dgo, dbo = L.groupnorm_backward(dz, heldo, _np(stats), groups, gamma)
+    for got, want in ((dx1.reshape(n, h * w, c), dxo), (dgamma, dgo), (dbeta, dbo)):
+        assert np.abs(_np(got) - want).max() <= (_half_step(ew.dtype) + 4 * K) * np.abs(want).max()
+    exact = ew.gn_backward(dy1, x1, stats, groups, _f32(gamma), act="relu", mask=y1)
+    off = float((ew.ckpt_decode(held1).float() - x1.float()).norm() / x1.float().norm())
+    for got, want in zip((dx1, dgamma, dbeta), exact):
+        assert float((got.float() - want.float()).norm() / want.float().norm()) <= 2 * off + _half_step(ew.dtype)
+    assert not conv.timed_out()
