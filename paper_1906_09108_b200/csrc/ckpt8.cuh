@@ -37,25 +37,47 @@ __device__ __forceinline__ CkptScale ckpt_scale(uint32_t top) {
   s.inv_step = top >= 0x7F800000u ? 0.f : __uint_as_float((254u - k) << 23);
   return s;
 }
-__device__ __forceinline__ uint32_t ckpt_top(const float (&v)[8]) {
-  uint32_t m = 0;
+// The largest magnitude of 8 values, in the storage type's own bits where it has 16 (two at a time), as fp32 bits.
+__device__ __forceinline__ uint32_t ckpt_top(const Raw8<__nv_bfloat16>& r) {
+  const uint32_t m = __vmaxu2(__vmaxu2(r.q[0].x & 0x7FFF7FFFu, r.q[0].y & 0x7FFF7FFFu), __vmaxu2(r.q[0].z & 0x7FFF7FFFu, r.q[0].w & 0x7FFF7FFFu));
+  return max(m & 0xFFFF0000u, m << 16);
+}
+__device__ __forceinline__ uint32_t ckpt_top(const Raw8<float>& r) {
+  float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  return m;
+  for (int j = 0; j < 2; ++j) {
+    m = max_nan(m, max_nan(fabsf(__uint_as_float(r.q[j].x)), fabsf(__uint_as_float(r.q[j].y))));
+    m = max_nan(m, max_nan(fabsf(__uint_as_float(r.q[j].z)), fabsf(__uint_as_float(r.q[j].w))));
+  }
+  return __float_as_uint(m);
 }
 // x / step rounded to the nearest even integer, in the low byte: the product is exact, and adding 1.5 * 2^23 rounds it.
+constexpr float kCkptRound = 12582912.f;
 __device__ __forceinline__ uint32_t ckpt_code(float x, const CkptScale& s) {
   float t = x * s.inv_step;
   if (s.clamp) {
     if (s.byte == 255u) return 0;
     t = fminf(fmaxf(t, -127.f), 127.f);
   }
-  return __float_as_uint(t + 12582912.f);
+  return __float_as_uint(t + kCkptRound);
 }
-__device__ __forceinline__ uint2 ckpt_codes(const float (&v)[8], const CkptScale& s) {
+__device__ __forceinline__ uint2 ckpt_codes(const F8& v, const CkptScale& s) {
   uint32_t q[8];
+  const f32x2 inv = pair(s.inv_step), round = pair(kCkptRound);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = ckpt_code(v[i], s);
+  for (int j = 0; j < 4; ++j) {
+    const float2 t = halves(fma2(v.p[j], inv, round));
+    q[2 * j] = __float_as_uint(t.x);
+    q[2 * j + 1] = __float_as_uint(t.y);
+  }
+  if (s.clamp) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 t = halves(v.p[j]);
+      q[2 * j] = ckpt_code(t.x, s);
+      q[2 * j + 1] = ckpt_code(t.y, s);
+    }
+  }
   uint2 r;
   r.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
   r.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
@@ -64,14 +86,24 @@ __device__ __forceinline__ uint2 ckpt_codes(const float (&v)[8], const CkptScale
 __device__ __forceinline__ float ckpt_step(uint32_t byte) {
   return byte == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(byte << 23);
 }
-// code + 128 in the mantissa of 2^23, then the offset off: an integer conversion on the fp32 pipe.
-__device__ __forceinline__ void ckpt_values(uint2 codes, float step, float (&v)[8]) {
+// The codes as fp32 numbers: code + 128 in the mantissa of 2^23, then the offset off, an integer conversion on the fp32 pipe.
+__device__ __forceinline__ F8 ckpt_numbers(uint2 codes) {
   const uint32_t lo = codes.x ^ 0x80808080u, hi = codes.y ^ 0x80808080u;
+  const f32x2 off = pair(-8388736.f);
+  F8 f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = (__uint_as_float(__byte_perm(lo, 0x4B000000u, 0x7540u + i)) - 8388736.f) * step;
-    v[4 + i] = (__uint_as_float(__byte_perm(hi, 0x4B000000u, 0x7540u + i)) - 8388736.f) * step;
+  for (int j = 0; j < 2; ++j) {
+    f.p[j] = add2(pair(__uint_as_float(__byte_perm(lo, 0x4B000000u, 0x7540u + 2 * j)), __uint_as_float(__byte_perm(lo, 0x4B000000u, 0x7541u + 2 * j))), off);
+    f.p[2 + j] = add2(pair(__uint_as_float(__byte_perm(hi, 0x4B000000u, 0x7540u + 2 * j)), __uint_as_float(__byte_perm(hi, 0x4B000000u, 0x7541u + 2 * j))), off);
   }
+  return f;
+}
+__device__ __forceinline__ F8 ckpt_values(uint2 codes, float step) {
+  F8 f = ckpt_numbers(codes);
+  const f32x2 st = pair(step);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) f.p[j] = mul2(f.p[j], st);
+  return f;
 }
 
 // Bytes of 8 codes at element offset `off`; VEC: one 8-byte access, else the first `left`.
@@ -125,11 +157,9 @@ __global__ void __launch_bounds__(kCkptThreads) ckpt_encode_kernel(const T* __re
 #pragma unroll
   for (int u = 0; u < kCkptUnroll; ++u) {
     const size_t i = first + (size_t)u * kCkptThreads;
-    float v[8];
-    raw8_to_f(raw[u], v);
-    const CkptScale s = ckpt_scale(ckpt_top_of_lanes(ckpt_top(v), lanes));
+    const CkptScale s = ckpt_scale(ckpt_top_of_lanes(ckpt_top(raw[u]), lanes));
     if (i < vecs) {
-      *reinterpret_cast<uint2*>(codes + i * 8) = ckpt_codes(v, s);
+      *reinterpret_cast<uint2*>(codes + i * 8) = ckpt_codes(raw8_to_f8(raw[u]), s);
       if ((i & (unsigned)(lanes - 1)) == 0) scales[i >> shift] = (uint8_t)s.byte;
     }
   }
@@ -184,9 +214,7 @@ __global__ void __launch_bounds__(kCkptThreads) ckpt_decode_kernel(const int8_t*
   for (int u = 0; u < kCkptUnroll; ++u) {
     const size_t i = first + (size_t)u * kCkptThreads;
     if (i >= vecs) break;
-    float v[8];
-    ckpt_values(q[u], ckpt_step(k[u]), v);
-    raw8_store<T, true>(x + i * 8, 8, v);
+    raw8_put<T, true>(x + i * 8, 8, f8_to_raw8<T>(ckpt_values(q[u], ckpt_step(k[u]))));
   }
 }
 // Decode, any row length and alignment: a thread takes values.

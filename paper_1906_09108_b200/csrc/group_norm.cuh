@@ -51,15 +51,22 @@ struct Geom {
 };
 
 // ---- device helpers -------------------------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ float silu(float z);
-template <> __device__ __forceinline__ float silu<float>(float z) { return z / (1.f + expf(-z)); }
-template <> __device__ __forceinline__ float silu<__nv_bfloat16>(float z) { return __fdividef(z, 1.f + __expf(-z)); }
-template <typename T> __device__ __forceinline__ float silu_slope(float z) {
-  const float s = sizeof(T) == 4 ? 1.f / (1.f + expf(-z)) : __fdividef(1.f, 1.f + __expf(-z));
-  return s * (1.f + z * (1.f - s));
+// 1/(1 + exp(-z)).  For tensors in 16 bits from the approximate exponential and reciprocal (relative error below 2^-20 for
+// |z| < 16, growing with |z| as the rounding of z*log2(e) does), for fp32 ones from expf and a division.
+template <typename T> __device__ __forceinline__ float sigmoid(float z) {
+  if constexpr (sizeof(T) == 2) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return r;
+  } else {
+    return 1.f / (1.f + expf(-z));
+  }
 }
-// NaN stays NaN.
-__device__ __forceinline__ float relu(float z) { return z < 0.f ? 0.f : z; }
+template <typename T> __device__ __forceinline__ float silu_slope(float z) {
+  const float s = sigmoid<T>(z);
+  return s * fmaf(z, 1.f - s, 1.f);
+}
 
 __device__ __forceinline__ void copy16_async(void* smem, const void* gmem) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem) : "memory");
@@ -107,6 +114,17 @@ struct Place {
   }
   __device__ __forceinline__ int channel(int i) const { return i < left ? c0 + i : c0; }
 };
+
+// take(i, channel, group) for the 8 channels of a column; those past the last channel stand in for the first.
+template <typename Take> __device__ __forceinline__ void each_channel(const Place& at, int Cg, Take take) {
+  const int first = at.c0 / Cg;
+  int s = first, rem = at.c0 - first * Cg;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    take(i, at.channel(i), i < at.left ? s : first);
+    if (++rem == Cg) { rem = 0; ++s; }
+  }
+}
 
 // red[r][8 * cols] = the 8 sums of each thread.
 __device__ __forceinline__ void put_sums(float* red, const Geom& g, const Place& at, const float (&v)[8]) {
@@ -157,97 +175,170 @@ template <typename T> struct Forward {
   int ckpt_lanes;
 };
 
-// Sums over this CTA's `count` pixels in `slots`: done(set, mean, sum of squared deviations from that mean) for sets of `size`
+// Moments of this CTA's `count` pixels in `slots`: done(set, mean, sum of squared deviations from that mean) for sets of `size`
 // consecutive channels.  `red`: 2048 floats, `mean`: a float per set.
+// A thread sums its values of a channel, and their squares, less the first of them: the square of the distance from that value
+// to the mean is at most n times the spread of the n values, so what cancels when the sum is taken out again is at most n times
+// the result, whatever the offset (n is a few dozen at most).  The threads' moments are then brought about the CTA's mean.
 template <typename T, typename Done>
 __device__ __forceinline__ void cta_moments(const Geom& g, const Place& at, const Slots<T>& slots, int count, int sets, int size, int lanes,
                                             float* red, float* mean, Done done) {
   const int width = g.cols * 8;
   const float inv = count > 0 ? 1.f / ((float)count * (float)size) : 0.f;
-  float a[8];
+  F8 first, sum, square;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) a[i] = 0.f;
-  if (at.active)
+  for (int j = 0; j < 4; ++j) first.p[j] = sum.p[j] = square.p[j] = 0;
+  int n = 0;
+  if (at.active && at.r < count) {
+    F8 less;
+    first = raw8_to_f8(slots.get(0));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) less.p[j] = mul2(first.p[j], pair(-1.f));
+    n = 1;
 #pragma unroll 4
-    for (int k = 0; k < g.iters; ++k) {
+    for (int k = 1; k < g.iters; ++k) {
       if (at.r + k * g.rp >= count) break;
-      float v[8];
-      raw8_to_f(slots.get(k), v);
+      const F8 x = raw8_to_f8(slots.get(k));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) a[i] += v[i];
+      for (int j = 0; j < 4; ++j) {
+        const f32x2 d = add2(x.p[j], less.p[j]);
+        sum.p[j] = add2(sum.p[j], d);
+        square.p[j] = fma2(d, d, square.p[j]);
+      }
+      ++n;
     }
-  put_sums(red, g, at, a);
+  }
+  const float fn = (float)n, over = n > 0 ? 1.f / fn : 0.f;
+  float a[8], mu[8];                  // the thread's mean and squared deviations
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = halves(first.p[j]), s1 = halves(sum.p[j]), s2 = halves(square.p[j]);
+    mu[2 * j] = fmaf(s1.x, over, f.x);
+    mu[2 * j + 1] = fmaf(s1.y, over, f.y);
+    a[2 * j] = max_nan(fmaf(-s1.x * over, s1.x, s2.x), 0.f);
+    a[2 * j + 1] = max_nan(fmaf(-s1.y * over, s1.y, s2.y), 0.f);
+  }
+  float t[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = mu[i] * fn;
+  put_sums(red, g, at, t);
   __syncthreads();
   auto value = [&](int r, int c) { return red[r * width + c]; };
-  add_sets(g.rp, sets, size, lanes, value, [&](int s, float sum) { mean[s] = sum * inv; });
+  add_sets(g.rp, sets, size, lanes, value, [&](int s, float total) { mean[s] = total * inv; });
   __syncthreads();
-  float mu[8];
+  if (at.active) {
+    int s = at.col * 8 / size, rem = at.col * 8 - s * size;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    mu[i] = mean[min((at.col * 8 + i) / size, sets - 1)];
-    a[i] = 0.f;
-  }
-  if (at.active)
-#pragma unroll 4
-    for (int k = 0; k < g.iters; ++k) {
-      if (at.r + k * g.rp >= count) break;
-      float v[8];
-      raw8_to_f(slots.get(k), v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { const float d = v[i] - mu[i]; a[i] += d * d; }
+    for (int i = 0; i < 8; ++i) {
+      const float d = mu[i] - mean[min(s, sets - 1)];
+      t[i] = fmaf(fn * d, d, a[i]);
+      if (++rem == size) { rem = 0; ++s; }
     }
-  put_sums(red, g, at, a);
+    put_sums(red, g, at, t);
+  }
   __syncthreads();
-  add_sets(g.rp, sets, size, lanes, value, [&](int s, float sum) { done(s, mean[s], sum); });
+  add_sets(g.rp, sets, size, lanes, value, [&](int s, float total) { done(s, mean[s], total); });
 }
 
-// y (and the gate's bits, and x in 8 bits) of this CTA's pixels: fetch(k) gives the thread's k-th vector of x.
-// Every lane takes every turn, since the lanes of a block of 32 channels exchange its maximum.
-template <typename T, bool VEC, typename Fetch>
-__device__ __forceinline__ void emit(const Forward<T>& p, const Place& at, size_t row0, int count, const float (&mean)[8],
-                                     const float (&scale)[8], const float (&shift)[8], Fetch fetch) {
-  const Geom& g = p.g;
-  const int all_cols = (g.C + 7) >> 3;
-#pragma unroll 2
-  for (int k = 0; k < g.iters; ++k) {
-    const int pixel = at.r + k * g.rp;
-    const bool live = at.active && pixel < count;
-    const size_t row = row0 + pixel, off = row * g.C + at.c0;
-    float v[8], z[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    if (live) {
-      raw8_to_f(fetch(k, off), v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = fmaf(v[i] - mean[i], scale[i], shift[i]);
-      if (p.res) {
-        float r[8];
-        raw8_to_f(raw8_load<T, VEC>(p.res + off, at.left), r);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] += r[i];
-      }
-      if (p.act == ACT_RELU) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = relu(z[i]);
-      } else if (p.act == ACT_SILU) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = silu<T>(z[i]);
-      }
-      const Raw8<T> out = raw8_of<T>(z);
-      raw8_put<T, VEC>(p.y + off, at.left, out);
-      if (p.gate) {
-        uint32_t b = 0;
-        raw8_to_f(out, z);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) b |= (i < at.left && z[i] > 0.f ? 1u : 0u) << i;
-        p.gate[row * all_cols + (at.c0 >> 3)] = (uint8_t)b;
-      }
+// What a thread multiplies its 8 channels by: scale = gamma*rstd and shift = beta, and the mean with its sign turned.  16-bit
+// tensors take the mean into the shift: that rounds |mean|*scale to 24 bits where x itself has 8.
+template <typename T> struct Affine {
+  static constexpr bool kFolded = sizeof(T) == 2;
+  f32x2 scale[4], shift[4], less[kFolded ? 1 : 4];
+  __device__ __forceinline__ void set(int j, float2 mean, float2 sc, float2 sh) {
+    scale[j] = pair(sc.x, sc.y);
+    if constexpr (kFolded) {
+      shift[j] = pair(fmaf(-mean.x, sc.x, sh.x), fmaf(-mean.y, sc.y, sh.y));
+    } else {
+      shift[j] = pair(sh.x, sh.y);
+      less[j] = pair(-mean.x, -mean.y);
     }
-    if (p.codes) {
-      const CkptScale s = ckpt_scale(ckpt_top_of_lanes(ckpt_top(v), p.ckpt_lanes));
+  }
+  __device__ __forceinline__ f32x2 of(int j, f32x2 x) const {
+    if constexpr (kFolded) return fma2(x, scale[j], shift[j]); else return fma2(add2(x, less[j]), scale[j], shift[j]);
+  }
+};
+
+// Bits of [y > 0] of 8 stored values.
+__device__ __forceinline__ uint32_t positive_bits(const Raw8<__nv_bfloat16>& y) {
+  const uint32_t w[4] = {y.q[0].x, y.q[0].y, y.q[0].z, y.q[0].w};
+  uint32_t b = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&w[j]);
+    b |= __hgt2_mask(v, __nv_bfloat162{__nv_bfloat16_raw{0}, __nv_bfloat16_raw{0}}) & ((1u << (2 * j)) | (1u << (2 * j + 17)));
+  }
+  return (b | b >> 16) & 0xFFu;
+}
+__device__ __forceinline__ uint32_t positive_bits(const Raw8<float>& y) {
+  const uint32_t w[8] = {y.q[0].x, y.q[0].y, y.q[0].z, y.q[0].w, y.q[1].x, y.q[1].y, y.q[1].z, y.q[1].w};
+  uint32_t b = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b |= (__uint_as_float(w[i]) > 0.f ? 1u : 0u) << i;
+  return b;
+}
+
+// y (and the gate's bits, and x in 8 bits) of this CTA's pixels: fetch(k, offset) gives the thread's k-th vector of x; U of them
+// (and of res) are fetched before the first is used.  Every lane takes every turn, since the lanes of a block of 32 channels
+// exchange its maximum.  Offsets inside a CTA's pixels fit 32 bits.
+template <typename T, bool VEC, int U, typename Fetch>
+__device__ __forceinline__ void emit(const Forward<T>& p, const Place& at, size_t row0, int count, const Affine<T>& affine, Fetch fetch) {
+  const Geom& g = p.g;
+  const int all_cols = (g.C + 7) >> 3, per_row = (g.C + kCkptBlock - 1) / kCkptBlock;
+  const size_t row = row0 + at.r, off = row * g.C + at.c0;
+  T* const y = p.y + off;
+  const T* const res = p.res + off;
+  int8_t* const codes = p.codes + off;
+  uint8_t* const gate = p.gate + (row * all_cols + (at.c0 >> 3));
+  uint8_t* const scales = p.scales + (row * per_row + at.c0 / kCkptBlock);
+  const bool has_res = p.res != nullptr, has_gate = p.gate != nullptr, has_codes = p.codes != nullptr;
+  const bool leads = (at.col & (p.ckpt_lanes - 1)) == 0;
+  const uint32_t step = (uint32_t)g.rp * g.C;
+  for (int k0 = 0; k0 < g.iters; k0 += U) {
+    Raw8<T> xs[U], rs[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u;
+      const bool live = at.active && at.r + k * g.rp < count;
+      xs[u] = live ? fetch(k, (uint32_t)k * step) : Raw8<T>{};
+      if (has_res) rs[u] = live ? raw8_load<T, VEC>(res + (uint32_t)k * step, at.left) : Raw8<T>{};
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u;
+      const bool live = at.active && at.r + k * g.rp < count;
+      const uint32_t o = (uint32_t)k * step;
+      const F8 x = raw8_to_f8(xs[u]);
       if (live) {
-        store_codes<VEC>(p.codes, off, at.left, ckpt_codes(v, s));
-        if ((at.col & (p.ckpt_lanes - 1)) == 0) p.scales[row * ((g.C + kCkptBlock - 1) / kCkptBlock) + at.c0 / kCkptBlock] = (uint8_t)s.byte;
+        F8 z;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z.p[j] = affine.of(j, x.p[j]);
+        if (has_res) {
+          const F8 r = raw8_to_f8(rs[u]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) z.p[j] = add2(z.p[j], r.p[j]);
+        }
+        if (p.act == ACT_RELU) {
+          const Raw8<T> out = f8_to_raw8<T, true>(z);
+          raw8_put<T, VEC>(y + o, at.left, out);
+          if (has_gate) gate[(uint32_t)(k * g.rp) * all_cols] = (uint8_t)(positive_bits(out) & (VEC ? 0xFFu : (1u << at.left) - 1));
+        } else {
+          if (p.act == ACT_SILU) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float2 h = halves(z.p[j]);
+              z.p[j] = mul2(z.p[j], pair(sigmoid<T>(h.x), sigmoid<T>(h.y)));
+            }
+          }
+          raw8_put<T, VEC>(y + o, at.left, f8_to_raw8<T>(z));
+        }
+      }
+      if (has_codes) {
+        const CkptScale s = ckpt_scale(ckpt_top_of_lanes(ckpt_top(xs[u]), p.ckpt_lanes));
+        if (live) {
+          store_codes<VEC>(codes + o, 0, at.left, ckpt_codes(x, s));
+          if (leads) scales[(uint32_t)(k * g.rp) * per_row] = (uint8_t)s.byte;
+        }
       }
     }
   }
@@ -255,12 +346,12 @@ __device__ __forceinline__ void emit(const Forward<T>& p, const Place& at, size_
 
 // The resident form: blockIdx.x = image * parts + share of its pixels, a cluster per image.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_constant__ Forward<T> p) {
+__global__ void __launch_bounds__(kThreads, 2) forward_kernel(const __grid_constant__ Forward<T> p) {
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
   float* red = reinterpret_cast<float*>(smem + (size_t)g.iters * Slots<T>::Q * kThreads);      // [2048]
   float* own = red + kThreads * 8;            // mean [G], squared deviations [G] of this CTA's pixels
-  float* mom = own + 2 * g.G;                 // mean [G], rstd [G] of the image
+  float2* mom = reinterpret_cast<float2*>(own + 2 * g.G);                 // mean, rstd [G] of the image
   const int rank = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
   const int p0 = rank * g.pix, count = max(0, min(g.pix, g.P - p0));
   const size_t row0 = (size_t)n * g.P + p0;
@@ -271,51 +362,50 @@ __global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_const
     const T* src = p.x + (row0 + at.r) * g.C + at.c0;
     for (int k = 0; k < g.iters && at.r + k * g.rp < count; ++k) slots.template fetch<VEC>(k, src + (size_t)k * g.rp * g.C, at.left);
   }
-  float scale[8], shift[8], mean[8];
+  float scale[8], shift[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) { scale[i] = p.gamma[at.channel(i)]; shift[i] = p.beta[at.channel(i)]; }
   copies_done();
   cta_moments(g, at, slots, count, g.G, g.Cg, g.lanes_g, red, own, [&](int s, float, float m2) { own[g.G + s] = m2; });
   cg::cluster_group cluster = cg::this_cluster();
   cluster.sync();
-  // Chan: the CTAs' moments about the image's mean
-  const double m = (double)g.P * g.Cg;
-  for (int s = threadIdx.x; s < g.G; s += kThreads) {
-    double mu = 0.0, m2 = 0.0;
-    for (int j = 0; j < g.parts; ++j) {
-      const double cnt = (double)max(0, min(g.pix, g.P - j * g.pix)) * g.Cg;
-      mu += cnt * (double)cluster.map_shared_rank(own, j)[s];
-    }
-    mu /= m;
-    for (int j = 0; j < g.parts; ++j) {
-      const double cnt = (double)max(0, min(g.pix, g.P - j * g.pix)) * g.Cg;
-      const float* other = cluster.map_shared_rank(own, j);
-      const double d = (double)other[s] - mu;
-      m2 += (double)other[g.G + s] + cnt * d * d;
-    }
-    const float rstd = (float)(1.0 / sqrt(m2 / m + (double)p.eps));
-    mom[s] = (float)mu;
-    mom[g.G + s] = rstd;
-    if (rank == 0) {
-      p.stats[(size_t)n * g.G + s] = (float)mu;
-      p.stats[(size_t)(g.N + n) * g.G + s] = rstd;
+  // Chan: the CTAs' moments about the image's mean; a lane per CTA and group
+  const int j = threadIdx.x & (g.parts - 1);
+  const float in_j = (float)max(0, min(g.pix, g.P - j * g.pix)), inv_p = 1.f / (float)g.P;
+  const float* other = cluster.map_shared_rank(own, j);
+  for (int s0 = 0; s0 < g.G; s0 += kThreads / g.parts) {
+    const int s = s0 + threadIdx.x / g.parts;
+    const float mean_j = s < g.G ? other[s] : 0.f, m2_j = s < g.G ? other[g.G + s] : 0.f;
+    float mu = mean_j * (in_j * inv_p);
+    for (int o = g.parts >> 1; o > 0; o >>= 1) mu += __shfl_xor_sync(0xffffffffu, mu, o);
+    const float d = mean_j - mu;
+    float var = fmaf(in_j * d, d, m2_j / (float)g.Cg);
+    for (int o = g.parts >> 1; o > 0; o >>= 1) var += __shfl_xor_sync(0xffffffffu, var, o);
+    const float rstd = 1.f / sqrtf(fmaf(var, inv_p, p.eps));
+    if (j == 0 && s < g.G) {
+      mom[s] = make_float2(mu, rstd);
+      if (rank == 0) {
+        p.stats[(size_t)n * g.G + s] = mu;
+        p.stats[(size_t)(g.N + n) * g.G + s] = rstd;
+      }
     }
   }
   cg::cluster_group::arrival_token token = cluster.barrier_arrive();      // this CTA reads its neighbours' sums no more
   __syncthreads();
+  Affine<T> affine;
+  float2 m[8];
+  each_channel(at, g.Cg, [&](int i, int, int s) { m[i] = mom[s]; });
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int s = at.channel(i) / g.Cg;
-    mean[i] = mom[s];
-    scale[i] *= mom[g.G + s];
-  }
-  emit<T, VEC>(p, at, row0, count, mean, scale, shift, [&](int k, size_t) { return slots.get(k); });
+  for (int i = 0; i < 4; ++i)
+    affine.set(i, make_float2(m[2 * i].x, m[2 * i + 1].x), make_float2(scale[2 * i] * m[2 * i].y, scale[2 * i + 1] * m[2 * i + 1].y),
+               make_float2(shift[2 * i], shift[2 * i + 1]));
+  emit<T, VEC, 2>(p, at, row0, count, affine, [&](int k, uint32_t) { return slots.get(k); });
   cluster.barrier_wait(std::move(token));                                 // nor do they read its own
 }
 
 // Streamed, first pass: mean and squared deviations of each channel over a chunk of pixels.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads, 3) moments_kernel(const __grid_constant__ Forward<T> p) {
+__global__ void __launch_bounds__(kThreads, 2) moments_kernel(const __grid_constant__ Forward<T> p) {
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
   float* red = reinterpret_cast<float*>(smem + (size_t)g.iters * Slots<T>::Q * kThreads);
@@ -387,23 +477,29 @@ __global__ void __launch_bounds__(1024) combine_kernel(const __grid_constant__ F
 
 // Streamed, last pass: y from x and the statistics, the last chunks first.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads, 3) apply_kernel(const __grid_constant__ Forward<T> p) {
+__global__ void __launch_bounds__(kThreads, 2) apply_kernel(const __grid_constant__ Forward<T> p) {
   const Geom& g = p.g;
   const int block = gridDim.x - 1 - blockIdx.x, part = block % g.parts, n = block / g.parts;
   const int p0 = part * g.pix, count = min(g.pix, g.P - p0);
   const size_t row0 = (size_t)n * g.P + p0;
   Place at(g, blockIdx.y);
   at.active = at.active && at.left > 0;
-  float scale[8], shift[8], mean[8];
+  if (!at.active) at.c0 = 0;
+  Affine<T> affine;
+  float mean[8], scale[8], shift[8];
   grid_dependency_wait();
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int c = at.active ? at.channel(i) : 0, s = c / g.Cg;
+  each_channel(at, g.Cg, [&](int i, int c, int s) {
+    c = at.active ? c : 0;
+    s = at.active ? s : 0;
     mean[i] = p.stats[(size_t)n * g.G + s];
     scale[i] = p.gamma[c] * p.stats[(size_t)(g.N + n) * g.G + s];
     shift[i] = p.beta[c];
-  }
-  emit<T, VEC>(p, at, row0, count, mean, scale, shift, [&](int, size_t off) { return raw8_load<T, VEC>(p.x + off, at.left); });
+  });
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    affine.set(j, make_float2(mean[2 * j], mean[2 * j + 1]), make_float2(scale[2 * j], scale[2 * j + 1]), make_float2(shift[2 * j], shift[2 * j + 1]));
+  const T* x = p.x + (row0 + at.r) * g.C + at.c0;
+  emit<T, VEC, sizeof(T) == 2 ? 4 : 2>(p, at, row0, count, affine, [&](int, uint32_t o) { return raw8_load<T, VEC>(x + o, at.left); });
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------
@@ -430,64 +526,103 @@ template <typename T, bool CK> struct Held {
   Raw8<T> dy;
   Raw8<T> x;
   uint2 codes;
-  uint32_t scale, open;       // scale byte of the codes, bits of the ReLU gate
+  uint32_t scale, open;       // scale byte of the codes, bits of the gate (all set without ReLU)
 };
 
 template <typename T, bool VEC> __device__ __forceinline__ uint32_t open_bits(const Backward<T>& p, const Place& at, size_t row) {
   if (p.gate) return p.gate[row * ((p.g.C + 7) >> 3) + (at.c0 >> 3)];
-  float m[8];
-  raw8_to_f(raw8_load<T, VEC>(p.mask + row * p.g.C + at.c0, at.left), m);
-  uint32_t b = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) b |= (m[i] > 0.f ? 1u : 0u) << i;
-  return b;
+  return positive_bits(raw8_load<T, VEC>(p.mask + row * p.g.C + at.c0, at.left));
 }
 __device__ __forceinline__ size_t scale_index(const Geom& g, const Place& at, size_t row) {
   return row * ((g.C + kCkptBlock - 1) / kCkptBlock) + at.c0 / kCkptBlock;
 }
 
-// A thread's 8 channels: mean, gamma * rstd, beta.
+// A thread's 8 channels: the mean with its sign turned, gamma * rstd, beta.
 struct Channels {
-  float mean[8], scale[8], shift[8];
+  f32x2 less[4], scale[4], shift[4];
 };
 
-// dz and x - mean of one vector.
+// dz where the gate's bits are set, 0 elsewhere.  A product by 0x10204080 moves 4 bits to the tops of 4 bytes, from where a
+// byte permutation spreads each over 16 bits.
+template <uint32_t SELECT> __device__ __forceinline__ uint32_t spread_signs(uint32_t v) {
+  uint32_t d;
+  asm("prmt.b32 %0, %1, %1, %2;" : "=r"(d) : "r"(v), "n"(SELECT));      // (__byte_perm has no sign-spreading selectors)
+  return d;
+}
+__device__ __forceinline__ Raw8<__nv_bfloat16> opened(const Raw8<__nv_bfloat16>& dy, uint32_t open) {
+  const uint32_t lo = (open & 15u) * 0x10204080u, hi = (open >> 4) * 0x10204080u;
+  Raw8<__nv_bfloat16> r;
+  r.q[0] = make_uint4(dy.q[0].x & spread_signs<0x9988>(lo), dy.q[0].y & spread_signs<0xBBAA>(lo),
+                      dy.q[0].z & spread_signs<0x9988>(hi), dy.q[0].w & spread_signs<0xBBAA>(hi));
+  return r;
+}
+__device__ __forceinline__ Raw8<float> opened(const Raw8<float>& dy, uint32_t open) {
+  Raw8<float> r;
+  const uint32_t* from = reinterpret_cast<const uint32_t*>(&dy);
+  uint32_t* to = reinterpret_cast<uint32_t*>(&r);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) to[i] = (open >> i & 1u) ? from[i] : 0u;
+  return r;
+}
+
+// x - mean and dz of one vector; h.dy is gated already where the gate is ReLU's.
 template <typename T, bool CK>
-__device__ __forceinline__ void gated(const Held<T, CK>& h, int act, const Channels& ch, float (&dz)[8], float (&d)[8]) {
-  raw8_to_f(h.dy, dz);
-  if constexpr (CK) ckpt_values(h.codes, ckpt_step(h.scale), d); else raw8_to_f(h.x, d);
+__device__ __forceinline__ void operands(const Held<T, CK>& h, int act, const Channels& ch, F8& dz, F8& d) {
+  dz = raw8_to_f8(h.dy);
+  if constexpr (CK) {
+    d = ckpt_numbers(h.codes);
+    const f32x2 step = pair(ckpt_step(h.scale));
 #pragma unroll
-  for (int i = 0; i < 8; ++i) d[i] -= ch.mean[i];
-  if (act == ACT_RELU) {
+    for (int j = 0; j < 4; ++j) d.p[j] = fma2(d.p[j], step, ch.less[j]);
+  } else {
+    d = raw8_to_f8(h.x);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dz[i] = (h.open >> i & 1u) ? dz[i] : 0.f;
-  } else if (act == ACT_SILU) {
+    for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], ch.less[j]);
+  }
+  if (act == ACT_SILU) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dz[i] *= silu_slope<T>(fmaf(d[i], ch.scale[i], ch.shift[i]));
+    for (int j = 0; j < 4; ++j) {
+      const float2 z = halves(fma2(d.p[j], ch.scale[j], ch.shift[j]));
+      dz.p[j] = mul2(dz.p[j], pair(silu_slope<T>(z.x), silu_slope<T>(z.y)));
+    }
   }
 }
 
-// dx of this CTA's pixels: fetch(k, row) gives the thread's k-th operands; k1 = rstd*S1/m, k2 = rstd^2*S2/m.
-template <typename T, bool VEC, bool CK, typename Fetch>
+// dx of this CTA's pixels: fetch(k) gives the thread's k-th operands; k1 = -rstd*S1/m, k2 = -rstd^2*S2/m.
+template <typename T, bool VEC, bool CK, int U, typename Fetch>
 __device__ __forceinline__ void emit_dx(const Backward<T>& p, const Place& at, size_t row0, int count, const Channels& ch,
-                                        const float (&k1)[8], const float (&k2)[8], Fetch fetch) {
+                                        const f32x2 (&k1)[4], const f32x2 (&k2)[4], Fetch fetch) {
   const Geom& g = p.g;
   if (!at.active) return;
-#pragma unroll 2
-  for (int k = 0; k < g.iters; ++k) {
-    const int pixel = at.r + k * g.rp;
-    if (pixel >= count) break;
-    const size_t row = row0 + pixel, off = row * g.C + at.c0;
-    float dz[8], d[8];
-    gated<T, CK>(fetch(k, row), p.act, ch, dz, d);
+  const size_t off = (row0 + at.r) * g.C + at.c0;
+  T* const dx = p.dx + off;
+  const T* const res = p.res + off;
+  const bool has_res = p.res != nullptr;
+  const uint32_t step = (uint32_t)g.rp * g.C;
+  for (int k0 = 0; k0 < g.iters; k0 += U) {
+    if (at.r + k0 * g.rp >= count) break;
+    Held<T, CK> hs[U];
+    Raw8<T> rs[U];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dz[i] = fmaf(ch.scale[i], dz[i], fmaf(-d[i], k2[i], -k1[i]));
-    if (p.res) {
-      raw8_to_f(raw8_load<T, VEC>(p.res + off, at.left), d);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) dz[i] += d[i];
+    for (int u = 0; u < U; ++u) {
+      if (at.r + (k0 + u) * g.rp >= count) continue;
+      hs[u] = fetch(k0 + u);
+      if (has_res) rs[u] = raw8_load<T, VEC>(res + (uint32_t)(k0 + u) * step, at.left);
     }
-    raw8_store<T, VEC>(p.dx + off, at.left, dz);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (at.r + (k0 + u) * g.rp >= count) continue;
+      F8 dz, d;
+      operands<T, CK>(hs[u], p.act, ch, dz, d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) dz.p[j] = fma2(ch.scale[j], dz.p[j], fma2(d.p[j], k2[j], k1[j]));
+      if (has_res) {
+        const F8 r = raw8_to_f8(rs[u]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dz.p[j] = add2(dz.p[j], r.p[j]);
+      }
+      raw8_put<T, VEC>(dx + (uint32_t)(k0 + u) * step, at.left, f8_to_raw8<T>(dz));
+    }
   }
 }
 
@@ -502,14 +637,63 @@ __device__ __forceinline__ Held<T, CK> load_held(const Backward<T>& p, const Pla
   } else {
     h.x = raw8_load<T, VEC>(p.x + off, at.left);
   }
-  h.open = p.act == ACT_RELU ? open_bits<T, VEC>(p, at, row) : 0u;
+  h.open = p.act == ACT_RELU ? open_bits<T, VEC>(p, at, row) : 0xFFu;
   return h;
 }
+// The constants of a thread's channels from the saved statistics.
+template <typename T>
+__device__ __forceinline__ void load_channels(const Backward<T>& p, const Place& at, int n, Channels& ch, float (&rstd)[8]) {
+  const Geom& g = p.g;
+  float mean[8], scale[8], shift[8];
+  each_channel(at, g.Cg, [&](int i, int c, int s) {
+    mean[i] = p.stats[(size_t)n * g.G + s];
+    rstd[i] = p.stats[(size_t)(g.N + n) * g.G + s];
+    scale[i] = p.gamma[c] * rstd[i];
+    shift[i] = p.act == ACT_SILU ? p.beta[c] : 0.f;
+  });
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    ch.less[j] = pair(-mean[2 * j], -mean[2 * j + 1]);
+    ch.scale[j] = pair(scale[2 * j], scale[2 * j + 1]);
+    ch.shift[j] = pair(shift[2 * j], shift[2 * j + 1]);
+  }
+}
+// k1, k2 of a thread's channels from those of the groups, the first of which is `first`.
+__device__ __forceinline__ void load_coefficients(const Place& at, int Cg, const float* c1, const float* c2, int first, f32x2 (&k1)[4], f32x2 (&k2)[4]) {
+  float a[8], b[8];
+  each_channel(at, Cg, [&](int i, int, int s) { a[i] = -c1[s - first]; b[i] = -c2[s - first]; });
+#pragma unroll
+  for (int j = 0; j < 4; ++j) { k1[j] = pair(a[2 * j], a[2 * j + 1]); k2[j] = pair(b[2 * j], b[2 * j + 1]); }
+}
+// A thread's sums of dz*(x - mean) and of dz.
+struct Sums {
+  F8 a, b;
+  __device__ __forceinline__ Sums() {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a.p[j] = b.p[j] = 0;
+  }
+  __device__ __forceinline__ void add(const F8& dz, const F8& d) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { a.p[j] = fma2(dz.p[j], d.p[j], a.p[j]); b.p[j] = add2(b.p[j], dz.p[j]); }
+  }
+  // A = rstd * sum dz*(x - mean) and B, to red[0..2048) and red[2048..4096)
+  __device__ __forceinline__ void put(float* red, const Geom& g, const Place& at, const float (&rstd)[8]) const {
+    float v[8], w[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 x = halves(a.p[j]), y = halves(b.p[j]);
+      v[2 * j] = x.x * rstd[2 * j]; v[2 * j + 1] = x.y * rstd[2 * j + 1];
+      w[2 * j] = y.x; w[2 * j + 1] = y.y;
+    }
+    put_sums(red, g, at, v);
+    put_sums(red + kThreads * 8, g, at, w);
+  }
+};
 
 // The resident form.  Shared memory: the thread's vectors of dy and x (or its codes), a byte per vector for the gate's bits and
 // one for the scale; then per-thread sums, per-channel sums A, B and per-group sums S1, S2 of this CTA, and k1, k2 of the image.
 template <typename T, bool VEC, bool CK>
-__global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_constant__ Backward<T> p) {
+__global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_constant__ Backward<T> p) {
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
   const size_t vecs = (size_t)g.iters * kThreads;
@@ -550,14 +734,7 @@ __global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_cons
   }
   Channels ch;
   float rstd[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int c = at.channel(i), s = c / g.Cg;
-    ch.mean[i] = p.stats[(size_t)n * g.G + s];
-    rstd[i] = p.stats[(size_t)(g.N + n) * g.G + s];
-    ch.scale[i] = p.gamma[c] * rstd[i];
-    ch.shift[i] = p.act == ACT_SILU ? p.beta[c] : 0.f;
-  }
+  load_channels(p, at, n, ch, rstd);
   copies_done();
   auto held = [&](int k) {
     Held<T, CK> h;
@@ -568,25 +745,23 @@ __global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_cons
     } else {
       h.x = xslots.get(k);
     }
-    h.open = p.act == ACT_RELU ? open[k * kThreads + tid] : 0u;
     return h;
   };
-  float a[8], b[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) a[i] = b[i] = 0.f;
+  Sums sums;
   if (at.active)
 #pragma unroll 2
     for (int k = 0; k < g.iters; ++k) {
       if (at.r + k * g.rp >= count) break;
-      float dz[8], d[8];
-      gated<T, CK>(held(k), p.act, ch, dz, d);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { a[i] = fmaf(dz[i], d[i], a[i]); b[i] += dz[i]; }
+      Held<T, CK> h = held(k);
+      if (p.act == ACT_RELU) {
+        h.dy = opened(h.dy, open[k * kThreads + tid]);
+        dys.put(k, h.dy);                           // gated once, for the second sweep too
+      }
+      F8 dz, d;
+      operands<T, CK>(h, p.act, ch, dz, d);
+      sums.add(dz, d);
     }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) a[i] *= rstd[i];
-  put_sums(red, g, at, a);
-  put_sums(red + kThreads * 8, g, at, b);
+  sums.put(red, g, at, rstd);
   __syncthreads();
   const int width = g.cols * 8;
   for (int s = 0; s < 2; ++s) {
@@ -619,13 +794,9 @@ __global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_cons
   cg::cluster_group::arrival_token token = cluster.barrier_arrive();
   __syncthreads();
   grid_dependency_release();
-  float k1[8], k2[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int s = at.channel(i) / g.Cg;
-    k1[i] = coef[s]; k2[i] = coef[g.G + s];
-  }
-  emit_dx<T, VEC, CK>(p, at, row0, count, ch, k1, k2, [&](int k, size_t) { return held(k); });
+  f32x2 k1[4], k2[4];
+  load_coefficients(at, g.Cg, coef, coef + g.G, 0, k1, k2);
+  emit_dx<T, VEC, CK, 2>(p, at, row0, count, ch, k1, k2, held);
   cluster.barrier_wait(std::move(token));
 }
 
@@ -637,27 +808,20 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
   const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
   const int p0 = part * g.pix, count = min(g.pix, g.P - p0);
   const size_t row0 = (size_t)n * g.P + p0;
-  const Place at(g, blockIdx.y);
-  const bool active = at.active && at.left > 0;
+  Place at(g, blockIdx.y);
+  at.active = at.active && at.left > 0;
+  if (!at.active) at.c0 = blockIdx.y * kMaxCols * 8;
   grid_dependency_wait();
   Channels ch;
-  float rstd[8], a[8], b[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int c = active ? at.channel(i) : 0, s = c / g.Cg;
-    ch.mean[i] = p.stats[(size_t)n * g.G + s];
-    rstd[i] = p.stats[(size_t)(g.N + n) * g.G + s];
-    ch.scale[i] = p.gamma[c] * rstd[i];
-    ch.shift[i] = p.act == ACT_SILU ? p.beta[c] : 0.f;
-    a[i] = b[i] = 0.f;
-  }
+  float rstd[8];
+  load_channels(p, at, n, ch, rstd);
+  Sums sums;
   auto add = [&](const Held<T, CK>& h) {
-    float dz[8], d[8];
-    gated<T, CK>(h, p.act, ch, dz, d);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { a[i] = fmaf(dz[i], d[i], a[i]); b[i] += dz[i]; }
+    F8 dz, d;
+    operands<T, CK>(h, p.act, ch, dz, d);
+    sums.add(dz, d);
   };
-  if (active) {
+  if (at.active) {
     constexpr int U = sizeof(T) == 4 ? 2 : 4;             // vectors in flight
     int pixel = at.r;
     for (; pixel + (U - 1) * g.rp < count; pixel += U * g.rp) {
@@ -665,14 +829,15 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
 #pragma unroll
       for (int u = 0; u < U; ++u) h[u] = load_held<T, VEC, CK>(p, at, row0 + pixel + u * g.rp);
 #pragma unroll
-      for (int u = 0; u < U; ++u) add(h[u]);
+      for (int u = 0; u < U; ++u) { h[u].dy = opened(h[u].dy, h[u].open); add(h[u]); }
     }
-    for (; pixel < count; pixel += g.rp) add(load_held<T, VEC, CK>(p, at, row0 + pixel));
+    for (; pixel < count; pixel += g.rp) {
+      Held<T, CK> h = load_held<T, VEC, CK>(p, at, row0 + pixel);
+      h.dy = opened(h.dy, h.open);
+      add(h);
+    }
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) a[i] *= rstd[i];
-  put_sums(red[0], g, at, a);
-  put_sums(red[1], g, at, b);
+  sums.put(red[0], g, at, rstd);
   __syncthreads();
   const int width = g.cols * 8, c_first = blockIdx.y * kMaxCols * 8, sets = min(width, g.C - c_first);
   for (int s = 0; s < 2; ++s) {
@@ -709,7 +874,7 @@ __global__ void __launch_bounds__(1024) add_rows_kernel(const float* __restrict_
 
 // Streamed, last pass: dx, the last chunks first.  Every CTA forms S1 and S2 of its tile's groups from the image's totals.
 template <typename T, bool VEC, bool CK>
-__global__ void __launch_bounds__(kThreads, 3) backward_apply_kernel(const __grid_constant__ Backward<T> p) {
+__global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __grid_constant__ Backward<T> p) {
   __shared__ float coef[2][kMaxCols * 8];
   const Geom& g = p.g;
   const int block = gridDim.x - 1 - blockIdx.x, part = block % g.parts, n = block / g.parts;
@@ -717,6 +882,7 @@ __global__ void __launch_bounds__(kThreads, 3) backward_apply_kernel(const __gri
   const size_t row0 = (size_t)n * g.P + p0;
   Place at(g, blockIdx.y);
   at.active = at.active && at.left > 0;
+  if (!at.active) at.c0 = blockIdx.y * kMaxCols * 8;
   const int c_first = blockIdx.y * kMaxCols * 8, c_last = min(g.C, c_first + g.cols * 8) - 1;
   const int g_first = c_first / g.Cg, sets = c_last / g.Cg - g_first + 1;
   const float inv_m = (float)(1.0 / ((double)g.P * g.Cg));
@@ -730,16 +896,15 @@ __global__ void __launch_bounds__(kThreads, 3) backward_apply_kernel(const __gri
            [&](int s, float sum) { coef[1][s] = rs[s] * rs[s] * sum * inv_m; });
   __syncthreads();
   Channels ch;
-  float k1[8], k2[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int c = at.active ? at.channel(i) : c_first, s = c / g.Cg;
-    ch.mean[i] = p.stats[(size_t)n * g.G + s];
-    ch.scale[i] = p.gamma[c] * p.stats[(size_t)(g.N + n) * g.G + s];
-    ch.shift[i] = p.act == ACT_SILU ? p.beta[c] : 0.f;
-    k1[i] = coef[0][s - g_first]; k2[i] = coef[1][s - g_first];
-  }
-  emit_dx<T, VEC, CK>(p, at, row0, count, ch, k1, k2, [&](int, size_t row) { return load_held<T, VEC, CK>(p, at, row); });
+  float rstd[8];
+  f32x2 k1[4], k2[4];
+  load_channels(p, at, n, ch, rstd);
+  load_coefficients(at, g.Cg, coef[0], coef[1], g_first, k1, k2);
+  emit_dx<T, VEC, CK, 2>(p, at, row0, count, ch, k1, k2, [&](int k) {
+    Held<T, CK> h = load_held<T, VEC, CK>(p, at, row0 + at.r + k * g.rp);
+    h.dy = opened(h.dy, h.open);
+    return h;
+  });
 }
 
 // ---- host side: plans ----------------------------------------------------------------------------------------

@@ -74,18 +74,6 @@ template <typename T, bool VEC> __device__ __forceinline__ Raw8<T> raw8_load(con
   }
   return r;
 }
-template <typename T> __device__ __forceinline__ void raw8_to_f(const Raw8<T>& r, float (&v)[8]) {
-  const T* e = reinterpret_cast<const T*>(&r);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = to_f(e[i]);
-}
-template <typename T> __device__ __forceinline__ Raw8<T> raw8_of(const float (&v)[8]) {
-  Raw8<T> r;
-  T* e = reinterpret_cast<T*>(&r);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) e[i] = from_f<T>(v[i]);
-  return r;
-}
 template <typename T, bool VEC> __device__ __forceinline__ void raw8_put(T* __restrict__ p, int left, const Raw8<T>& r) {
   if constexpr (VEC) {
 #pragma unroll
@@ -97,8 +85,82 @@ template <typename T, bool VEC> __device__ __forceinline__ void raw8_put(T* __re
       if (i < left) p[i] = e[i];
   }
 }
-template <typename T, bool VEC> __device__ __forceinline__ void raw8_store(T* __restrict__ p, int left, const float (&v)[8]) {
-  raw8_put<T, VEC>(p, left, raw8_of<T>(v));
+
+// Pairs of fp32 values in one 64-bit register pair.  sm_100a adds, multiplies and multiply-adds both halves with one
+// instruction (each half rounded as the scalar instruction rounds it), which halves the arithmetic issued by kernels that have
+// a handful of operations on every value they stream.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+  f32x2 d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ f32x2 pair(float v) { return pair(v, v); }
+__device__ __forceinline__ float2 halves(f32x2 v) {
+  float2 d;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(v));
+  return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+
+// Eight fp32 values as pairs, and the way from and to the storage type.
+struct F8 { f32x2 p[4]; };
+__device__ __forceinline__ F8 raw8_to_f8(const Raw8<__nv_bfloat16>& r) {
+  const uint32_t w[4] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w};
+  F8 f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) f.p[j] = pair(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
+  return f;
+}
+__device__ __forceinline__ F8 raw8_to_f8(const Raw8<float>& r) {
+  F8 f;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    f.p[2 * j] = pair(__uint_as_float(r.q[j].x), __uint_as_float(r.q[j].y));
+    f.p[2 * j + 1] = pair(__uint_as_float(r.q[j].z), __uint_as_float(r.q[j].w));
+  }
+  return f;
+}
+// The storage type's values, and with RELU those of max(v, 0), NaN staying NaN.
+template <bool RELU> __device__ __forceinline__ uint32_t pack_bf16x2(f32x2 v) {
+  const float2 h = halves(v);
+  uint32_t d;
+  if (RELU) asm("cvt.rn.relu.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(h.y), "f"(h.x));
+  else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(h.y), "f"(h.x));
+  return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+template <typename T, bool RELU = false> __device__ __forceinline__ Raw8<T> f8_to_raw8(const F8& f) {
+  Raw8<T> r;
+  if constexpr (sizeof(T) == 2) {
+    r.q[0] = make_uint4(pack_bf16x2<RELU>(f.p[0]), pack_bf16x2<RELU>(f.p[1]), pack_bf16x2<RELU>(f.p[2]), pack_bf16x2<RELU>(f.p[3]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float2 a = halves(f.p[2 * j]), b = halves(f.p[2 * j + 1]);
+      if (RELU) { a.x = max_nan(a.x, 0.f); a.y = max_nan(a.y, 0.f); b.x = max_nan(b.x, 0.f); b.y = max_nan(b.y, 0.f); }
+      r.q[j] = make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+    }
+  }
+  return r;
 }
 
 }  // namespace fdg
