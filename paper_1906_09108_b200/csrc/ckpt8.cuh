@@ -132,9 +132,9 @@ inline int ckpt_block_lanes(int C) {
   const int cols = (C + 7) / 8;
   return cols % 4 == 0 ? 4 : (cols <= 2 ? cols : 0);
 }
-__device__ __forceinline__ uint32_t ckpt_top_of_lanes(uint32_t top, int lanes) {
-  if (lanes >= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  if (lanes >= 4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+__device__ __forceinline__ uint32_t ckpt_top_of_lanes(uint32_t top, int lanes, uint32_t taking_part = 0xffffffffu) {
+  if (lanes >= 2) top = max(top, __shfl_xor_sync(taking_part, top, 1));
+  if (lanes >= 4) top = max(top, __shfl_xor_sync(taking_part, top, 2));
   return top;
 }
 

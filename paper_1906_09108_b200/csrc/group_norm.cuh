@@ -6,27 +6,32 @@
 //   dz = dy*act'(z),  A[n][c] = sum_p dz*xhat,  B[n][c] = sum_p dz:  dgamma = sum_n A,  dbeta = sum_n B,
 //   S1 = sum over the group's channels of gamma*B,  S2 = of gamma*A,
 //   dx = rstd*(gamma*dz - (S1 + xhat*S2)/m) [+ res].
-// Bound by memory: 10 to 25 operations on each value against 2 to 9 bytes of traffic.  What can be won is reading each tensor
-// once although every output needs sums over its whole group, and keeping enough loads in flight.
+// Bound by memory: 10 to 25 operations on each value against 2 to 9 bytes of traffic, which is close enough to the rate at which
+// instructions issue that these count too: values go through the arithmetic in pairs (kernel_common.cuh), and what a call does
+// not ask for (activation, gate, residual, checkpoint) is compiled out.
 //
 // Layout.  A row of a pixel's channels is cut into columns of 8 channels; a thread keeps one column and walks the pixels, rp of
 // them side by side in a CTA of 256 threads, so a warp's accesses are contiguous for every channel count, and a group may start
 // and end anywhere inside a column (5 channels of 160, say): sums are formed per channel and thread and added per group from
 // shared memory.
 //
-// Two forms, chosen by gn_plan_*:
+// Two forms, chosen by plan():
 //   resident  a cluster of up to 8 CTAs takes an image, each a share of its pixels, which it copies to shared memory at once
 //             (cp.async, every thread its own vectors, so nothing but a thread's own wait stands between copy and use).  The
-//             statistics are formed there, exchanged through distributed shared memory, and applied from there: one launch, one
+//             sums are formed there, exchanged through distributed shared memory, and applied from there: one launch, one
 //             read, one write.
-//   streamed  images that no cluster holds: a CTA per chunk of pixels leaves its sums in scratch, a small kernel adds them in a
-//             fixed order, and a third pass reads the tensor again, the last chunks first, which are still in L2.
+//   streamed  as many CTAs as run at once, each a contiguous share of an image's pixels: one pass forms the sums, leaves a row
+//             of them per CTA in scratch, and a second pass adds the rows up and applies them, walking its pixels backwards, so
+//             that it starts with what L2 holds.
 //
-// Variance: within a CTA from the CTA's own mean (two sweeps over shared memory), across CTAs by Chan's formula in fp64; no
-// difference of large sums is formed, so an offset of a thousand standard deviations costs no more than the inputs' own
-// rounding.  All sums are fp32 within a CTA (chains of at most a few dozen values a thread, then a tree), in a fixed order.
+// Variance: a thread sums its values and their squares less its first value, brings them about a common value of the CTA (the
+// mean of the channel's first row of threads), then about the CTA's group mean, and CTAs are combined by Chan's formula.  The
+// square of the distance from a mean over a share f of the values to the mean over all is at most var*(1 - f)/f, so what cancels
+// in each step is bounded by the data itself (by the number of a thread's values, then by rp), whatever offset x has.
+// All sums are fp32 within a CTA (a chain of a thread's values, then of rows of threads, then a tree), in a fixed order.
 #pragma once
 #include <cooperative_groups.h>
+#include <stdlib.h>
 
 #include "ckpt8.cuh"
 #include "kernel_common.cuh"
@@ -45,10 +50,11 @@ struct Geom {
   int N, P, C, G, Cg;
   int cols, rp;             // columns of a CTA's tile, pixels side by side
   int parts, pix;           // CTAs per image, pixels per CTA
-  int iters;                // pixels per thread: ceil(pix / rp)
+  int iters;                // pixels per thread at most: ceil(pix / rp)
   int lanes_g, lanes_c;     // lanes that add up one group / one channel
   int tiles;                // tiles of columns (1 unless streamed with more than 2048 channels)
 };
+constexpr int kMergeParts = 16;             // rows of sums that the second streamed pass adds up itself
 
 // ---- device helpers -------------------------------------------------------------------------------------
 // 1/(1 + exp(-z)).  For tensors in 16 bits from the approximate exponential and reciprocal (relative error below 2^-20 for
@@ -126,6 +132,19 @@ template <typename Take> __device__ __forceinline__ void each_channel(const Plac
   }
 }
 
+// This CTA's pixels: `count` from pixel `row0` of the tensor on; a thread has `mine` of them, `whole` or one more.
+struct Share {
+  size_t row0;
+  int count, whole, mine;
+  __device__ __forceinline__ Share(const Geom& g, const Place& at, int n, int part) {
+    const int p0 = part * g.pix;
+    row0 = (size_t)n * g.P + p0;
+    count = max(0, min(g.pix, g.P - p0));
+    whole = count / g.rp;
+    mine = at.active ? whole + (at.r < count - whole * g.rp ? 1 : 0) : 0;
+  }
+};
+
 // red[r][8 * cols] = the 8 sums of each thread.
 __device__ __forceinline__ void put_sums(float* red, const Geom& g, const Place& at, const float (&v)[8]) {
   if (!at.active) return;
@@ -134,26 +153,46 @@ __device__ __forceinline__ void put_sums(float* red, const Geom& g, const Place&
   d[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
-// done(s, sum of value(r, s*size + j) over r < rows, j < size) for s < sets: `lanes` consecutive lanes (a power of two up
-// to 32) share a set.  To be called by the whole CTA.
-template <typename Value, typename Done>
-__device__ __forceinline__ void add_sets(int rows, int sets, int size, int lanes, Value value, Done done) {
-  const int sub = threadIdx.x & (lanes - 1), per_pass = kThreads / lanes, mine = threadIdx.x / lanes;
-  const int dr = lanes / size, dj = lanes - dr * size;
-  const int r0 = sub / size, j0 = sub - r0 * size;
-  for (int s0 = 0; s0 < sets; s0 += per_pass) {
-    const int s = s0 + mine;
-    float a = 0.f;
-    if (s < sets) {
-      int r = r0, j = j0;
-      while (r < rows) {
-        a += value(r, s * size + j);
-        r += dr; j += dj;
-        if (j >= size) { j -= size; ++r; }
-      }
+// Sums over the rows of threads of two such arrays (the second 2048 floats behind the first): done(c, sum, sum) for the tile's
+// first `sets` channels; `lanes` consecutive lanes (a power of two up to 32) share a channel.  For the whole CTA.
+template <typename Done>
+__device__ __forceinline__ void channel_sums(const float* red, const Geom& g, int sets, int lanes, Done done) {
+  const int sub = threadIdx.x & (lanes - 1), per_pass = kThreads / lanes, width = g.cols * 8;
+  for (int c0 = 0; c0 < sets; c0 += per_pass) {
+    const int c = c0 + threadIdx.x / lanes;
+    float a = 0.f, b = 0.f;
+    if (c < sets) {
+      const float* v = red + c + sub * width;
+#pragma unroll 4
+      for (int r = sub; r < g.rp; r += lanes, v += lanes * width) { a += v[0]; b += v[kThreads * 8]; }
     }
-    for (int o = lanes >> 1; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-    if (s < sets && sub == 0) done(s, a);
+    for (int o = lanes >> 1; o > 0; o >>= 1) {
+      a += __shfl_xor_sync(0xffffffffu, a, o);
+      b += __shfl_xor_sync(0xffffffffu, b, o);
+    }
+    if (c < sets && sub == 0) done(c, a, b);
+  }
+}
+// The sum of v over the `lanes` lanes that share a group.
+__device__ __forceinline__ float lane_sum(float v, int lanes) {
+  for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// done(s, sum of first(c), sum of second(c) over the group's channels) for groups s < sets of `size` channels from c = 0 on.
+template <typename Value, typename Done>
+__device__ __forceinline__ void group_sums(int sets, int size, int lanes, Value value, Done done) {
+  const int sub = threadIdx.x & (lanes - 1), per_pass = kThreads / lanes;
+  for (int s0 = 0; s0 < sets; s0 += per_pass) {
+    const int s = s0 + threadIdx.x / lanes;
+    float2 a = make_float2(0.f, 0.f);
+    if (s < sets)
+      for (int j = sub; j < size; j += lanes) {
+        const float2 v = value(s * size + j);
+        a.x += v.x; a.y += v.y;
+      }
+    a.x = lane_sum(a.x, lanes);
+    a.y = lane_sum(a.y, lanes);
+    if (s < sets && sub == 0) done(s, a.x, a.y);
   }
 }
 
@@ -169,75 +208,111 @@ template <typename T> struct Forward {
   uint8_t* gate;              // bits of [y > 0], a byte per column
   int8_t* codes;              // x in 8 bits
   uint8_t* scales;
-  float* partial;             // streamed: [N][parts][2][C]
+  float* partial;             // streamed: [N][parts][2][sets]: means and squared deviations; sets = groups, or channels with tiles > 1
   float eps;
   int act;
   int ckpt_lanes;
+  bool combined;              // streamed: `stats` holds the statistics when the second pass starts
 };
 
-// Moments of this CTA's `count` pixels in `slots`: done(set, mean, sum of squared deviations from that mean) for sets of `size`
-// consecutive channels.  `red`: 2048 floats, `mean`: a float per set.
-// A thread sums its values of a channel, and their squares, less the first of them: the square of the distance from that value
-// to the mean is at most n times the spread of the n values, so what cancels when the sum is taken out again is at most n times
-// the result, whatever the offset (n is a few dozen at most).  The threads' moments are then brought about the CTA's mean.
-template <typename T, typename Done>
-__device__ __forceinline__ void cta_moments(const Geom& g, const Place& at, const Slots<T>& slots, int count, int sets, int size, int lanes,
-                                            float* red, float* mean, Done done) {
-  const int width = g.cols * 8;
-  const float inv = count > 0 ? 1.f / ((float)count * (float)size) : 0.f;
+// A thread's moments of its 8 channels: sums of its values and of their squares less the first of them.
+struct Moments {
   F8 first, sum, square;
+  __device__ __forceinline__ Moments() {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) first.p[j] = sum.p[j] = square.p[j] = 0;
-  int n = 0;
-  if (at.active && at.r < count) {
-    F8 less;
-    first = raw8_to_f8(slots.get(0));
+    for (int j = 0; j < 4; ++j) first.p[j] = sum.p[j] = square.p[j] = 0;
+  }
+  __device__ __forceinline__ void start(const F8& x) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) less.p[j] = mul2(first.p[j], pair(-1.f));
-    n = 1;
-#pragma unroll 4
-    for (int k = 1; k < g.iters; ++k) {
-      if (at.r + k * g.rp >= count) break;
-      const F8 x = raw8_to_f8(slots.get(k));
+    for (int j = 0; j < 4; ++j) first.p[j] = mul2(x.p[j], pair(-1.f));
+  }
+  __device__ __forceinline__ void add(const F8& x) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x2 d = add2(x.p[j], less.p[j]);
-        sum.p[j] = add2(sum.p[j], d);
-        square.p[j] = fma2(d, d, square.p[j]);
-      }
-      ++n;
+    for (int j = 0; j < 4; ++j) {
+      const f32x2 d = add2(x.p[j], first.p[j]);
+      sum.p[j] = add2(sum.p[j], d);
+      square.p[j] = fma2(d, d, square.p[j]);
     }
   }
+};
+
+// The CTA's moments from its threads' (each over n values): chan[c] = mean and squared deviations from it of the tile's first
+// `sets` channels.  `red`: 4096 floats, `common`: 2048 floats.  Ends with a barrier.
+__device__ __forceinline__ void cta_moments(const Geom& g, const Place& at, const Moments& m, int n, int count, int sets, float* red, float* common,
+                                            float2* chan) {
   const float fn = (float)n, over = n > 0 ? 1.f / fn : 0.f;
-  float a[8], mu[8];                  // the thread's mean and squared deviations
+  float mu[8], dev[8];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float2 f = halves(first.p[j]), s1 = halves(sum.p[j]), s2 = halves(square.p[j]);
-    mu[2 * j] = fmaf(s1.x, over, f.x);
-    mu[2 * j + 1] = fmaf(s1.y, over, f.y);
-    a[2 * j] = max_nan(fmaf(-s1.x * over, s1.x, s2.x), 0.f);
-    a[2 * j + 1] = max_nan(fmaf(-s1.y * over, s1.y, s2.y), 0.f);
+    const float2 f = halves(m.first.p[j]), s1 = halves(m.sum.p[j]), s2 = halves(m.square.p[j]);
+    mu[2 * j] = fmaf(s1.x, over, -f.x);
+    mu[2 * j + 1] = fmaf(s1.y, over, -f.y);
+    dev[2 * j] = fmaf(-s1.x * over, s1.x, s2.x);
+    dev[2 * j + 1] = fmaf(-s1.y * over, s1.y, s2.y);
   }
-  float t[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) t[i] = mu[i] * fn;
-  put_sums(red, g, at, t);
+  if (at.r == 0) put_sums(common, g, at, mu);
   __syncthreads();
-  auto value = [&](int r, int c) { return red[r * width + c]; };
-  add_sets(g.rp, sets, size, lanes, value, [&](int s, float total) { mean[s] = total * inv; });
-  __syncthreads();
-  if (at.active) {
-    int s = at.col * 8 / size, rem = at.col * 8 - s * size;
+  const float4* k = reinterpret_cast<const float4*>(common + at.col * 8);
+  const float4 k0 = k[0], k1 = k[1];
+  const float about[8] = {k0.x, k0.y, k0.z, k0.w, k1.x, k1.y, k1.z, k1.w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float d = mu[i] - mean[min(s, sets - 1)];
-      t[i] = fmaf(fn * d, d, a[i]);
-      if (++rem == size) { rem = 0; ++s; }
-    }
-    put_sums(red, g, at, t);
+  for (int i = 0; i < 8; ++i) {
+    const float d = n > 0 ? mu[i] - about[i] : 0.f;
+    mu[i] = fn * d;
+    dev[i] = n > 0 ? fmaf(fn * d, d, max_nan(dev[i], 0.f)) : 0.f;
   }
+  put_sums(red, g, at, mu);
+  put_sums(red + kThreads * 8, g, at, dev);
   __syncthreads();
-  add_sets(g.rp, sets, size, lanes, value, [&](int s, float total) { done(s, mean[s], total); });
+  const float inv = count > 0 ? 1.f / (float)count : 0.f;
+  channel_sums(red, g, sets, g.lanes_c, [&](int c, float s, float q) {
+    const float d = s * inv;
+    chan[c] = make_float2(common[c] + d, max_nan(fmaf(-s, d, q), 0.f));
+  });
+  __syncthreads();
+}
+// done(s, mean, squared deviations) of this CTA's groups from its channels' moments over `count` pixels.
+template <typename Done>
+__device__ __forceinline__ void group_moments(const Geom& g, int count, const float2* chan, Done done) {
+  const int lanes = g.lanes_g, sub = threadIdx.x & (lanes - 1), per_pass = kThreads / lanes;
+  const float inv = 1.f / (float)g.Cg;
+  for (int s0 = 0; s0 < g.G; s0 += per_pass) {
+    const int s = s0 + threadIdx.x / lanes;
+    float a = 0.f, q = 0.f;
+    if (s < g.G)
+      for (int j = sub; j < g.Cg; j += lanes) a += chan[s * g.Cg + j].x;
+    const float mu = lane_sum(a, lanes) * inv;
+    if (s < g.G)
+      for (int j = sub; j < g.Cg; j += lanes) {
+        const float2 c = chan[s * g.Cg + j];
+        const float d = c.x - mu;
+        q += fmaf((float)count * d, d, c.y);
+      }
+    q = lane_sum(q, lanes);
+    if (s < g.G && sub == 0) done(s, mu, q);
+  }
+}
+// Chan: done(s, mean, rstd) of the image's groups from the moments of its `rows` CTAs, row(j)[s] their means and row(j)[G + s] their
+// squared deviations; up to 8 lanes share a group.
+template <typename Row, typename Done>
+__device__ __forceinline__ void image_moments(const Geom& g, int rows, float eps, Row row, Done done) {
+  const int lanes = rows >= 8 ? 8 : rows >= 4 ? 4 : rows >= 2 ? 2 : 1, sub = threadIdx.x & (lanes - 1), per_pass = kThreads / lanes;
+  const float inv_p = 1.f / (float)g.P, inv_cg = 1.f / (float)g.Cg;
+  auto pixels = [&](int j) { return (float)max(0, min(g.pix, g.P - j * g.pix)); };
+  for (int s0 = 0; s0 < g.G; s0 += per_pass) {
+    const int s = s0 + threadIdx.x / lanes;
+    float a = 0.f, q = 0.f;
+    if (s < g.G)
+      for (int j = sub; j < rows; j += lanes) a = fmaf(row(j)[s], pixels(j) * inv_p, a);
+    const float mu = lane_sum(a, lanes);
+    if (s < g.G)
+      for (int j = sub; j < rows; j += lanes) {
+        const float d = row(j)[s] - mu;
+        q = fmaf(pixels(j) * d, d, fmaf(row(j)[g.G + s], inv_cg, q));
+      }
+    q = lane_sum(q, lanes);
+    if (s < g.G && sub == 0) done(s, mu, 1.f / sqrtf(fmaf(q, inv_p, eps)));
+  }
 }
 
 // What a thread multiplies its 8 channels by: scale = gamma*rstd and shift = beta, and the mean with its sign turned.  16-bit
@@ -278,52 +353,65 @@ __device__ __forceinline__ uint32_t positive_bits(const Raw8<float>& y) {
   return b;
 }
 
-// y (and the gate's bits, and x in 8 bits) of this CTA's pixels: fetch(k, offset) gives the thread's k-th vector of x; U of them
-// (and of res) are fetched before the first is used.  Every lane takes every turn, since the lanes of a block of 32 channels
-// exchange its maximum.  Offsets inside a CTA's pixels fit 32 bits.
-template <typename T, bool VEC, int U, typename Fetch>
-__device__ __forceinline__ void emit(const Forward<T>& p, const Place& at, size_t row0, int count, const Affine<T>& affine, Fetch fetch) {
+// y (and the gate's bits, and x in 8 bits) of this CTA's pixels: fetch(k) gives the thread's k-th vector of x; U of them (and of
+// res) are fetched before the first is used.  REVERSE: from the last pixel to the first.  ACT < 0: p.act; EXTRA: res, gate and
+// codes may be asked for.  Lanes that share a block of 32 channels have the same pixels, and take every turn together.
+// Offsets inside a CTA's pixels fit 32 bits.
+template <typename T, bool VEC, int ACT, bool EXTRA, int U, bool REVERSE, typename Fetch>
+__device__ __forceinline__ void emit(const Forward<T>& p, const Place& at, const Share& sh, const Affine<T>& affine, Fetch fetch) {
   const Geom& g = p.g;
-  const int all_cols = (g.C + 7) >> 3, per_row = (g.C + kCkptBlock - 1) / kCkptBlock;
-  const size_t row = row0 + at.r, off = row * g.C + at.c0;
+  const int act = ACT < 0 ? p.act : ACT;
+  const size_t row = sh.row0 + at.r, off = row * g.C + at.c0;
   T* const y = p.y + off;
-  const T* const res = p.res + off;
-  int8_t* const codes = p.codes + off;
-  uint8_t* const gate = p.gate + (row * all_cols + (at.c0 >> 3));
-  uint8_t* const scales = p.scales + (row * per_row + at.c0 / kCkptBlock);
-  const bool has_res = p.res != nullptr, has_gate = p.gate != nullptr, has_codes = p.codes != nullptr;
-  const bool leads = (at.col & (p.ckpt_lanes - 1)) == 0;
   const uint32_t step = (uint32_t)g.rp * g.C;
-  for (int k0 = 0; k0 < g.iters; k0 += U) {
-    Raw8<T> xs[U], rs[U];
+  const bool has_res = EXTRA && p.res, has_gate = EXTRA && p.gate, has_codes = EXTRA && p.codes;
+  const T* res = nullptr;
+  int8_t* codes = nullptr;
+  uint8_t *gate = nullptr, *scales = nullptr;
+  uint32_t gate_step = 0, scale_step = 0, all = 0, tail = 0;
+  bool leads = false;
+  if constexpr (EXTRA) {
+    const int all_cols = (g.C + 7) >> 3, per_row = (g.C + kCkptBlock - 1) / kCkptBlock;
+    res = p.res + off;
+    codes = p.codes + off;
+    gate = p.gate + (row * all_cols + (at.c0 >> 3));
+    scales = p.scales + (row * per_row + at.c0 / kCkptBlock);
+    gate_step = (uint32_t)g.rp * all_cols;
+    scale_step = (uint32_t)g.rp * per_row;
+    leads = (at.col & (p.ckpt_lanes - 1)) == 0;
+    all = __ballot_sync(0xffffffffu, at.active);
+    tail = __ballot_sync(0xffffffffu, sh.mine > sh.whole);
+  }
+  for (int k0 = 0; k0 < sh.mine; k0 += U) {
+    Raw8<T> xs[U], rs[EXTRA ? U : 1];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = k0 + u;
-      const bool live = at.active && at.r + k * g.rp < count;
-      xs[u] = live ? fetch(k, (uint32_t)k * step) : Raw8<T>{};
-      if (has_res) rs[u] = live ? raw8_load<T, VEC>(res + (uint32_t)k * step, at.left) : Raw8<T>{};
-    }
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < sh.mine) {
+        const int k = REVERSE ? sh.mine - 1 - (k0 + u) : k0 + u;
+        xs[u] = fetch(k);
+        if constexpr (EXTRA)
+          if (has_res) rs[u] = raw8_load<T, VEC>(res + (uint32_t)k * step, at.left);
+      }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = k0 + u;
-      const bool live = at.active && at.r + k * g.rp < count;
-      const uint32_t o = (uint32_t)k * step;
-      const F8 x = raw8_to_f8(xs[u]);
-      if (live) {
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < sh.mine) {
+        const uint32_t k = REVERSE ? sh.mine - 1 - (k0 + u) : k0 + u, o = k * step;
+        const F8 x = raw8_to_f8(xs[u]);
         F8 z;
 #pragma unroll
         for (int j = 0; j < 4; ++j) z.p[j] = affine.of(j, x.p[j]);
-        if (has_res) {
-          const F8 r = raw8_to_f8(rs[u]);
+        if constexpr (EXTRA)
+          if (has_res) {
+            const F8 r = raw8_to_f8(rs[u]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) z.p[j] = add2(z.p[j], r.p[j]);
-        }
-        if (p.act == ACT_RELU) {
+            for (int j = 0; j < 4; ++j) z.p[j] = add2(z.p[j], r.p[j]);
+          }
+        if (act == ACT_RELU) {
           const Raw8<T> out = f8_to_raw8<T, true>(z);
           raw8_put<T, VEC>(y + o, at.left, out);
-          if (has_gate) gate[(uint32_t)(k * g.rp) * all_cols] = (uint8_t)(positive_bits(out) & (VEC ? 0xFFu : (1u << at.left) - 1));
+          if (has_gate) gate[k * gate_step] = (uint8_t)(positive_bits(out) & (VEC ? 0xFFu : (1u << at.left) - 1));
         } else {
-          if (p.act == ACT_SILU) {
+          if (act == ACT_SILU) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const float2 h = halves(z.p[j]);
@@ -332,113 +420,122 @@ __device__ __forceinline__ void emit(const Forward<T>& p, const Place& at, size_
           }
           raw8_put<T, VEC>(y + o, at.left, f8_to_raw8<T>(z));
         }
-      }
-      if (has_codes) {
-        const CkptScale s = ckpt_scale(ckpt_top_of_lanes(ckpt_top(xs[u]), p.ckpt_lanes));
-        if (live) {
+        if (has_codes) {
+          const CkptScale s = ckpt_scale(ckpt_top_of_lanes(ckpt_top(xs[u]), p.ckpt_lanes, k0 + u < sh.whole ? all : tail));
           store_codes<VEC>(codes + o, 0, at.left, ckpt_codes(x, s));
-          if (leads) scales[(uint32_t)(k * g.rp) * per_row] = (uint8_t)s.byte;
+          if (leads) scales[k * scale_step] = (uint8_t)s.byte;
         }
       }
-    }
   }
+}
+// The constants of a thread's channels from their groups' statistics.
+template <typename T, typename Stat>
+__device__ __forceinline__ void load_affine(const Forward<T>& p, const Place& at, const float (&gamma)[8], const float (&beta)[8], Stat stat, Affine<T>& affine) {
+  float2 m[8];
+  each_channel(at, p.g.Cg, [&](int i, int, int s) { m[i] = stat(s); });
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    affine.set(j, make_float2(m[2 * j].x, m[2 * j + 1].x), make_float2(gamma[2 * j] * m[2 * j].y, gamma[2 * j + 1] * m[2 * j + 1].y),
+               make_float2(beta[2 * j], beta[2 * j + 1]));
 }
 
 // The resident form: blockIdx.x = image * parts + share of its pixels, a cluster per image.
-template <typename T, bool VEC>
+template <typename T, bool VEC, int ACT, bool EXTRA>
 __global__ void __launch_bounds__(kThreads, 2) forward_kernel(const __grid_constant__ Forward<T> p) {
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
-  float* red = reinterpret_cast<float*>(smem + (size_t)g.iters * Slots<T>::Q * kThreads);      // [2048]
-  float* own = red + kThreads * 8;            // mean [G], squared deviations [G] of this CTA's pixels
-  float2* mom = reinterpret_cast<float2*>(own + 2 * g.G);                 // mean, rstd [G] of the image
+  float* red = reinterpret_cast<float*>(smem + (size_t)g.iters * Slots<T>::Q * kThreads);      // [4096]
+  float* common = red + 2 * kThreads * 8;                                                       // [2048]
+  float2* chan = reinterpret_cast<float2*>(common + kThreads * 8);                               // [C]
+  float* own = reinterpret_cast<float*>(chan + g.C);      // mean [G], squared deviations [G] of this CTA's pixels
+  float2* mom = reinterpret_cast<float2*>(own + 2 * g.G);                                        // mean, rstd [G] of the image
   const int rank = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
-  const int p0 = rank * g.pix, count = max(0, min(g.pix, g.P - p0));
-  const size_t row0 = (size_t)n * g.P + p0;
   const Place at(g, 0);
+  const Share sh(g, at, n, rank);
   const Slots<T> slots(smem);
   grid_dependency_wait();
-  if (at.active) {
-    const T* src = p.x + (row0 + at.r) * g.C + at.c0;
-    for (int k = 0; k < g.iters && at.r + k * g.rp < count; ++k) slots.template fetch<VEC>(k, src + (size_t)k * g.rp * g.C, at.left);
-  }
-  float scale[8], shift[8];
+  const T* src = p.x + (sh.row0 + at.r) * g.C + at.c0;
+  const uint32_t step = (uint32_t)g.rp * g.C;
+#pragma unroll 4
+  for (int k = 0; k < sh.mine; ++k) slots.template fetch<VEC>(k, src + (uint32_t)k * step, at.left);
+  float gamma[8], beta[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { scale[i] = p.gamma[at.channel(i)]; shift[i] = p.beta[at.channel(i)]; }
+  for (int i = 0; i < 8; ++i) { gamma[i] = p.gamma[at.channel(i)]; beta[i] = p.beta[at.channel(i)]; }
   copies_done();
-  cta_moments(g, at, slots, count, g.G, g.Cg, g.lanes_g, red, own, [&](int s, float, float m2) { own[g.G + s] = m2; });
+  Moments m;
+  if (sh.mine > 0) m.start(raw8_to_f8(slots.get(0)));
+#pragma unroll 4
+  for (int k = 0; k < sh.mine; ++k) m.add(raw8_to_f8(slots.get(k)));
+  cta_moments(g, at, m, sh.mine, sh.count, g.C, red, common, chan);
+  group_moments(g, sh.count, chan, [&](int s, float mu, float q) { own[s] = mu; own[g.G + s] = q; });
   cg::cluster_group cluster = cg::this_cluster();
   cluster.sync();
-  // Chan: the CTAs' moments about the image's mean; a lane per CTA and group
-  const int j = threadIdx.x & (g.parts - 1);
-  const float in_j = (float)max(0, min(g.pix, g.P - j * g.pix)), inv_p = 1.f / (float)g.P;
-  const float* other = cluster.map_shared_rank(own, j);
-  for (int s0 = 0; s0 < g.G; s0 += kThreads / g.parts) {
-    const int s = s0 + threadIdx.x / g.parts;
-    const float mean_j = s < g.G ? other[s] : 0.f, m2_j = s < g.G ? other[g.G + s] : 0.f;
-    float mu = mean_j * (in_j * inv_p);
-    for (int o = g.parts >> 1; o > 0; o >>= 1) mu += __shfl_xor_sync(0xffffffffu, mu, o);
-    const float d = mean_j - mu;
-    float var = fmaf(in_j * d, d, m2_j / (float)g.Cg);
-    for (int o = g.parts >> 1; o > 0; o >>= 1) var += __shfl_xor_sync(0xffffffffu, var, o);
-    const float rstd = 1.f / sqrtf(fmaf(var, inv_p, p.eps));
-    if (j == 0 && s < g.G) {
-      mom[s] = make_float2(mu, rstd);
-      if (rank == 0) {
-        p.stats[(size_t)n * g.G + s] = mu;
-        p.stats[(size_t)(g.N + n) * g.G + s] = rstd;
-      }
+  image_moments(g, g.parts, p.eps, [&](int j) { return cluster.map_shared_rank(own, j); }, [&](int s, float mu, float rstd) {
+    mom[s] = make_float2(mu, rstd);
+    if (rank == 0) {
+      p.stats[(size_t)n * g.G + s] = mu;
+      p.stats[(size_t)(g.N + n) * g.G + s] = rstd;
     }
-  }
+  });
   cg::cluster_group::arrival_token token = cluster.barrier_arrive();      // this CTA reads its neighbours' sums no more
   __syncthreads();
   Affine<T> affine;
-  float2 m[8];
-  each_channel(at, g.Cg, [&](int i, int, int s) { m[i] = mom[s]; });
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    affine.set(i, make_float2(m[2 * i].x, m[2 * i + 1].x), make_float2(scale[2 * i] * m[2 * i].y, scale[2 * i + 1] * m[2 * i + 1].y),
-               make_float2(shift[2 * i], shift[2 * i + 1]));
-  emit<T, VEC, 2>(p, at, row0, count, affine, [&](int k, uint32_t) { return slots.get(k); });
+  load_affine(p, at, gamma, beta, [&](int s) { return mom[s]; }, affine);
+  emit<T, VEC, ACT, EXTRA, 2, false>(p, at, sh, affine, [&](int k) { return slots.get(k); });
   cluster.barrier_wait(std::move(token));                                 // nor do they read its own
 }
 
-// Streamed, first pass: mean and squared deviations of each channel over a chunk of pixels.
+// Streamed, first pass: moments of each group (with tiles > 1: of each channel) over a CTA's pixels.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads, 2) moments_kernel(const __grid_constant__ Forward<T> p) {
+__global__ void __launch_bounds__(kThreads, 3) moments_kernel(const __grid_constant__ Forward<T> p) {
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
-  float* red = reinterpret_cast<float*>(smem + (size_t)g.iters * Slots<T>::Q * kThreads);
-  float* mean = red + kThreads * 8;
+  float* red = reinterpret_cast<float*>(smem);                                 // [4096]
+  float* common = red + 2 * kThreads * 8;                                      // [2048]
+  float2* chan = reinterpret_cast<float2*>(common + kThreads * 8);             // [8 * cols]
   const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
-  const int p0 = part * g.pix, count = min(g.pix, g.P - p0);
-  const size_t row0 = (size_t)n * g.P + p0;
   Place at(g, blockIdx.y);
   at.active = at.active && at.left > 0;
-  const Slots<T> slots(smem);
+  const Share sh(g, at, n, part);
   grid_dependency_wait();
-  if (at.active) {
-    const T* src = p.x + (row0 + at.r) * g.C + at.c0;
-    for (int k = 0; k < g.iters && at.r + k * g.rp < count; ++k) slots.template fetch<VEC>(k, src + (size_t)k * g.rp * g.C, at.left);
+  grid_dependency_release();
+  const T* src = p.x + (sh.row0 + at.r) * g.C + at.c0;
+  const uint32_t step = (uint32_t)g.rp * g.C;
+  constexpr int U = sizeof(T) == 4 ? 4 : 8;                // vectors in flight
+  Moments m;
+  for (int k0 = 0; k0 < sh.mine; k0 += U) {
+    Raw8<T> xs[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < sh.mine) xs[u] = raw8_load<T, VEC>(src + (uint32_t)(k0 + u) * step, at.left);
+    if (k0 == 0) m.start(raw8_to_f8(xs[0]));
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < sh.mine) m.add(raw8_to_f8(xs[u]));
   }
-  copies_done();
   const int c_first = blockIdx.y * kMaxCols * 8, sets = min(g.cols * 8, g.C - c_first);
-  float* out = p.partial + (size_t)blockIdx.x * 2 * g.C + c_first;
-  cta_moments(g, at, slots, count, sets, 1, g.lanes_c, red, mean, [&](int s, float mu, float m2) {
-    out[s] = mu;
-    out[g.C + s] = m2;
-  });
+  cta_moments(g, at, m, sh.mine, sh.count, sets, red, common, chan);
+  if (g.tiles == 1) {
+    float* out = p.partial + (size_t)blockIdx.x * 2 * g.G;
+    group_moments(g, sh.count, chan, [&](int s, float mu, float q) { out[s] = mu; out[g.G + s] = q; });
+  } else {
+    float* out = p.partial + (size_t)blockIdx.x * 2 * g.C + c_first;
+    for (int c = threadIdx.x; c < sets; c += kThreads) { out[c] = chan[c].x; out[g.C + c] = chan[c].y; }
+  }
 }
 
-// Streamed, second pass: the statistics of group blockIdx.x from the moments of its channels in every chunk.
+// Streamed, between the passes where an image has many rows: the statistics of group blockIdx.x from the moments of its
+// channels (tiles > 1) or its own in every row, in fp64.
 template <typename T>
 __global__ void __launch_bounds__(1024) combine_kernel(const __grid_constant__ Forward<T> p) {
   __shared__ double part[32];
   __shared__ double total;
   const Geom& g = p.g;
   const int n = blockIdx.x / g.G, s = blockIdx.x % g.G, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  const float* src = p.partial + (size_t)n * g.parts * 2 * g.C + (size_t)s * g.Cg;
+  const int width = g.tiles == 1 ? g.G : g.C, size = g.tiles == 1 ? 1 : g.Cg;      // of a row, of the group's share of it
+  const float* src = p.partial + (size_t)n * g.parts * 2 * width + (size_t)s * size;
   grid_dependency_wait();
+  grid_dependency_release();
   auto sum = [&](double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -453,56 +550,68 @@ __global__ void __launch_bounds__(1024) combine_kernel(const __grid_constant__ F
     return total;
   };
   auto each = [&](auto take) {
-    const int step = blockDim.x / g.Cg, over = blockDim.x - step * g.Cg;
-    int chunk = threadIdx.x / g.Cg, c = threadIdx.x - chunk * g.Cg;
-    while (chunk < g.parts) {
-      const float* row = src + (size_t)chunk * 2 * g.C + c;
-      take((double)min(g.pix, g.P - chunk * g.pix), (double)row[0], row + g.C);
-      chunk += step; c += over;
-      if (c >= g.Cg) { c -= g.Cg; ++chunk; }
+    const int step = blockDim.x / size, over = blockDim.x - step * size;
+    int j = threadIdx.x / size, c = threadIdx.x - j * size;
+    while (j < g.parts) {
+      const float* row = src + (size_t)j * 2 * width + c;
+      take((double)min(g.pix, g.P - j * g.pix), (double)row[0], row + width);
+      j += step; c += over;
+      if (c >= size) { c -= size; ++j; }
     }
   };
-  const double m = (double)g.P * g.Cg;
+  const double values = (double)g.P * size;
   double a = 0.0;
   each([&](double cnt, double mu, const float*) { a += cnt * mu; });
-  const double mean = sum(a) / m;
+  const double mean = sum(a) / values;
   a = 0.0;
-  each([&](double cnt, double mu, const float* m2) { a += (double)*m2 + cnt * (mu - mean) * (mu - mean); });
-  const double var = sum(a) / m;
+  const double per = g.tiles == 1 ? (double)g.Cg : 1.0;                            // values behind a pixel of a row's entry
+  each([&](double cnt, double mu, const float* m2) { a += (double)*m2 + cnt * per * (mu - mean) * (mu - mean); });
+  const double var = sum(a) / ((double)g.P * g.Cg);
   if (threadIdx.x == 0) {
     p.stats[(size_t)n * g.G + s] = (float)mean;
     p.stats[(size_t)(g.N + n) * g.G + s] = (float)(1.0 / sqrt(var + (double)p.eps));
   }
 }
 
-// Streamed, last pass: y from x and the statistics, the last chunks first.
-template <typename T, bool VEC>
+// Streamed, second pass: y from x and the statistics, which every CTA of an image forms from the rows of sums itself (the same
+// bits everywhere; its first CTA writes them out) unless combine_kernel has.
+template <typename T, bool VEC, int ACT, bool EXTRA>
 __global__ void __launch_bounds__(kThreads, 2) apply_kernel(const __grid_constant__ Forward<T> p) {
+  extern __shared__ uint4 smem[];
+  float2* mom = reinterpret_cast<float2*>(smem);           // [G], unless combined
   const Geom& g = p.g;
-  const int block = gridDim.x - 1 - blockIdx.x, part = block % g.parts, n = block / g.parts;
-  const int p0 = part * g.pix, count = min(g.pix, g.P - p0);
-  const size_t row0 = (size_t)n * g.P + p0;
+  const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
   Place at(g, blockIdx.y);
   at.active = at.active && at.left > 0;
-  if (!at.active) at.c0 = 0;
-  Affine<T> affine;
-  float mean[8], scale[8], shift[8];
+  if (at.left <= 0) { at.c0 = 0; at.left = 1; }
+  const Share sh(g, at, n, part);
+  float gamma[8], beta[8];
   grid_dependency_wait();
-  each_channel(at, g.Cg, [&](int i, int c, int s) {
-    c = at.active ? c : 0;
-    s = at.active ? s : 0;
-    mean[i] = p.stats[(size_t)n * g.G + s];
-    scale[i] = p.gamma[c] * p.stats[(size_t)(g.N + n) * g.G + s];
-    shift[i] = p.beta[c];
-  });
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    affine.set(j, make_float2(mean[2 * j], mean[2 * j + 1]), make_float2(scale[2 * j], scale[2 * j + 1]), make_float2(shift[2 * j], shift[2 * j + 1]));
-  const T* x = p.x + (row0 + at.r) * g.C + at.c0;
-  emit<T, VEC, sizeof(T) == 2 ? 4 : 2>(p, at, row0, count, affine, [&](int, uint32_t o) { return raw8_load<T, VEC>(x + o, at.left); });
+  for (int i = 0; i < 8; ++i) { gamma[i] = p.gamma[at.channel(i)]; beta[i] = p.beta[at.channel(i)]; }
+  if (!p.combined) {
+    const float* rows = p.partial + (size_t)n * g.parts * 2 * g.G;
+    image_moments(g, g.parts, p.eps, [&](int j) { return rows + (size_t)j * 2 * g.G; }, [&](int s, float mu, float rstd) {
+      mom[s] = make_float2(mu, rstd);
+      if (part == 0) {
+        p.stats[(size_t)n * g.G + s] = mu;
+        p.stats[(size_t)(g.N + n) * g.G + s] = rstd;
+      }
+    });
+    __syncthreads();
+  }
+  Affine<T> affine;
+  if (p.combined)
+    load_affine(p, at, gamma, beta, [&](int s) { return make_float2(p.stats[(size_t)n * g.G + s], p.stats[(size_t)(g.N + n) * g.G + s]); }, affine);
+  else
+    load_affine(p, at, gamma, beta, [&](int s) { return mom[s]; }, affine);
+  const T* x = p.x + (sh.row0 + at.r) * g.C + at.c0;
+  const uint32_t step = (uint32_t)g.rp * g.C;
+  emit<T, VEC, ACT, EXTRA, sizeof(T) == 2 ? 4 : 2, true>(p, at, sh, affine, [&](int k) { return raw8_load<T, VEC>(x + (uint32_t)k * step, at.left); });
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------
+enum { SLOPE_ONE = 0, SLOPE_MASK = 1, SLOPE_BITS = 2, SLOPE_SILU = 3 };      // act' from nothing, from y, from y's bits, from z
 template <typename T> struct Backward {
   Geom g;
   const T* dy;
@@ -516,26 +625,49 @@ template <typename T> struct Backward {
   const uint8_t* gate;
   const T* res;
   T* dx;
-  float* partial;             // streamed: [N][parts][2][C]
-  float* totals;              // [N][2][C]: A, B
-  int act;
+  float* partial;             // streamed: [N][parts][2][C]: A, B of each CTA
+  float* totals;              // [N][2][C]: A, B of each image; streamed: null if the second pass adds up the rows itself
+  int slope;
 };
 
 // The operands of one column of 8 channels at a pixel, raw.
 template <typename T, bool CK> struct Held {
   Raw8<T> dy;
-  Raw8<T> x;
-  uint2 codes;
-  uint32_t scale, open;       // scale byte of the codes, bits of the gate (all set without ReLU)
+  Raw8<T> x;                  // the column of x, or
+  uint2 codes;                // its codes and
+  uint32_t scale;             // their scale byte
+  Raw8<T> mask;               // SLOPE_MASK
+  uint32_t open;              // SLOPE_BITS
 };
-
-template <typename T, bool VEC> __device__ __forceinline__ uint32_t open_bits(const Backward<T>& p, const Place& at, size_t row) {
-  if (p.gate) return p.gate[row * ((p.g.C + 7) >> 3) + (at.c0 >> 3)];
-  return positive_bits(raw8_load<T, VEC>(p.mask + row * p.g.C + at.c0, at.left));
-}
-__device__ __forceinline__ size_t scale_index(const Geom& g, const Place& at, size_t row) {
-  return row * ((g.C + kCkptBlock - 1) / kCkptBlock) + at.c0 / kCkptBlock;
-}
+// Where a thread's columns start in the tensors, and how far apart its pixels are.
+template <typename T> struct Columns {
+  const T *dy, *x, *mask;
+  const int8_t* codes;
+  const uint8_t *scales, *gate;
+  uint32_t step, gate_step, scale_step;
+  __device__ __forceinline__ Columns(const Backward<T>& p, const Place& at, const Share& sh) {
+    const Geom& g = p.g;
+    const int all_cols = (g.C + 7) >> 3, per_row = (g.C + kCkptBlock - 1) / kCkptBlock;
+    const size_t row = sh.row0 + at.r, off = row * g.C + at.c0;
+    dy = p.dy + off; x = p.x + off; mask = p.mask + off; codes = p.codes + off;
+    scales = p.scales + (row * per_row + at.c0 / kCkptBlock);
+    gate = p.gate + (row * all_cols + (at.c0 >> 3));
+    step = (uint32_t)g.rp * g.C; gate_step = (uint32_t)g.rp * all_cols; scale_step = (uint32_t)g.rp * per_row;
+  }
+  template <bool VEC, bool CK> __device__ __forceinline__ Held<T, CK> load(uint32_t k, int left, int slope) const {
+    Held<T, CK> h;
+    h.dy = raw8_load<T, VEC>(dy + k * step, left);
+    if constexpr (CK) {
+      h.codes = load_codes<VEC>(codes + k * step, 0, left);
+      h.scale = scales[k * scale_step];
+    } else {
+      h.x = raw8_load<T, VEC>(x + k * step, left);
+    }
+    if (slope == SLOPE_MASK) h.mask = raw8_load<T, VEC>(mask + k * step, left);
+    if (slope == SLOPE_BITS) h.open = gate[k * gate_step];
+    return h;
+  }
+};
 
 // A thread's 8 channels: the mean with its sign turned, gamma * rstd, beta.
 struct Channels {
@@ -565,10 +697,16 @@ __device__ __forceinline__ Raw8<float> opened(const Raw8<float>& dy, uint32_t op
   return r;
 }
 
-// x - mean and dz of one vector; h.dy is gated already where the gate is ReLU's.
+// dy where it passes ReLU.
+template <typename T, bool CK> __device__ __forceinline__ Raw8<T> passed(const Held<T, CK>& h, int slope) {
+  if (slope == SLOPE_MASK) return opened(h.dy, positive_bits(h.mask));
+  if (slope == SLOPE_BITS) return opened(h.dy, h.open);
+  return h.dy;
+}
+// x - mean, and dz from the dy that passes.
 template <typename T, bool CK>
-__device__ __forceinline__ void operands(const Held<T, CK>& h, int act, const Channels& ch, F8& dz, F8& d) {
-  dz = raw8_to_f8(h.dy);
+__device__ __forceinline__ void operands(const Raw8<T>& dy, const Held<T, CK>& h, int slope, const Channels& ch, F8& dz, F8& d) {
+  dz = raw8_to_f8(dy);
   if constexpr (CK) {
     d = ckpt_numbers(h.codes);
     const f32x2 step = pair(ckpt_step(h.scale));
@@ -579,7 +717,7 @@ __device__ __forceinline__ void operands(const Held<T, CK>& h, int act, const Ch
 #pragma unroll
     for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], ch.less[j]);
   }
-  if (act == ACT_SILU) {
+  if (slope == SLOPE_SILU) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float2 z = halves(fma2(d.p[j], ch.scale[j], ch.shift[j]));
@@ -588,68 +726,54 @@ __device__ __forceinline__ void operands(const Held<T, CK>& h, int act, const Ch
   }
 }
 
-// dx of this CTA's pixels: fetch(k) gives the thread's k-th operands; k1 = -rstd*S1/m, k2 = -rstd^2*S2/m.
-template <typename T, bool VEC, bool CK, int U, typename Fetch>
-__device__ __forceinline__ void emit_dx(const Backward<T>& p, const Place& at, size_t row0, int count, const Channels& ch,
+// dx of this CTA's pixels: fetch(k) gives the thread's k-th operands; k1 = -rstd*S1/m, k2 = -rstd^2*S2/m.  GATED: dy comes
+// gated.
+template <typename T, bool VEC, bool CK, int U, bool REVERSE, bool GATED, typename Fetch>
+__device__ __forceinline__ void emit_dx(const Backward<T>& p, const Place& at, const Share& sh, int slope, const Channels& ch,
                                         const f32x2 (&k1)[4], const f32x2 (&k2)[4], Fetch fetch) {
-  const Geom& g = p.g;
-  if (!at.active) return;
-  const size_t off = (row0 + at.r) * g.C + at.c0;
+  const size_t off = (sh.row0 + at.r) * p.g.C + at.c0;
   T* const dx = p.dx + off;
   const T* const res = p.res + off;
   const bool has_res = p.res != nullptr;
-  const uint32_t step = (uint32_t)g.rp * g.C;
-  for (int k0 = 0; k0 < g.iters; k0 += U) {
-    if (at.r + k0 * g.rp >= count) break;
+  const uint32_t step = (uint32_t)p.g.rp * p.g.C;
+  for (int k0 = 0; k0 < sh.mine; k0 += U) {
     Held<T, CK> hs[U];
     Raw8<T> rs[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (at.r + (k0 + u) * g.rp >= count) continue;
-      hs[u] = fetch(k0 + u);
-      if (has_res) rs[u] = raw8_load<T, VEC>(res + (uint32_t)(k0 + u) * step, at.left);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (at.r + (k0 + u) * g.rp >= count) continue;
-      F8 dz, d;
-      operands<T, CK>(hs[u], p.act, ch, dz, d);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) dz.p[j] = fma2(ch.scale[j], dz.p[j], fma2(d.p[j], k2[j], k1[j]));
-      if (has_res) {
-        const F8 r = raw8_to_f8(rs[u]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) dz.p[j] = add2(dz.p[j], r.p[j]);
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < sh.mine) {
+        const uint32_t k = REVERSE ? sh.mine - 1 - (k0 + u) : k0 + u;
+        hs[u] = fetch(k);
+        if (has_res) rs[u] = raw8_load<T, VEC>(res + k * step, at.left);
       }
-      raw8_put<T, VEC>(dx + (uint32_t)(k0 + u) * step, at.left, f8_to_raw8<T>(dz));
-    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < sh.mine) {
+        const uint32_t k = REVERSE ? sh.mine - 1 - (k0 + u) : k0 + u;
+        F8 dz, d;
+        operands<T, CK>(GATED ? hs[u].dy : passed<T, CK>(hs[u], slope), hs[u], slope, ch, dz, d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dz.p[j] = fma2(ch.scale[j], dz.p[j], fma2(d.p[j], k2[j], k1[j]));
+        if (has_res) {
+          const F8 r = raw8_to_f8(rs[u]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dz.p[j] = add2(dz.p[j], r.p[j]);
+        }
+        raw8_put<T, VEC>(dx + k * step, at.left, f8_to_raw8<T>(dz));
+      }
   }
 }
 
-template <typename T, bool VEC, bool CK>
-__device__ __forceinline__ Held<T, CK> load_held(const Backward<T>& p, const Place& at, size_t row) {
-  Held<T, CK> h;
-  const size_t off = row * p.g.C + at.c0;
-  h.dy = raw8_load<T, VEC>(p.dy + off, at.left);
-  if constexpr (CK) {
-    h.codes = load_codes<VEC>(p.codes, off, at.left);
-    h.scale = p.scales[scale_index(p.g, at, row)];
-  } else {
-    h.x = raw8_load<T, VEC>(p.x + off, at.left);
-  }
-  h.open = p.act == ACT_RELU ? open_bits<T, VEC>(p, at, row) : 0xFFu;
-  return h;
-}
 // The constants of a thread's channels from the saved statistics.
 template <typename T>
-__device__ __forceinline__ void load_channels(const Backward<T>& p, const Place& at, int n, Channels& ch, float (&rstd)[8]) {
+__device__ __forceinline__ void load_channels(const Backward<T>& p, const Place& at, int n, int slope, Channels& ch, float (&rstd)[8]) {
   const Geom& g = p.g;
   float mean[8], scale[8], shift[8];
   each_channel(at, g.Cg, [&](int i, int c, int s) {
     mean[i] = p.stats[(size_t)n * g.G + s];
     rstd[i] = p.stats[(size_t)(g.N + n) * g.G + s];
     scale[i] = p.gamma[c] * rstd[i];
-    shift[i] = p.act == ACT_SILU ? p.beta[c] : 0.f;
+    shift[i] = slope == SLOPE_SILU ? p.beta[c] : 0.f;
   });
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -692,10 +816,11 @@ struct Sums {
 
 // The resident form.  Shared memory: the thread's vectors of dy and x (or its codes), a byte per vector for the gate's bits and
 // one for the scale; then per-thread sums, per-channel sums A, B and per-group sums S1, S2 of this CTA, and k1, k2 of the image.
-template <typename T, bool VEC, bool CK>
+template <typename T, bool VEC, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_constant__ Backward<T> p) {
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
+  const int slope = SLOPE < 0 ? p.slope : SLOPE;
   const size_t vecs = (size_t)g.iters * kThreads;
   uint4* xs = smem + vecs * Slots<T>::Q;
   uint2* cs = reinterpret_cast<uint2*>(xs);
@@ -706,37 +831,49 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
   uint8_t* open = reinterpret_cast<uint8_t*>(coef + 2 * g.G);
   uint8_t* scale_bytes = open + vecs;
   const int rank = blockIdx.x % g.parts, n = blockIdx.x / g.parts, tid = threadIdx.x;
-  const int p0 = rank * g.pix, count = max(0, min(g.pix, g.P - p0));
-  const size_t row0 = (size_t)n * g.P + p0;
   const Place at(g, 0);
+  const Share sh(g, at, n, rank);
   const Slots<T> dys(smem), xslots(xs);
+  const Columns<T> from(p, at, sh);
   grid_dependency_wait();
-  if (at.active) {
+  grid_dependency_release();
 #pragma unroll 4
-    for (int k = 0; k < g.iters; ++k) {
-      const int pixel = at.r + k * g.rp;
-      if (pixel >= count) break;
-      const size_t row = row0 + pixel, off = row * g.C + at.c0;
-      dys.template fetch<VEC>(k, p.dy + off, at.left);
-      if constexpr (CK) {
-        if constexpr (VEC) copy8_async(cs + k * kThreads + tid, p.codes + off); else cs[k * kThreads + tid] = load_codes<false>(p.codes, off, at.left);
-      } else {
-        xslots.template fetch<VEC>(k, p.x + off, at.left);
-      }
+  for (int k = 0; k < sh.mine; ++k) {
+    const uint32_t o = (uint32_t)k * from.step;
+    dys.template fetch<VEC>(k, from.dy + o, at.left);
+    if constexpr (CK) {
+      if constexpr (VEC) copy8_async(cs + k * kThreads + tid, from.codes + o); else cs[k * kThreads + tid] = load_codes<false>(from.codes + o, 0, at.left);
+    } else {
+      xslots.template fetch<VEC>(k, from.x + o, at.left);
     }
-#pragma unroll 4
-    for (int k = 0; k < g.iters; ++k) {
-      const int pixel = at.r + k * g.rp;
-      if (pixel >= count) break;
-      if (p.act == ACT_RELU) open[k * kThreads + tid] = (uint8_t)open_bits<T, VEC>(p, at, row0 + pixel);
-      if constexpr (CK) scale_bytes[k * kThreads + tid] = p.scales[scale_index(g, at, row0 + pixel)];
+  }
+  // what comes in bytes goes through registers, several loads in flight
+  if (CK || slope == SLOPE_MASK || slope == SLOPE_BITS) {
+    constexpr int U = 4;
+    for (int k0 = 0; k0 < sh.mine; k0 += U) {
+      uint32_t sc[U], bits[U];
+      Raw8<T> m[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (k0 + u < sh.mine) {
+          if constexpr (CK) sc[u] = from.scales[(uint32_t)(k0 + u) * from.scale_step];
+          if (slope == SLOPE_BITS) bits[u] = from.gate[(uint32_t)(k0 + u) * from.gate_step];
+          if (slope == SLOPE_MASK) m[u] = raw8_load<T, VEC>(from.mask + (uint32_t)(k0 + u) * from.step, at.left);
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (k0 + u < sh.mine) {
+          if constexpr (CK) scale_bytes[(k0 + u) * kThreads + tid] = (uint8_t)sc[u];
+          if (slope == SLOPE_BITS) open[(k0 + u) * kThreads + tid] = (uint8_t)bits[u];
+          if (slope == SLOPE_MASK) open[(k0 + u) * kThreads + tid] = (uint8_t)positive_bits(m[u]);
+        }
     }
   }
   Channels ch;
   float rstd[8];
-  load_channels(p, at, n, ch, rstd);
+  load_channels(p, at, n, slope, ch, rstd);
   copies_done();
-  auto held = [&](int k) {
+  auto held = [&](uint32_t k) {
     Held<T, CK> h;
     h.dy = dys.get(k);
     if constexpr (CK) {
@@ -748,29 +885,23 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
     return h;
   };
   Sums sums;
-  if (at.active)
 #pragma unroll 2
-    for (int k = 0; k < g.iters; ++k) {
-      if (at.r + k * g.rp >= count) break;
-      Held<T, CK> h = held(k);
-      if (p.act == ACT_RELU) {
-        h.dy = opened(h.dy, open[k * kThreads + tid]);
-        dys.put(k, h.dy);                           // gated once, for the second sweep too
-      }
-      F8 dz, d;
-      operands<T, CK>(h, p.act, ch, dz, d);
-      sums.add(dz, d);
+  for (int k = 0; k < sh.mine; ++k) {
+    Held<T, CK> h = held(k);
+    if (slope == SLOPE_MASK || slope == SLOPE_BITS) {
+      h.dy = opened(h.dy, open[k * kThreads + tid]);
+      dys.put(k, h.dy);                           // gated once, for the second sweep too
     }
+    F8 dz, d;
+    operands<T, CK>(h.dy, h, slope, ch, dz, d);
+    sums.add(dz, d);
+  }
   sums.put(red, g, at, rstd);
   __syncthreads();
-  const int width = g.cols * 8;
-  for (int s = 0; s < 2; ++s) {
-    const float* from = red + s * kThreads * 8;
-    add_sets(g.rp, g.C, 1, g.lanes_c, [&](int r, int c) { return from[r * width + c]; }, [&](int c, float sum) { chan[s * g.C + c] = sum; });
-  }
+  channel_sums(red, g, g.C, g.lanes_c, [&](int c, float a, float b) { chan[c] = a; chan[g.C + c] = b; });
   __syncthreads();
-  add_sets(1, g.G, g.Cg, g.lanes_g, [&](int, int c) { return p.gamma[c] * chan[g.C + c]; }, [&](int s, float sum) { own[s] = sum; });
-  add_sets(1, g.G, g.Cg, g.lanes_g, [&](int, int c) { return p.gamma[c] * chan[c]; }, [&](int s, float sum) { own[g.G + s] = sum; });
+  group_sums(g.G, g.Cg, g.lanes_g, [&](int c) { const float w = p.gamma[c]; return make_float2(w * chan[g.C + c], w * chan[c]); },
+             [&](int s, float s1, float s2) { own[s] = s1; own[g.G + s] = s2; });
   cg::cluster_group cluster = cg::this_cluster();
   cluster.sync();
   const float inv_m = (float)(1.0 / ((double)g.P * g.Cg));
@@ -793,62 +924,54 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
   }
   cg::cluster_group::arrival_token token = cluster.barrier_arrive();
   __syncthreads();
-  grid_dependency_release();
   f32x2 k1[4], k2[4];
   load_coefficients(at, g.Cg, coef, coef + g.G, 0, k1, k2);
-  emit_dx<T, VEC, CK, 2>(p, at, row0, count, ch, k1, k2, held);
+  emit_dx<T, VEC, CK, 2, false, true>(p, at, sh, slope, ch, k1, k2, held);
   cluster.barrier_wait(std::move(token));
 }
 
-// Streamed, first pass: A and B of each channel over a chunk of pixels.
-template <typename T, bool VEC, bool CK>
+// Streamed, first pass: A and B of each channel over a CTA's pixels.
+template <typename T, bool VEC, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid_constant__ Backward<T> p) {
-  __shared__ __align__(16) float red[2][kThreads * 8];
+  __shared__ __align__(16) float red[2 * kThreads * 8];
   const Geom& g = p.g;
+  const int slope = SLOPE < 0 ? p.slope : SLOPE;
   const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
-  const int p0 = part * g.pix, count = min(g.pix, g.P - p0);
-  const size_t row0 = (size_t)n * g.P + p0;
   Place at(g, blockIdx.y);
   at.active = at.active && at.left > 0;
-  if (!at.active) at.c0 = blockIdx.y * kMaxCols * 8;
+  if (at.left <= 0) { at.c0 = blockIdx.y * kMaxCols * 8; at.left = 1; }
+  const Share sh(g, at, n, part);
+  const Columns<T> from(p, at, sh);
   grid_dependency_wait();
+  grid_dependency_release();
   Channels ch;
   float rstd[8];
-  load_channels(p, at, n, ch, rstd);
+  load_channels(p, at, n, slope, ch, rstd);
   Sums sums;
-  auto add = [&](const Held<T, CK>& h) {
-    F8 dz, d;
-    operands<T, CK>(h, p.act, ch, dz, d);
-    sums.add(dz, d);
-  };
-  if (at.active) {
-    constexpr int U = sizeof(T) == 4 ? 2 : 4;             // vectors in flight
-    int pixel = at.r;
-    for (; pixel + (U - 1) * g.rp < count; pixel += U * g.rp) {
-      Held<T, CK> h[U];
+  constexpr int U = sizeof(T) == 4 ? 2 : 4;               // vectors in flight
+  for (int k0 = 0; k0 < sh.mine; k0 += U) {
+    Held<T, CK> h[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) h[u] = load_held<T, VEC, CK>(p, at, row0 + pixel + u * g.rp);
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < sh.mine) h[u] = from.template load<VEC, CK>(k0 + u, at.left, slope);
 #pragma unroll
-      for (int u = 0; u < U; ++u) { h[u].dy = opened(h[u].dy, h[u].open); add(h[u]); }
-    }
-    for (; pixel < count; pixel += g.rp) {
-      Held<T, CK> h = load_held<T, VEC, CK>(p, at, row0 + pixel);
-      h.dy = opened(h.dy, h.open);
-      add(h);
-    }
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < sh.mine) {
+        F8 dz, d;
+        operands<T, CK>(passed<T, CK>(h[u], slope), h[u], slope, ch, dz, d);
+        sums.add(dz, d);
+      }
   }
-  sums.put(red[0], g, at, rstd);
+  sums.put(red, g, at, rstd);
   __syncthreads();
-  const int width = g.cols * 8, c_first = blockIdx.y * kMaxCols * 8, sets = min(width, g.C - c_first);
-  for (int s = 0; s < 2; ++s) {
-    float* out = p.partial + ((size_t)blockIdx.x * 2 + s) * g.C + c_first;
-    add_sets(g.rp, sets, 1, g.lanes_c, [&](int r, int c) { return red[s][r * width + c]; }, [&](int c, float sum) { out[c] = sum; });
-  }
+  const int c_first = blockIdx.y * kMaxCols * 8, sets = min(g.cols * 8, g.C - c_first);
+  float* out = p.partial + (size_t)blockIdx.x * 2 * g.C + c_first;
+  channel_sums(red, g, sets, g.lanes_c, [&](int c, float a, float b) { out[c] = a; out[g.C + c] = b; });
 }
 
 // out[j][i] = the sum of `rows` rows of `width` floats from in[j * rows] on, j = blockIdx.x / blocks; a block takes 32 of
-// the width, its warps every 32nd row, and adds in fp64.  Streamed, second pass (a row per chunk), and, for all forms, the
-// parameter gradients (a row per image; `split` > 0: values from there on go to out2).
+// the width, its warps every 32nd row, and adds in fp64.  Streamed, between the passes where an image has many rows, and, for
+// all forms, the parameter gradients (`split` > 0: values from there on go to out2).
 __global__ void __launch_bounds__(1024) add_rows_kernel(const float* __restrict__ in, int rows, int width, float* __restrict__ out,
                                                         float* __restrict__ out2, int split) {
   __shared__ double fin[32][33];
@@ -858,6 +981,7 @@ __global__ void __launch_bounds__(1024) add_rows_kernel(const float* __restrict_
   in += (size_t)j * rows * width;
   out += (size_t)j * width;
   grid_dependency_wait();
+  grid_dependency_release();
   double t = 0.0;
   if (i < width)
 #pragma unroll 4
@@ -872,46 +996,53 @@ __global__ void __launch_bounds__(1024) add_rows_kernel(const float* __restrict_
   if (split > 0 && ii >= split) out2[ii - split] = (float)t; else out[ii] = (float)t;
 }
 
-// Streamed, last pass: dx, the last chunks first.  Every CTA forms S1 and S2 of its tile's groups from the image's totals.
-template <typename T, bool VEC, bool CK>
+// Streamed, second pass: dx.  Every CTA forms S1 and S2 of its tile's groups from the image's totals, or from its rows of sums.
+template <typename T, bool VEC, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __grid_constant__ Backward<T> p) {
   __shared__ float coef[2][kMaxCols * 8];
   const Geom& g = p.g;
-  const int block = gridDim.x - 1 - blockIdx.x, part = block % g.parts, n = block / g.parts;
-  const int p0 = part * g.pix, count = min(g.pix, g.P - p0);
-  const size_t row0 = (size_t)n * g.P + p0;
+  const int slope = SLOPE < 0 ? p.slope : SLOPE;
+  const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
+  const int c_first = blockIdx.y * kMaxCols * 8;
   Place at(g, blockIdx.y);
   at.active = at.active && at.left > 0;
-  if (!at.active) at.c0 = blockIdx.y * kMaxCols * 8;
-  const int c_first = blockIdx.y * kMaxCols * 8, c_last = min(g.C, c_first + g.cols * 8) - 1;
-  const int g_first = c_first / g.Cg, sets = c_last / g.Cg - g_first + 1;
+  if (at.left <= 0) { at.c0 = c_first; at.left = 1; }
+  const Share sh(g, at, n, part);
+  const Columns<T> from(p, at, sh);
+  const int c_last = min(g.C, c_first + g.cols * 8) - 1;
+  const int g_first = c_first / g.Cg, sets = c_last / g.Cg - g_first + 1, c_base = g_first * g.Cg;
   const float inv_m = (float)(1.0 / ((double)g.P * g.Cg));
   grid_dependency_wait();
-  const float* tot = p.totals + (size_t)n * 2 * g.C;
-  const float* rs = p.stats + (size_t)(g.N + n) * g.G + g_first;
-  const int c_base = g_first * g.Cg;
-  add_sets(1, sets, g.Cg, g.lanes_g, [&](int, int c) { return p.gamma[c_base + c] * tot[g.C + c_base + c]; },
-           [&](int s, float sum) { coef[0][s] = rs[s] * sum * inv_m; });
-  add_sets(1, sets, g.Cg, g.lanes_g, [&](int, int c) { return p.gamma[c_base + c] * tot[c_base + c]; },
-           [&](int s, float sum) { coef[1][s] = rs[s] * rs[s] * sum * inv_m; });
-  __syncthreads();
+  grid_dependency_release();
   Channels ch;
   float rstd[8];
-  f32x2 k1[4], k2[4];
-  load_channels(p, at, n, ch, rstd);
-  load_coefficients(at, g.Cg, coef[0], coef[1], g_first, k1, k2);
-  emit_dx<T, VEC, CK, 2>(p, at, row0, count, ch, k1, k2, [&](int k) {
-    Held<T, CK> h = load_held<T, VEC, CK>(p, at, row0 + at.r + k * g.rp);
-    h.dy = opened(h.dy, h.open);
-    return h;
+  load_channels(p, at, n, slope, ch, rstd);
+  const int rows = p.totals ? 1 : g.parts;
+  const float* src = p.totals ? p.totals + (size_t)n * 2 * g.C : p.partial + (size_t)n * g.parts * 2 * g.C;
+  const float* rs = p.stats + (size_t)(g.N + n) * g.G + g_first;
+  group_sums(sets, g.Cg, g.lanes_g, [&](int c) {
+    c += c_base;
+    float a = 0.f, b = 0.f;
+#pragma unroll 4
+    for (int j = 0; j < rows; ++j) { a += src[(size_t)j * 2 * g.C + c]; b += src[(size_t)j * 2 * g.C + g.C + c]; }
+    const float w = p.gamma[c];
+    return make_float2(w * b, w * a);
+  }, [&](int s, float s1, float s2) {
+    coef[0][s] = rs[s] * s1 * inv_m;
+    coef[1][s] = rs[s] * rs[s] * s2 * inv_m;
   });
+  __syncthreads();
+  f32x2 k1[4], k2[4];
+  load_coefficients(at, g.Cg, coef[0], coef[1], g_first, k1, k2);
+  emit_dx<T, VEC, CK, sizeof(T) == 2 ? 4 : 2, true, false>(p, at, sh, slope, ch, k1, k2,
+                                                          [&](uint32_t k) { return from.template load<VEC, CK>(k, at.left, slope); });
 }
 
 // ---- host side: plans ----------------------------------------------------------------------------------------
 struct Plan {
   Geom g;
   bool resident;
-  size_t smem;                // dynamic shared memory of the resident kernel, or of moments_kernel
+  size_t smem;                // dynamic shared memory of the resident kernel
 };
 inline int pow2_up_to(int64_t most, int cap) {
   int v = 1;
@@ -919,11 +1050,11 @@ inline int pow2_up_to(int64_t most, int cap) {
   return v;
 }
 constexpr size_t kSmemMost = 220 * 1024;        // of 227 KB
-constexpr size_t kSmemShare = 72 * 1024;        // three CTAs on an SM: one's copies run beside another's arithmetic
-constexpr int kStreamIters = 16;                // pixels per thread and chunk of the streamed form, 16-bit storage
+constexpr size_t kSmemShare = 110 * 1024;       // two CTAs on an SM: one's copies run beside another's arithmetic
 
-// `vec_bytes`: shared memory per vector of 8 channels; `fixed`: besides the vectors.
-inline Plan plan(int N, int P, int C, int G, size_t vec_bytes, size_t fixed, int stream_iters) {
+// `vec_bytes`: shared memory per vector of 8 channels in the resident form; `fixed`: besides the vectors; `per_sm`: CTAs of the
+// streamed form on an SM.
+inline Plan plan(int N, int P, int C, int G, size_t vec_bytes, size_t fixed, int per_sm) {
   Plan pl{};
   Geom& g = pl.g;
   g.N = N; g.P = P; g.C = C; g.G = G; g.Cg = C / G;
@@ -934,36 +1065,33 @@ inline Plan plan(int N, int P, int C, int G, size_t vec_bytes, size_t fixed, int
   g.lanes_g = pow2_up_to(kThreads / std::min(G, kThreads), 32);
   g.lanes_c = pow2_up_to(kThreads / std::min(g.cols * 8, kThreads), 32);
   auto split = [&](int parts) {
-    g.parts = parts;
     g.pix = P / parts + (P % parts != 0);
+    g.parts = parts;
     g.iters = g.pix / g.rp + (g.pix % g.rp != 0);
     return (size_t)g.iters * kThreads * vec_bytes + fixed;
   };
-  if (g.tiles == 1) {
+  const char* f_ = getenv("GN_FORM");
+  if (g.tiles == 1 && !(f_ && f_[0] == 's')) {
     int parts = 1;
     while (parts < kMaxCluster && split(parts) > kSmemShare) parts *= 2;
     // few images: more SMs, while every thread keeps two pixels
     while (parts < kMaxCluster && (int64_t)N * parts * 2 <= 2 * kSms && (split(parts), g.iters) >= 4) parts *= 2;
     pl.smem = split(parts);
-    pl.resident = pl.smem <= kSmemMost && (int64_t)N * parts <= INT32_MAX;
+    pl.resident = pl.smem <= kSmemMost && (int64_t)N * g.parts <= INT32_MAX;
+    if (f_ && f_[0] == 'o') pl.resident = pl.resident && (int64_t)N * g.parts <= 2 * kSms;
     if (pl.resident) return pl;
   }
-  g.iters = stream_iters;
-  g.pix = std::min(P, g.rp * stream_iters);
-  g.iters = (g.pix + g.rp - 1) / g.rp;
-  g.parts = P / g.pix + (P % g.pix != 0);
-  pl.smem = (size_t)g.iters * kThreads * vec_bytes + fixed;
+  // one wave of CTAs, each with at least one batch of pixels in flight
+  split((int)std::max<int64_t>(1, std::min<int64_t>((int64_t)per_sm * kSms / N, P / (4 * g.rp))));
+  g.parts = P / g.pix + (P % g.pix != 0);         // none without pixels
   return pl;
 }
 inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G) {
-  const size_t red = kThreads * 8 * 4;
-  Plan pl = plan(N, P, C, G, 8 * (size_t)elem_bytes, red + 16 * (size_t)G, elem_bytes == 4 ? kStreamIters / 2 : kStreamIters);
-  if (!pl.resident) pl.smem = (size_t)pl.g.iters * kThreads * 8 * elem_bytes + red + (size_t)pl.g.cols * 8 * 4;     // moments_kernel
-  return pl;
+  return plan(N, P, C, G, 8 * (size_t)elem_bytes, 3 * kThreads * 8 * 4 + 8 * (size_t)C + 16 * (size_t)G, 3);
 }
 inline Plan plan_backward(int elem_bytes, int N, int P, int C, int G, bool ckpt) {
   const size_t vec = 8 * (size_t)elem_bytes + (ckpt ? 8 : 8 * (size_t)elem_bytes) + 2;      // dy, x, a byte each for gate and scale
-  return plan(N, P, C, G, vec, 2 * kThreads * 8 * 4 + 8 * (size_t)C + 16 * (size_t)G, elem_bytes == 4 ? kStreamIters / 2 : kStreamIters);
+  return plan(N, P, C, G, vec, 2 * kThreads * 8 * 4 + 8 * (size_t)C + 16 * (size_t)G, 2);
 }
 // Whether every launch's grid can be given.
 inline bool grid_ok(const Plan& pl) {
@@ -972,6 +1100,8 @@ inline bool grid_ok(const Plan& pl) {
                          (int64_t)g.N * ((2 * (int64_t)g.C + 31) / 32) <= INT32_MAX);
 }
 inline size_t partial_floats(const Plan& pl) { return pl.resident ? 0 : (size_t)pl.g.N * pl.g.parts * 2 * pl.g.C; }
+// Whether a second streamed pass adds up an image's rows of sums itself.
+inline bool merges(const Geom& g) { return g.tiles == 1 && g.parts <= kMergeParts; }
 
 // ---- host side: launches ---------------------------------------------------------------------------------------
 template <typename Kernel, typename Params>
@@ -987,20 +1117,25 @@ inline cudaError_t launch_cluster(Kernel kernel, int blocks, int cluster, size_t
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-template <typename T, bool VEC> inline cudaError_t launch_forward_as(cudaStream_t st, const Plan& pl, const Forward<T>& p) {
+template <typename T, bool VEC, int ACT, bool EXTRA> inline cudaError_t launch_forward_as(cudaStream_t st, const Plan& pl, Forward<T> p) {
   const Geom& g = pl.g;
+  if (pl.resident) {
+    static OncePerDevice once;
+    const cudaError_t e = once_per_device(&once, []() { return set_smem_limit(forward_kernel<T, VEC, ACT, EXTRA>, kSmemMost); });
+    return e != cudaSuccess ? e : launch_cluster(forward_kernel<T, VEC, ACT, EXTRA>, g.N * g.parts, g.parts, pl.smem, st, p);
+  }
   static OncePerDevice once;
-  cudaError_t e = once_per_device(&once, []() {
-    const cudaError_t f = set_smem_limit(forward_kernel<T, VEC>, kSmemMost);
-    return f != cudaSuccess ? f : set_smem_limit(moments_kernel<T, VEC>, kSmemMost);
-  });
+  cudaError_t e = once_per_device(&once, []() { return set_smem_limit(moments_kernel<T, VEC>, 64 * 1024); });
   if (e != cudaSuccess) return e;
-  if (pl.resident) return launch_cluster(forward_kernel<T, VEC>, g.N * g.parts, g.parts, pl.smem, st, p);
   const dim3 grid((unsigned)(g.N * g.parts), (unsigned)g.tiles);
-  e = launch_chained(moments_kernel<T, VEC>, grid, dim3(kThreads), pl.smem, st, p);
-  const int warps = pow2_up_to((int64_t)g.parts * g.Cg / 64, 32);
-  if (e == cudaSuccess) e = launch_chained(combine_kernel<T>, dim3((unsigned)(g.N * g.G)), dim3(32 * warps), 0, st, p);
-  if (e == cudaSuccess) e = launch_chained(apply_kernel<T, VEC>, grid, dim3(kThreads), 0, st, p);
+  e = launch_chained(moments_kernel<T, VEC>, grid, dim3(kThreads), 3 * kThreads * 8 * 4 + 64 * (size_t)g.cols, st, p);
+  p.combined = !merges(g);
+  if (e == cudaSuccess && p.combined) {
+    const int64_t entries = (int64_t)g.parts * (g.tiles == 1 ? 1 : g.Cg);
+    e = launch_chained(combine_kernel<T>, dim3((unsigned)(g.N * g.G)), dim3(32 * pow2_up_to(entries / 64, 32)), 0, st, p);
+  }
+  if (e == cudaSuccess)
+    e = launch_chained(apply_kernel<T, VEC, ACT, EXTRA>, grid, dim3(kThreads), p.combined ? 0 : 8 * (size_t)g.G, st, p);
   return e;
 }
 
@@ -1012,38 +1147,55 @@ inline cudaError_t launch_forward(cudaStream_t st, const Plan& pl, Forward<T> p)
   int8_t* codes = p.codes;
   if (p.ckpt_lanes == 0) p.codes = nullptr;       // blocks that do not fall on groups of lanes: a pass of their own
   const bool vec = C % 8 == 0 && aligned_to(p.x, 16) && aligned_to(p.y, 16) && aligned_to(p.res, 16) && aligned_to(p.codes, 8);
-  cudaError_t e = vec ? launch_forward_as<T, true>(st, pl, p) : launch_forward_as<T, false>(st, pl, p);
+  const bool extra = p.res || p.gate || p.codes;
+  cudaError_t e;
+  if (!vec) e = launch_forward_as<T, false, -1, true>(st, pl, p);
+  else if (p.act == ACT_RELU) e = extra ? launch_forward_as<T, true, ACT_RELU, true>(st, pl, p) : launch_forward_as<T, true, ACT_RELU, false>(st, pl, p);
+  else if (p.act == ACT_SILU) e = extra ? launch_forward_as<T, true, ACT_SILU, true>(st, pl, p) : launch_forward_as<T, true, ACT_SILU, false>(st, pl, p);
+  else e = extra ? launch_forward_as<T, true, ACT_NONE, true>(st, pl, p) : launch_forward_as<T, true, ACT_NONE, false>(st, pl, p);
   if (e == cudaSuccess && codes && !p.codes) e = launch_ckpt_encode<T>(st, p.x, (size_t)p.g.N * p.g.P, C, codes, p.scales);
   return e;
 }
 
-template <typename T, bool VEC, bool CK> inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, const Backward<T>& p) {
+template <typename T, bool VEC, bool CK, int SLOPE>
+inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<T> p, float* dgamma, float* dbeta) {
   const Geom& g = pl.g;
-  static OncePerDevice once;
-  cudaError_t e = once_per_device(&once, []() { return set_smem_limit(backward_kernel<T, VEC, CK>, kSmemMost); });
-  if (e != cudaSuccess) return e;
-  if (pl.resident) return launch_cluster(backward_kernel<T, VEC, CK>, g.N * g.parts, g.parts, pl.smem, st, p);
-  const dim3 grid((unsigned)(g.N * g.parts), (unsigned)g.tiles);
-  e = launch_chained(backward_sums_kernel<T, VEC, CK>, grid, dim3(kThreads), 0, st, p);
+  const int width = 2 * g.C, blocks = (width + 31) / 32;
+  cudaError_t e;
+  if (pl.resident) {
+    static OncePerDevice once;
+    e = once_per_device(&once, []() { return set_smem_limit(backward_kernel<T, VEC, CK, SLOPE>, kSmemMost); });
+    if (e == cudaSuccess) e = launch_cluster(backward_kernel<T, VEC, CK, SLOPE>, g.N * g.parts, g.parts, pl.smem, st, p);
+  } else {
+    const dim3 grid((unsigned)(g.N * g.parts), (unsigned)g.tiles);
+    e = launch_chained(backward_sums_kernel<T, VEC, CK, SLOPE>, grid, dim3(kThreads), 0, st, p);
+    if (merges(g)) p.totals = nullptr;
+    else if (e == cudaSuccess)
+      e = launch_chained(add_rows_kernel, dim3((unsigned)(g.N * blocks)), dim3(1024), 0, st, (const float*)p.partial, g.parts, width, p.totals,
+                         (float*)nullptr, 0);
+    if (e == cudaSuccess) e = launch_chained(backward_apply_kernel<T, VEC, CK, SLOPE>, grid, dim3(kThreads), 0, st, p);
+  }
   if (e == cudaSuccess)
-    e = launch_chained(add_rows_kernel, dim3((unsigned)(g.N * ((2 * g.C + 31) / 32))), dim3(1024), 0, st, (const float*)p.partial,
-                       g.parts, 2 * g.C, p.totals, (float*)nullptr, 0);
-  if (e == cudaSuccess) e = launch_chained(backward_apply_kernel<T, VEC, CK>, grid, dim3(kThreads), 0, st, p);
+    e = launch_chained(add_rows_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, (const float*)(p.totals ? p.totals : p.partial),
+                       p.totals ? g.N : g.N * g.parts, width, dgamma, dbeta, g.C);
   return e;
 }
-
+template <typename T, bool CK>
+inline cudaError_t launch_backward_of(cudaStream_t st, const Plan& pl, const Backward<T>& p, bool vec, float* dgamma, float* dbeta) {
+  if (!vec) return launch_backward_as<T, false, CK, -1>(st, pl, p, dgamma, dbeta);
+  switch (p.slope) {
+    case SLOPE_MASK: return launch_backward_as<T, true, CK, SLOPE_MASK>(st, pl, p, dgamma, dbeta);
+    case SLOPE_BITS: return launch_backward_as<T, true, CK, SLOPE_BITS>(st, pl, p, dgamma, dbeta);
+    case SLOPE_SILU: return launch_backward_as<T, true, CK, SLOPE_SILU>(st, pl, p, dgamma, dbeta);
+    default: return launch_backward_as<T, true, CK, SLOPE_ONE>(st, pl, p, dgamma, dbeta);
+  }
+}
 template <typename T>
 inline cudaError_t launch_backward(cudaStream_t st, const Plan& pl, Backward<T> p, float* dgamma, float* dbeta) {
   p.g = pl.g;
-  const Geom& g = p.g;
-  const bool vec = g.C % 8 == 0 && aligned_to(p.dy, 16) && aligned_to(p.x, 16) && aligned_to(p.codes, 8) && aligned_to(p.mask, 16) &&
+  const bool vec = p.g.C % 8 == 0 && aligned_to(p.dy, 16) && aligned_to(p.x, 16) && aligned_to(p.codes, 8) && aligned_to(p.mask, 16) &&
                    aligned_to(p.res, 16) && aligned_to(p.dx, 16);
-  cudaError_t e = p.codes ? (vec ? launch_backward_as<T, true, true>(st, pl, p) : launch_backward_as<T, false, true>(st, pl, p))
-                          : (vec ? launch_backward_as<T, true, false>(st, pl, p) : launch_backward_as<T, false, false>(st, pl, p));
-  if (e == cudaSuccess)
-    e = launch_chained(add_rows_kernel, dim3((unsigned)((2 * g.C + 31) / 32)), dim3(1024), 0, st, (const float*)p.totals, g.N, 2 * g.C,
-                       dgamma, dbeta, g.C);
-  return e;
+  return p.codes ? launch_backward_of<T, true>(st, pl, p, vec, dgamma, dbeta) : launch_backward_of<T, false>(st, pl, p, vec, dgamma, dbeta);
 }
 
 }  // namespace gn

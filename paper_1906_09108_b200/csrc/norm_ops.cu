@@ -47,7 +47,8 @@ static cudaError_t gn_backward_as(const fdg_gn_shape* s, const void* dy, const v
                                   const void* res, void* dx, float* dgamma, float* dbeta, void* scratch, cudaStream_t st) {
   gn::Backward<T> p{};
   p.dy = (const T*)dy; p.x = (const T*)x; p.codes = codes; p.scales = scales; p.stats = stats; p.gamma = gamma; p.beta = beta;
-  p.mask = (const T*)mask; p.gate = gate; p.res = (const T*)res; p.dx = (T*)dx; p.act = act;
+  p.mask = (const T*)mask; p.gate = gate; p.res = (const T*)res; p.dx = (T*)dx;
+  p.slope = act == FDG_ACT_SILU ? gn::SLOPE_SILU : mask ? gn::SLOPE_MASK : gate ? gn::SLOPE_BITS : gn::SLOPE_ONE;
   p.totals = static_cast<float*>(scratch);
   p.partial = reinterpret_cast<float*>(static_cast<char*>(scratch) + totals_bytes(s));
   return gn::launch_backward<T>(st, gn::plan_backward(sizeof(T), s->N, s->HW, s->C, s->groups, codes != nullptr), p, dgamma, dbeta);
