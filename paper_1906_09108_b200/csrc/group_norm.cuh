@@ -53,6 +53,7 @@ struct Geom {
   int iters;                // pixels per thread at most: ceil(pix / rp)
   int lanes_g, lanes_c;     // lanes that add up one group / one channel
   int tiles;                // tiles of columns (1 unless streamed with more than 2048 channels)
+  float inv_m;              // 1 / (P * Cg)
 };
 constexpr int kMergeParts = 16;             // rows of sums that the second streamed pass adds up itself
 
@@ -81,6 +82,7 @@ __device__ __forceinline__ void copy8_async(void* smem, const void* gmem) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem) : "memory");
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void prefetch_l2(const void* gmem) { asm volatile("prefetch.global.L2 [%0];" ::"l"(gmem)); }
 
 // Vectors a thread keeps in shared memory: its own [iters] of them, 16 bytes of consecutive threads side by side.
 template <typename T> struct Slots {
@@ -106,6 +108,32 @@ template <typename T> struct Slots {
     for (int j = 0; j < Q; ++j) base[(k * Q + j) * kThreads] = r.q[j];
   }
 };
+
+// The streamed passes copy to shared memory ahead of what they use, every thread its own vectors, B of them to a commit group
+// (32 bytes) and kAhead groups under way: 96 to 128 bytes per thread are on
+// their way at any time, which costs no registers and needs no barrier.  turn(k) is called for k = 0, B, ... once vectors
+// k .. k + B - 1 have come; issue(k) starts the copy of vector k into slot k % ring_of<T>().
+constexpr int kAhead = 3;
+template <typename T> __host__ __device__ constexpr int batch_of() { return sizeof(T) == 2 ? 2 : 1; }
+template <typename T> __host__ __device__ constexpr int ring_of() { return batch_of<T>() * (kAhead + 1); }
+template <int B, typename Issue, typename Turn> __device__ __forceinline__ void stream(int n, Issue issue, Turn turn) {
+  constexpr int kBatch = B;
+#pragma unroll
+  for (int k = 0; k < kBatch * kAhead; k += kBatch) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (k + u < n) issue(k + u);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  for (int k = 0; k < n; k += kBatch) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (k + kBatch * kAhead + u < n) issue(k + kBatch * kAhead + u);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+    turn(k);
+  }
+}
 
 // This thread's place in a CTA's tile.
 struct Place {
@@ -353,81 +381,76 @@ __device__ __forceinline__ uint32_t positive_bits(const Raw8<float>& y) {
   return b;
 }
 
-// y (and the gate's bits, and x in 8 bits) of this CTA's pixels: fetch(k) gives the thread's k-th vector of x; U of them (and of
-// res) are fetched before the first is used.  REVERSE: from the last pixel to the first.  ACT < 0: p.act; EXTRA: res, gate and
-// codes may be asked for.  Lanes that share a block of 32 channels have the same pixels, and take every turn together.
-// Offsets inside a CTA's pixels fit 32 bits.
-template <typename T, bool VEC, int ACT, bool EXTRA, int U, bool REVERSE, typename Fetch>
-__device__ __forceinline__ void emit(const Forward<T>& p, const Place& at, const Share& sh, const Affine<T>& affine, Fetch fetch) {
-  const Geom& g = p.g;
-  const int act = ACT < 0 ? p.act : ACT;
-  const size_t row = sh.row0 + at.r, off = row * g.C + at.c0;
-  T* const y = p.y + off;
-  const uint32_t step = (uint32_t)g.rp * g.C;
-  const bool has_res = EXTRA && p.res, has_gate = EXTRA && p.gate, has_codes = EXTRA && p.codes;
-  const T* res = nullptr;
-  int8_t* codes = nullptr;
-  uint8_t *gate = nullptr, *scales = nullptr;
-  uint32_t gate_step = 0, scale_step = 0, all = 0, tail = 0;
-  bool leads = false;
-  if constexpr (EXTRA) {
-    const int all_cols = (g.C + 7) >> 3, per_row = (g.C + kCkptBlock - 1) / kCkptBlock;
-    res = p.res + off;
-    codes = p.codes + off;
-    gate = p.gate + (row * all_cols + (at.c0 >> 3));
-    scales = p.scales + (row * per_row + at.c0 / kCkptBlock);
-    gate_step = (uint32_t)g.rp * all_cols;
-    scale_step = (uint32_t)g.rp * per_row;
-    leads = (at.col & (p.ckpt_lanes - 1)) == 0;
-    all = __ballot_sync(0xffffffffu, at.active);
-    tail = __ballot_sync(0xffffffffu, sh.mine > sh.whole);
+// y (and the gate's bits, and x in 8 bits) of a thread's pixels, one at a time.  ACT < 0: p.act; EXTRA: res, gate and codes may
+// be asked for.  Lanes that share a block of 32 channels have the same pixels, and take their turns together.  Offsets inside a
+// CTA's pixels fit 32 bits.
+template <typename T, bool VEC, int ACT, bool EXTRA> struct Emitter {
+  T* y;
+  const T* res;
+  int8_t* codes;
+  uint8_t *gate, *scales;
+  uint32_t step, gate_step, scale_step, all, tail;
+  int act, left, lanes, whole;
+  bool leads, has_gate, has_codes;
+  __device__ __forceinline__ Emitter(const Forward<T>& p, const Place& at, const Share& sh) {
+    const Geom& g = p.g;
+    const size_t row = sh.row0 + at.r, off = row * g.C + at.c0;
+    act = ACT < 0 ? p.act : ACT;
+    left = at.left; whole = sh.whole;
+    y = p.y + off;
+    step = (uint32_t)g.rp * g.C;
+    if constexpr (EXTRA) {
+      const int all_cols = (g.C + 7) >> 3, per_row = (g.C + kCkptBlock - 1) / kCkptBlock;
+      res = p.res ? p.res + off : nullptr;
+      has_gate = p.gate != nullptr; has_codes = p.codes != nullptr;
+      codes = p.codes + off;
+      gate = p.gate + (row * all_cols + (at.c0 >> 3));
+      scales = p.scales + (row * per_row + at.c0 / kCkptBlock);
+      gate_step = (uint32_t)g.rp * all_cols;
+      scale_step = (uint32_t)g.rp * per_row;
+      lanes = p.ckpt_lanes;
+      leads = (at.col & (lanes - 1)) == 0;
+      all = __ballot_sync(0xffffffffu, at.active);
+      tail = __ballot_sync(0xffffffffu, sh.mine > sh.whole);
+    } else {
+      res = nullptr;
+    }
   }
-  for (int k0 = 0; k0 < sh.mine; k0 += U) {
-    Raw8<T> xs[U], rs[EXTRA ? U : 1];
+  // `turn`: how many of its pixels the thread has had; k: which of them this one is.
+  __device__ __forceinline__ void one(int turn, uint32_t k, const Affine<T>& affine, const Raw8<T>& raw, const Raw8<T>& raw_res) const {
+    const F8 x = raw8_to_f8(raw);
+    F8 z;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (k0 + u < sh.mine) {
-        const int k = REVERSE ? sh.mine - 1 - (k0 + u) : k0 + u;
-        xs[u] = fetch(k);
-        if constexpr (EXTRA)
-          if (has_res) rs[u] = raw8_load<T, VEC>(res + (uint32_t)k * step, at.left);
+    for (int j = 0; j < 4; ++j) z.p[j] = affine.of(j, x.p[j]);
+    if constexpr (EXTRA)
+      if (res) {
+        const F8 r = raw8_to_f8(raw_res);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z.p[j] = add2(z.p[j], r.p[j]);
       }
+    if (act == ACT_RELU) {
+      const Raw8<T> out = f8_to_raw8<T, true>(z);
+      raw8_put<T, VEC>(y + k * step, left, out);
+      if constexpr (EXTRA)
+        if (has_gate) gate[k * gate_step] = (uint8_t)(positive_bits(out) & (VEC ? 0xFFu : (1u << left) - 1));
+    } else {
+      if (act == ACT_SILU) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (k0 + u < sh.mine) {
-        const uint32_t k = REVERSE ? sh.mine - 1 - (k0 + u) : k0 + u, o = k * step;
-        const F8 x = raw8_to_f8(xs[u]);
-        F8 z;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) z.p[j] = affine.of(j, x.p[j]);
-        if constexpr (EXTRA)
-          if (has_res) {
-            const F8 r = raw8_to_f8(rs[u]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) z.p[j] = add2(z.p[j], r.p[j]);
-          }
-        if (act == ACT_RELU) {
-          const Raw8<T> out = f8_to_raw8<T, true>(z);
-          raw8_put<T, VEC>(y + o, at.left, out);
-          if (has_gate) gate[k * gate_step] = (uint8_t)(positive_bits(out) & (VEC ? 0xFFu : (1u << at.left) - 1));
-        } else {
-          if (act == ACT_SILU) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float2 h = halves(z.p[j]);
-              z.p[j] = mul2(z.p[j], pair(sigmoid<T>(h.x), sigmoid<T>(h.y)));
-            }
-          }
-          raw8_put<T, VEC>(y + o, at.left, f8_to_raw8<T>(z));
-        }
-        if (has_codes) {
-          const CkptScale s = ckpt_scale(ckpt_top_of_lanes(ckpt_top(xs[u]), p.ckpt_lanes, k0 + u < sh.whole ? all : tail));
-          store_codes<VEC>(codes + o, 0, at.left, ckpt_codes(x, s));
-          if (leads) scales[k * scale_step] = (uint8_t)s.byte;
+        for (int j = 0; j < 4; ++j) {
+          const float2 h = halves(z.p[j]);
+          z.p[j] = mul2(z.p[j], pair(sigmoid<T>(h.x), sigmoid<T>(h.y)));
         }
       }
+      raw8_put<T, VEC>(y + k * step, left, f8_to_raw8<T>(z));
+    }
+    if constexpr (EXTRA)
+      if (has_codes) {
+        const CkptScale s = ckpt_scale(ckpt_top_of_lanes(ckpt_top(raw), lanes, turn < whole ? all : tail));
+        store_codes<VEC>(codes + k * step, 0, left, ckpt_codes(x, s));
+        if (leads) scales[k * scale_step] = (uint8_t)s.byte;
+      }
   }
-}
+};
 // The constants of a thread's channels from their groups' statistics.
 template <typename T, typename Stat>
 __device__ __forceinline__ void load_affine(const Forward<T>& p, const Place& at, const float (&gamma)[8], const float (&beta)[8], Stat stat, Affine<T>& affine) {
@@ -442,6 +465,7 @@ __device__ __forceinline__ void load_affine(const Forward<T>& p, const Place& at
 // The resident form: blockIdx.x = image * parts + share of its pixels, a cluster per image.
 template <typename T, bool VEC, int ACT, bool EXTRA>
 __global__ void __launch_bounds__(kThreads, 2) forward_kernel(const __grid_constant__ Forward<T> p) {
+  constexpr int kBatch = 2;
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
   float* red = reinterpret_cast<float*>(smem + (size_t)g.iters * Slots<T>::Q * kThreads);      // [4096]
@@ -458,6 +482,10 @@ __global__ void __launch_bounds__(kThreads, 2) forward_kernel(const __grid_const
   const uint32_t step = (uint32_t)g.rp * g.C;
 #pragma unroll 4
   for (int k = 0; k < sh.mine; ++k) slots.template fetch<VEC>(k, src + (uint32_t)k * step, at.left);
+  const Emitter<T, VEC, ACT, EXTRA> out(p, at, sh);
+  if constexpr (EXTRA)
+    if (out.res)
+      for (int k = 0; k < sh.mine; ++k) prefetch_l2(out.res + (uint32_t)k * step);
   float gamma[8], beta[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) { gamma[i] = p.gamma[at.channel(i)]; beta[i] = p.beta[at.channel(i)]; }
@@ -481,16 +509,29 @@ __global__ void __launch_bounds__(kThreads, 2) forward_kernel(const __grid_const
   __syncthreads();
   Affine<T> affine;
   load_affine(p, at, gamma, beta, [&](int s) { return mom[s]; }, affine);
-  emit<T, VEC, ACT, EXTRA, 2, false>(p, at, sh, affine, [&](int k) { return slots.get(k); });
+  for (int k = 0; k < sh.mine; k += kBatch) {
+    Raw8<T> xs[kBatch], rs[EXTRA ? kBatch : 1];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (k + u < sh.mine) {
+        xs[u] = slots.get(k + u);
+        if constexpr (EXTRA)
+          if (out.res) rs[u] = raw8_load<T, VEC>(out.res + (uint32_t)(k + u) * step, at.left);
+      }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (k + u < sh.mine) out.one(k + u, k + u, affine, xs[u], rs[EXTRA ? u : 0]);
+  }
   cluster.barrier_wait(std::move(token));                                 // nor do they read its own
 }
 
 // Streamed, first pass: moments of each group (with tiles > 1: of each channel) over a CTA's pixels.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads, 3) moments_kernel(const __grid_constant__ Forward<T> p) {
+  constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
-  float* red = reinterpret_cast<float*>(smem);                                 // [4096]
+  float* red = reinterpret_cast<float*>(smem + kRing * Slots<T>::Q * kThreads);   // [4096]
   float* common = red + 2 * kThreads * 8;                                      // [2048]
   float2* chan = reinterpret_cast<float2*>(common + kThreads * 8);             // [8 * cols]
   const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
@@ -501,18 +542,14 @@ __global__ void __launch_bounds__(kThreads, 3) moments_kernel(const __grid_const
   grid_dependency_release();
   const T* src = p.x + (sh.row0 + at.r) * g.C + at.c0;
   const uint32_t step = (uint32_t)g.rp * g.C;
-  constexpr int U = sizeof(T) == 4 ? 4 : 8;                // vectors in flight
+  const Slots<T> ring(smem);
   Moments m;
-  for (int k0 = 0; k0 < sh.mine; k0 += U) {
-    Raw8<T> xs[U];
+  stream<kBatch>(sh.mine, [&](int k) { ring.template fetch<VEC>(k % kRing, src + (uint32_t)k * step, at.left); }, [&](int k) {
+    if (k == 0) m.start(raw8_to_f8(ring.get(0)));
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (k0 + u < sh.mine) xs[u] = raw8_load<T, VEC>(src + (uint32_t)(k0 + u) * step, at.left);
-    if (k0 == 0) m.start(raw8_to_f8(xs[0]));
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (k0 + u < sh.mine) m.add(raw8_to_f8(xs[u]));
-  }
+    for (int u = 0; u < kBatch; ++u)
+      if (k + u < sh.mine) m.add(raw8_to_f8(ring.get((k + u) % kRing)));
+  });
   const int c_first = blockIdx.y * kMaxCols * 8, sets = min(g.cols * 8, g.C - c_first);
   cta_moments(g, at, m, sh.mine, sh.count, sets, red, common, chan);
   if (g.tiles == 1) {
@@ -577,9 +614,11 @@ __global__ void __launch_bounds__(1024) combine_kernel(const __grid_constant__ F
 // bits everywhere; its first CTA writes them out) unless combine_kernel has.
 template <typename T, bool VEC, int ACT, bool EXTRA>
 __global__ void __launch_bounds__(kThreads, 2) apply_kernel(const __grid_constant__ Forward<T> p) {
+  constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
-  float2* mom = reinterpret_cast<float2*>(smem);           // [G], unless combined
   const Geom& g = p.g;
+  const Slots<T> ring(smem), res_ring(smem + kRing * Slots<T>::Q * kThreads);
+  float2* mom = reinterpret_cast<float2*>(smem + (EXTRA && p.res ? 2 : 1) * kRing * Slots<T>::Q * kThreads);    // [G], unless combined
   const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
   Place at(g, blockIdx.y);
   at.active = at.active && at.left > 0;
@@ -587,6 +626,7 @@ __global__ void __launch_bounds__(kThreads, 2) apply_kernel(const __grid_constan
   const Share sh(g, at, n, part);
   float gamma[8], beta[8];
   grid_dependency_wait();
+  grid_dependency_release();
 #pragma unroll
   for (int i = 0; i < 8; ++i) { gamma[i] = p.gamma[at.channel(i)]; beta[i] = p.beta[at.channel(i)]; }
   if (!p.combined) {
@@ -606,8 +646,23 @@ __global__ void __launch_bounds__(kThreads, 2) apply_kernel(const __grid_constan
   else
     load_affine(p, at, gamma, beta, [&](int s) { return mom[s]; }, affine);
   const T* x = p.x + (sh.row0 + at.r) * g.C + at.c0;
-  const uint32_t step = (uint32_t)g.rp * g.C;
-  emit<T, VEC, ACT, EXTRA, sizeof(T) == 2 ? 4 : 2, true>(p, at, sh, affine, [&](int k) { return raw8_load<T, VEC>(x + (uint32_t)k * step, at.left); });
+  const Emitter<T, VEC, ACT, EXTRA> out(p, at, sh);
+  const int last = sh.mine - 1;
+  stream<kBatch>(sh.mine, [&](int k) {
+    const uint32_t o = (uint32_t)(last - k) * out.step;
+    ring.template fetch<VEC>(k % kRing, x + o, at.left);
+    if constexpr (EXTRA)
+      if (out.res) res_ring.template fetch<VEC>(k % kRing, out.res + o, at.left);
+  }, [&](int k) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (k + u < sh.mine) {
+        Raw8<T> r;
+        if constexpr (EXTRA)
+          if (out.res) r = res_ring.get((k + u) % kRing);
+        out.one(k + u, last - (k + u), affine, ring.get((k + u) % kRing), r);
+      }
+  });
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------
@@ -653,19 +708,6 @@ template <typename T> struct Columns {
     scales = p.scales + (row * per_row + at.c0 / kCkptBlock);
     gate = p.gate + (row * all_cols + (at.c0 >> 3));
     step = (uint32_t)g.rp * g.C; gate_step = (uint32_t)g.rp * all_cols; scale_step = (uint32_t)g.rp * per_row;
-  }
-  template <bool VEC, bool CK> __device__ __forceinline__ Held<T, CK> load(uint32_t k, int left, int slope) const {
-    Held<T, CK> h;
-    h.dy = raw8_load<T, VEC>(dy + k * step, left);
-    if constexpr (CK) {
-      h.codes = load_codes<VEC>(codes + k * step, 0, left);
-      h.scale = scales[k * scale_step];
-    } else {
-      h.x = raw8_load<T, VEC>(x + k * step, left);
-    }
-    if (slope == SLOPE_MASK) h.mask = raw8_load<T, VEC>(mask + k * step, left);
-    if (slope == SLOPE_BITS) h.open = gate[k * gate_step];
-    return h;
   }
 };
 
@@ -726,43 +768,85 @@ __device__ __forceinline__ void operands(const Raw8<T>& dy, const Held<T, CK>& h
   }
 }
 
-// dx of this CTA's pixels: fetch(k) gives the thread's k-th operands; k1 = -rstd*S1/m, k2 = -rstd^2*S2/m.  GATED: dy comes
-// gated.
-template <typename T, bool VEC, bool CK, int U, bool REVERSE, bool GATED, typename Fetch>
-__device__ __forceinline__ void emit_dx(const Backward<T>& p, const Place& at, const Share& sh, int slope, const Channels& ch,
-                                        const f32x2 (&k1)[4], const f32x2 (&k2)[4], Fetch fetch) {
-  const size_t off = (sh.row0 + at.r) * p.g.C + at.c0;
-  T* const dx = p.dx + off;
-  const T* const res = p.res + off;
-  const bool has_res = p.res != nullptr;
-  const uint32_t step = (uint32_t)p.g.rp * p.g.C;
-  for (int k0 = 0; k0 < sh.mine; k0 += U) {
-    Held<T, CK> hs[U];
-    Raw8<T> rs[U];
+// dx of one vector: k1 = -rstd*S1/m, k2 = -rstd^2*S2/m.
+template <typename T, bool CK>
+__device__ __forceinline__ Raw8<T> dx_of(const Raw8<T>& dy, const Held<T, CK>& h, int slope, const Channels& ch, const f32x2 (&k1)[4],
+                                         const f32x2 (&k2)[4], const Raw8<T>* res) {
+  F8 dz, d;
+  operands<T, CK>(dy, h, slope, ch, dz, d);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (k0 + u < sh.mine) {
-        const uint32_t k = REVERSE ? sh.mine - 1 - (k0 + u) : k0 + u;
-        hs[u] = fetch(k);
-        if (has_res) rs[u] = raw8_load<T, VEC>(res + k * step, at.left);
-      }
+  for (int j = 0; j < 4; ++j) dz.p[j] = fma2(ch.scale[j], dz.p[j], fma2(d.p[j], k2[j], k1[j]));
+  if (res) {
+    const F8 r = raw8_to_f8(*res);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (k0 + u < sh.mine) {
-        const uint32_t k = REVERSE ? sh.mine - 1 - (k0 + u) : k0 + u;
-        F8 dz, d;
-        operands<T, CK>(GATED ? hs[u].dy : passed<T, CK>(hs[u], slope), hs[u], slope, ch, dz, d);
+    for (int j = 0; j < 4; ++j) dz.p[j] = add2(dz.p[j], r.p[j]);
+  }
+  return f8_to_raw8<T>(dz);
+}
+
+// The operands of the streamed passes: rings of dy, x (or its codes), the mask and res, as far as a pass has them; the bytes
+// (scales, gate bits) come through registers, two turns ahead.
+template <typename T, bool VEC, bool CK> struct Feed {
+  static constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
+  const Columns<T> from;
+  const Slots<T> dys, xs, masks, ress;
+  uint2* codes;
+  const T* res;
+  int left, slope, n;
+  bool reverse;
+  uint32_t scale[3][kBatch], open[3][kBatch];     // of this turn, the next, and the one after
+  static constexpr int kVec = kRing * Slots<T>::Q * kThreads;        // 16-byte words of a ring
+  // words of shared memory of a pass, in 16 bytes
+  static __host__ __device__ __forceinline__ int words(bool mask, bool res) {
+    return kVec + (CK ? kRing * kThreads / 2 : kVec) + (mask ? kVec : 0) + (res ? kVec : 0);
+  }
+  __device__ __forceinline__ Feed(const Backward<T>& p, const Place& at, const Share& sh, int slope_, const T* res_, bool reverse_, uint4* smem)
+      : from(p, at, sh), dys(smem), xs(smem + kVec), masks(smem + kVec + (CK ? kRing * kThreads / 2 : kVec)),
+        ress(smem + words(slope_ == SLOPE_MASK, false)), codes(reinterpret_cast<uint2*>(smem + kVec) + threadIdx.x),
+        res(res_ ? res_ + (sh.row0 + at.r) * p.g.C + at.c0 : nullptr), left(at.left), slope(slope_), n(sh.mine), reverse(reverse_) {
+    bytes(0, 1);
+    bytes(kBatch, 2);
+  }
+  __device__ __forceinline__ uint32_t at(int k) const { return (uint32_t)(reverse ? n - 1 - k : k); }
+  __device__ __forceinline__ void bytes(int k, int to) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) dz.p[j] = fma2(ch.scale[j], dz.p[j], fma2(d.p[j], k2[j], k1[j]));
-        if (has_res) {
-          const F8 r = raw8_to_f8(rs[u]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) dz.p[j] = add2(dz.p[j], r.p[j]);
-        }
-        raw8_put<T, VEC>(dx + k * step, at.left, f8_to_raw8<T>(dz));
+    for (int u = 0; u < kBatch; ++u)
+      if (k + u < n) {
+        if constexpr (CK) scale[to][u] = from.scales[at(k + u) * from.scale_step];
+        if (slope == SLOPE_BITS) open[to][u] = from.gate[at(k + u) * from.gate_step];
       }
   }
-}
+  __device__ __forceinline__ void issue(int k) const {
+    const uint32_t o = at(k) * from.step;
+    const int s = k % kRing;
+    dys.template fetch<VEC>(s, from.dy + o, left);
+    if constexpr (CK) {
+      if constexpr (VEC) copy8_async(codes + s * kThreads, from.codes + o); else codes[s * kThreads] = load_codes<false>(from.codes + o, 0, left);
+    } else {
+      xs.template fetch<VEC>(s, from.x + o, left);
+    }
+    if (slope == SLOPE_MASK) masks.template fetch<VEC>(s, from.mask + o, left);
+    if (res) ress.template fetch<VEC>(s, res + o, left);
+  }
+  // At the start of turn k: moves the bytes on.
+  __device__ __forceinline__ void turn(int k) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      scale[0][u] = scale[1][u]; scale[1][u] = scale[2][u];
+      open[0][u] = open[1][u]; open[1][u] = open[2][u];
+    }
+    bytes(k + 2 * kBatch, 2);
+  }
+  __device__ __forceinline__ Held<T, CK> get(int k, int u) const {
+    Held<T, CK> h;
+    const int s = (k + u) % kRing;
+    h.dy = dys.get(s);
+    if constexpr (CK) { h.codes = codes[s * kThreads]; h.scale = scale[0][u]; } else { h.x = xs.get(s); }
+    if (slope == SLOPE_MASK) h.mask = masks.get(s);
+    if (slope == SLOPE_BITS) h.open = open[0][u];
+    return h;
+  }
+};
 
 // The constants of a thread's channels from the saved statistics.
 template <typename T>
@@ -818,6 +902,7 @@ struct Sums {
 // one for the scale; then per-thread sums, per-channel sums A, B and per-group sums S1, S2 of this CTA, and k1, k2 of the image.
 template <typename T, bool VEC, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_constant__ Backward<T> p) {
+  constexpr int kBatch = 2;
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
   const int slope = SLOPE < 0 ? p.slope : SLOPE;
@@ -847,6 +932,9 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
       xslots.template fetch<VEC>(k, from.x + o, at.left);
     }
   }
+  const T* const res = p.res ? p.res + (sh.row0 + at.r) * g.C + at.c0 : nullptr;
+  if (res)
+    for (int k = 0; k < sh.mine; ++k) prefetch_l2(res + (uint32_t)k * from.step);
   // what comes in bytes goes through registers, several loads in flight
   if (CK || slope == SLOPE_MASK || slope == SLOPE_BITS) {
     constexpr int U = 4;
@@ -904,7 +992,6 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
              [&](int s, float s1, float s2) { own[s] = s1; own[g.G + s] = s2; });
   cg::cluster_group cluster = cg::this_cluster();
   cluster.sync();
-  const float inv_m = (float)(1.0 / ((double)g.P * g.Cg));
   for (int s = tid; s < g.G; s += kThreads) {
     float s1 = 0.f, s2 = 0.f;
     for (int j = 0; j < g.parts; ++j) {
@@ -912,8 +999,8 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
       s1 += other[s]; s2 += other[g.G + s];
     }
     const float r = p.stats[(size_t)(g.N + n) * g.G + s];
-    coef[s] = r * s1 * inv_m;
-    coef[g.G + s] = r * r * s2 * inv_m;
+    coef[s] = r * s1 * g.inv_m;
+    coef[g.G + s] = r * r * s2 * g.inv_m;
   }
   // each CTA of the cluster adds up a share of the channels for the parameter gradients
   const int share = (2 * g.C + g.parts - 1) / g.parts;
@@ -926,14 +1013,27 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
   __syncthreads();
   f32x2 k1[4], k2[4];
   load_coefficients(at, g.Cg, coef, coef + g.G, 0, k1, k2);
-  emit_dx<T, VEC, CK, 2, false, true>(p, at, sh, slope, ch, k1, k2, held);
+  T* const dx = p.dx + (sh.row0 + at.r) * g.C + at.c0;
+  for (int k = 0; k < sh.mine; k += kBatch) {
+    Raw8<T> rs[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (res && k + u < sh.mine) rs[u] = raw8_load<T, VEC>(res + (uint32_t)(k + u) * from.step, at.left);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (k + u < sh.mine) {
+        const Held<T, CK> h = held(k + u);
+        raw8_put<T, VEC>(dx + (uint32_t)(k + u) * from.step, at.left, dx_of<T, CK>(h.dy, h, slope, ch, k1, k2, res ? &rs[u] : nullptr));
+      }
+  }
   cluster.barrier_wait(std::move(token));
 }
 
 // Streamed, first pass: A and B of each channel over a CTA's pixels.
 template <typename T, bool VEC, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid_constant__ Backward<T> p) {
-  __shared__ __align__(16) float red[2 * kThreads * 8];
+  constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
+  extern __shared__ uint4 smem[];
   const Geom& g = p.g;
   const int slope = SLOPE < 0 ? p.slope : SLOPE;
   const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
@@ -941,27 +1041,26 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
   at.active = at.active && at.left > 0;
   if (at.left <= 0) { at.c0 = blockIdx.y * kMaxCols * 8; at.left = 1; }
   const Share sh(g, at, n, part);
-  const Columns<T> from(p, at, sh);
   grid_dependency_wait();
   grid_dependency_release();
+  Feed<T, VEC, CK> feed(p, at, sh, slope, nullptr, false, smem);
   Channels ch;
   float rstd[8];
   load_channels(p, at, n, slope, ch, rstd);
   Sums sums;
-  constexpr int U = sizeof(T) == 4 ? 2 : 4;               // vectors in flight
-  for (int k0 = 0; k0 < sh.mine; k0 += U) {
-    Held<T, CK> h[U];
+  stream<kBatch>(sh.mine, [&](int k) { feed.issue(k); }, [&](int k) {
+    feed.turn(k);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (k0 + u < sh.mine) h[u] = from.template load<VEC, CK>(k0 + u, at.left, slope);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (k0 + u < sh.mine) {
+    for (int u = 0; u < kBatch; ++u)
+      if (k + u < sh.mine) {
+        const Held<T, CK> h = feed.get(k, u);
         F8 dz, d;
-        operands<T, CK>(passed<T, CK>(h[u], slope), h[u], slope, ch, dz, d);
+        operands<T, CK>(passed<T, CK>(h, slope), h, slope, ch, dz, d);
         sums.add(dz, d);
       }
-  }
+  });
+  __syncthreads();                    // the sums go where the rings were
+  float* red = reinterpret_cast<float*>(smem);
   sums.put(red, g, at, rstd);
   __syncthreads();
   const int c_first = blockIdx.y * kMaxCols * 8, sets = min(g.cols * 8, g.C - c_first);
@@ -999,8 +1098,10 @@ __global__ void __launch_bounds__(1024) add_rows_kernel(const float* __restrict_
 // Streamed, second pass: dx.  Every CTA forms S1 and S2 of its tile's groups from the image's totals, or from its rows of sums.
 template <typename T, bool VEC, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __grid_constant__ Backward<T> p) {
-  __shared__ float coef[2][kMaxCols * 8];
+  constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
+  extern __shared__ uint4 smem[];
   const Geom& g = p.g;
+  float* coef = reinterpret_cast<float*>(smem + Feed<T, VEC, CK>::words((SLOPE < 0 ? p.slope : SLOPE) == SLOPE_MASK, p.res != nullptr));   // [2][sets]
   const int slope = SLOPE < 0 ? p.slope : SLOPE;
   const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
   const int c_first = blockIdx.y * kMaxCols * 8;
@@ -1008,12 +1109,11 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   at.active = at.active && at.left > 0;
   if (at.left <= 0) { at.c0 = c_first; at.left = 1; }
   const Share sh(g, at, n, part);
-  const Columns<T> from(p, at, sh);
   const int c_last = min(g.C, c_first + g.cols * 8) - 1;
   const int g_first = c_first / g.Cg, sets = c_last / g.Cg - g_first + 1, c_base = g_first * g.Cg;
-  const float inv_m = (float)(1.0 / ((double)g.P * g.Cg));
   grid_dependency_wait();
   grid_dependency_release();
+  Feed<T, VEC, CK> feed(p, at, sh, slope, p.res, true, smem);
   Channels ch;
   float rstd[8];
   load_channels(p, at, n, slope, ch, rstd);
@@ -1028,14 +1128,25 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
     const float w = p.gamma[c];
     return make_float2(w * b, w * a);
   }, [&](int s, float s1, float s2) {
-    coef[0][s] = rs[s] * s1 * inv_m;
-    coef[1][s] = rs[s] * rs[s] * s2 * inv_m;
+    coef[s] = rs[s] * s1 * g.inv_m;
+    coef[sets + s] = rs[s] * rs[s] * s2 * g.inv_m;
   });
   __syncthreads();
   f32x2 k1[4], k2[4];
-  load_coefficients(at, g.Cg, coef[0], coef[1], g_first, k1, k2);
-  emit_dx<T, VEC, CK, sizeof(T) == 2 ? 4 : 2, true, false>(p, at, sh, slope, ch, k1, k2,
-                                                          [&](uint32_t k) { return from.template load<VEC, CK>(k, at.left, slope); });
+  load_coefficients(at, g.Cg, coef, coef + sets, g_first, k1, k2);
+  T* const dx = p.dx + (sh.row0 + at.r) * g.C + at.c0;
+  stream<kBatch>(sh.mine, [&](int k) { feed.issue(k); }, [&](int k) {
+    feed.turn(k);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (k + u < sh.mine) {
+        const Held<T, CK> h = feed.get(k, u);
+        Raw8<T> r;
+        if (feed.res) r = feed.ress.get((k + u) % kRing);
+        raw8_put<T, VEC>(dx + feed.at(k + u) * feed.from.step, at.left,
+                         dx_of<T, CK>(passed<T, CK>(h, slope), h, slope, ch, k1, k2, feed.res ? &r : nullptr));
+      }
+  });
 }
 
 // ---- host side: plans ----------------------------------------------------------------------------------------
@@ -1058,6 +1169,7 @@ inline Plan plan(int N, int P, int C, int G, size_t vec_bytes, size_t fixed, int
   Plan pl{};
   Geom& g = pl.g;
   g.N = N; g.P = P; g.C = C; g.G = G; g.Cg = C / G;
+  g.inv_m = (float)(1.0 / ((double)P * g.Cg));
   const int all_cols = C / 8 + (C % 8 != 0);
   g.cols = std::min(all_cols, kMaxCols);
   g.tiles = (all_cols + kMaxCols - 1) / kMaxCols;
@@ -1125,17 +1237,21 @@ template <typename T, bool VEC, int ACT, bool EXTRA> inline cudaError_t launch_f
     return e != cudaSuccess ? e : launch_cluster(forward_kernel<T, VEC, ACT, EXTRA>, g.N * g.parts, g.parts, pl.smem, st, p);
   }
   static OncePerDevice once;
-  cudaError_t e = once_per_device(&once, []() { return set_smem_limit(moments_kernel<T, VEC>, 64 * 1024); });
+  cudaError_t e = once_per_device(&once, []() {
+    const cudaError_t f = set_smem_limit(moments_kernel<T, VEC>, kSmemMost);
+    return f != cudaSuccess ? f : set_smem_limit(apply_kernel<T, VEC, ACT, EXTRA>, kSmemMost);
+  });
   if (e != cudaSuccess) return e;
   const dim3 grid((unsigned)(g.N * g.parts), (unsigned)g.tiles);
-  e = launch_chained(moments_kernel<T, VEC>, grid, dim3(kThreads), 3 * kThreads * 8 * 4 + 64 * (size_t)g.cols, st, p);
+  const size_t ring = (size_t)ring_of<T>() * kThreads * 8 * sizeof(T);
+  e = launch_chained(moments_kernel<T, VEC>, grid, dim3(kThreads), ring + 3 * kThreads * 8 * 4 + 64 * (size_t)g.cols, st, p);
   p.combined = !merges(g);
   if (e == cudaSuccess && p.combined) {
     const int64_t entries = (int64_t)g.parts * (g.tiles == 1 ? 1 : g.Cg);
     e = launch_chained(combine_kernel<T>, dim3((unsigned)(g.N * g.G)), dim3(32 * pow2_up_to(entries / 64, 32)), 0, st, p);
   }
   if (e == cudaSuccess)
-    e = launch_chained(apply_kernel<T, VEC, ACT, EXTRA>, grid, dim3(kThreads), p.combined ? 0 : 8 * (size_t)g.G, st, p);
+    e = launch_chained(apply_kernel<T, VEC, ACT, EXTRA>, grid, dim3(kThreads), (p.res ? 2 : 1) * ring + (p.combined ? 0 : 8 * (size_t)g.G), st, p);
   return e;
 }
 
@@ -1167,13 +1283,20 @@ inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<
     e = once_per_device(&once, []() { return set_smem_limit(backward_kernel<T, VEC, CK, SLOPE>, kSmemMost); });
     if (e == cudaSuccess) e = launch_cluster(backward_kernel<T, VEC, CK, SLOPE>, g.N * g.parts, g.parts, pl.smem, st, p);
   } else {
+    static OncePerDevice once;
+    e = once_per_device(&once, []() {
+      const cudaError_t f = set_smem_limit(backward_sums_kernel<T, VEC, CK, SLOPE>, kSmemMost);
+      return f != cudaSuccess ? f : set_smem_limit(backward_apply_kernel<T, VEC, CK, SLOPE>, kSmemMost);
+    });
     const dim3 grid((unsigned)(g.N * g.parts), (unsigned)g.tiles);
-    e = launch_chained(backward_sums_kernel<T, VEC, CK, SLOPE>, grid, dim3(kThreads), 0, st, p);
+    auto rings = [&](bool res) { return 16 * (size_t)Feed<T, VEC, CK>::words(p.slope == SLOPE_MASK, res); };
+    if (e == cudaSuccess)
+      e = launch_chained(backward_sums_kernel<T, VEC, CK, SLOPE>, grid, dim3(kThreads), std::max(rings(false), (size_t)2 * kThreads * 8 * 4), st, p);
     if (merges(g)) p.totals = nullptr;
     else if (e == cudaSuccess)
       e = launch_chained(add_rows_kernel, dim3((unsigned)(g.N * blocks)), dim3(1024), 0, st, (const float*)p.partial, g.parts, width, p.totals,
                          (float*)nullptr, 0);
-    if (e == cudaSuccess) e = launch_chained(backward_apply_kernel<T, VEC, CK, SLOPE>, grid, dim3(kThreads), 0, st, p);
+    if (e == cudaSuccess) e = launch_chained(backward_apply_kernel<T, VEC, CK, SLOPE>, grid, dim3(kThreads), rings(p.res != nullptr) + 8 * (size_t)g.cols * 8, st, p);
   }
   if (e == cudaSuccess)
     e = launch_chained(add_rows_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, (const float*)(p.totals ? p.totals : p.partial),
