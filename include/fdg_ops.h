@@ -182,7 +182,7 @@ fdg_status fdg_ckpt_decode(int precision, const int8_t* codes, const uint8_t* sc
 /* ---- group normalisation with an activation -------------------------------------------------------------------------
  * The normalisation that does not depend on which images share a batch.  x [N][HW][C]; group g of an image is channels
  * [g*C/groups, (g+1)*C/groups) at all of its pixels (groups = 1: layer norm over an image, groups = C: instance norm).
- * `groups` divides C; any C, any alignment that the storage type has (multiples of 8 channels on 16-byte aligned tensors are
+ * `groups` divides C; any C up to 65536, any alignment that the storage type has (multiples of 8 channels on 16-byte aligned tensors are
  * fastest).  gamma, beta, dgamma, dbeta [C], stats [2][N][groups] (mean, then 1/sqrt(var + eps), biased variance) are fp32.
  * `scratch`: fdg_gn_scratch_bytes bytes of device memory, 256-byte aligned, any contents; it serves both calls, and is not
  * to be shared by calls that may run at the same time.  The result of a call does not depend on scheduling.  No output

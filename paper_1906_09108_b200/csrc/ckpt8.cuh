@@ -30,16 +30,27 @@ struct CkptScale {
 };
 __device__ __forceinline__ CkptScale ckpt_scale(uint32_t top) {
   CkptScale s;
+  const uint32_t t = max(top + 0x10000u, 7u << 23);                 // its exponent is e + 127 + 6, 7 at least
+  s.byte = (t >> 23) - 6u;
+  s.inv_step = __uint_as_float((260u << 23) - (t & 0x7F800000u));    // exponent 254 - (e + 127)
   s.clamp = top >= 0x7F7F0000u;
-  const uint32_t e = min((top + 0x10000u) >> 23, 254u);
-  const uint32_t k = max(e, 7u) - 6u;
-  s.byte = top >= 0x7F800000u ? 255u : k;
-  s.inv_step = top >= 0x7F800000u ? 0.f : __uint_as_float((254u - k) << 23);
+  if (s.clamp) {
+    s.byte = top >= 0x7F800000u ? 255u : 248u;
+    s.inv_step = top >= 0x7F800000u ? 0.f : __uint_as_float(6u << 23);
+  }
   return s;
 }
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
 // The largest magnitude of 8 values, in the storage type's own bits where it has 16 (two at a time), as fp32 bits.
+__device__ __forceinline__ uint32_t ckpt_top2(const Raw8<__nv_bfloat16>& r) {
+  return max_u16x2(max_u16x2(r.q[0].x & 0x7FFF7FFFu, r.q[0].y & 0x7FFF7FFFu), max_u16x2(r.q[0].z & 0x7FFF7FFFu, r.q[0].w & 0x7FFF7FFFu));
+}
 __device__ __forceinline__ uint32_t ckpt_top(const Raw8<__nv_bfloat16>& r) {
-  const uint32_t m = __vmaxu2(__vmaxu2(r.q[0].x & 0x7FFF7FFFu, r.q[0].y & 0x7FFF7FFFu), __vmaxu2(r.q[0].z & 0x7FFF7FFFu, r.q[0].w & 0x7FFF7FFFu));
+  const uint32_t m = ckpt_top2(r);
   return max(m & 0xFFFF0000u, m << 16);
 }
 __device__ __forceinline__ uint32_t ckpt_top(const Raw8<float>& r) {

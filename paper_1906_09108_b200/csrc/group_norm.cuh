@@ -51,7 +51,9 @@ struct Geom {
   int cols, rp;             // columns of a CTA's tile, pixels side by side
   int parts, pix;           // CTAs per image, pixels per CTA
   int iters;                // pixels per thread at most: ceil(pix / rp)
+  int whole, whole_last;    // pixels that each of a thread's rows has at least: in a full share, in the last one with pixels
   int lanes_g, lanes_c;     // lanes that add up one group / one channel
+  uint32_t col_mul, cg_mul; // tid / cols = tid * col_mul >> 16;  c / Cg = the high word of c * cg_mul (0: Cg = 1)
   int tiles;                // tiles of columns (1 unless streamed with more than 2048 channels)
   float inv_m;              // 1 / (P * Cg)
 };
@@ -110,30 +112,38 @@ template <typename T> struct Slots {
 };
 
 // The streamed passes copy to shared memory ahead of what they use, every thread its own vectors, B of them to a commit group
-// (32 bytes) and kAhead groups under way: 96 to 128 bytes per thread are on
-// their way at any time, which costs no registers and needs no barrier.  turn(k) is called for k = 0, B, ... once vectors
-// k .. k + B - 1 have come; issue(k) starts the copy of vector k into slot k % ring_of<T>().
+// (32 bytes) and kAhead groups under way: 96 to 128 bytes per thread are on their way at any time, which costs no registers and
+// needs no barrier.  start(mine, issue) begins; run() calls turn(k, slot) for k = 0, B, ... < n once vectors k .. k + B - 1 have
+// come to slots slot .. slot + B - 1; issue(slot) starts the copy of the thread's next vector (of `mine`) into a slot.  The loop is
+// unrolled over the ring, so that slots are constants.
 constexpr int kAhead = 3;
 template <typename T> __host__ __device__ constexpr int batch_of() { return sizeof(T) == 2 ? 2 : 1; }
 template <typename T> __host__ __device__ constexpr int ring_of() { return batch_of<T>() * (kAhead + 1); }
-template <int B, typename Issue, typename Turn> __device__ __forceinline__ void stream(int n, Issue issue, Turn turn) {
-  constexpr int kBatch = B;
+template <int B> struct Stream {
+  static constexpr int R = B * (kAhead + 1);
+  template <typename Issue> static __device__ __forceinline__ void start(int mine, Issue issue) {
 #pragma unroll
-  for (int k = 0; k < kBatch * kAhead; k += kBatch) {
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (k + u < n) issue(k + u);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    for (int k = 0; k < B * kAhead; ++k) {
+      if (k < mine) issue(k);
+      if (k % B == B - 1) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
   }
-  for (int k = 0; k < n; k += kBatch) {
+  template <typename Issue, typename Turn> static __device__ __forceinline__ void run(int n, int mine, Issue issue, Turn turn) {
+    for (int k0 = 0; k0 < n; k0 += R) {
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (k + kBatch * kAhead + u < n) issue(k + kBatch * kAhead + u);
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
-    turn(k);
+      for (int b = 0; b < R; b += B) {
+        if (k0 + b < n) {
+#pragma unroll
+          for (int u = 0; u < B; ++u)
+            if (k0 + b + B * kAhead + u < mine) issue((b + B * kAhead + u) % R);
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+          turn(k0 + b, b);
+        }
+      }
+    }
   }
-}
+};
 
 // This thread's place in a CTA's tile.
 struct Place {
@@ -141,7 +151,7 @@ struct Place {
   bool active;
   int c0, left;               // first channel, channels of the column that exist
   __device__ __forceinline__ Place(const Geom& g, int tile) {
-    col = threadIdx.x % g.cols; r = threadIdx.x / g.cols;
+    r = (int)(threadIdx.x * g.col_mul >> 16); col = (int)threadIdx.x - r * g.cols;
     active = r < g.rp;
     c0 = (tile * kMaxCols + col) * 8;
     left = min(8, g.C - c0);
@@ -150,8 +160,9 @@ struct Place {
 };
 
 // take(i, channel, group) for the 8 channels of a column; those past the last channel stand in for the first.
-template <typename Take> __device__ __forceinline__ void each_channel(const Place& at, int Cg, Take take) {
-  const int first = at.c0 / Cg;
+__device__ __forceinline__ int group_of(const Geom& g, int c) { return g.cg_mul ? (int)__umulhi((uint32_t)c, g.cg_mul) : c; }
+template <typename Take> __device__ __forceinline__ void each_channel(const Geom& g, const Place& at, Take take) {
+  const int Cg = g.Cg, first = group_of(g, at.c0);
   int s = first, rem = at.c0 - first * Cg;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -164,11 +175,13 @@ template <typename Take> __device__ __forceinline__ void each_channel(const Plac
 struct Share {
   size_t row0;
   int count, whole, mine;
+  int turns;                  // of the CTA's threads, the most that one has
   __device__ __forceinline__ Share(const Geom& g, const Place& at, int n, int part) {
     const int p0 = part * g.pix;
     row0 = (size_t)n * g.P + p0;
     count = max(0, min(g.pix, g.P - p0));
-    whole = count / g.rp;
+    whole = count == g.pix ? g.whole : count > 0 ? g.whole_last : 0;
+    turns = whole + (count > whole * g.rp ? 1 : 0);
     mine = at.active ? whole + (at.r < count - whole * g.rp ? 1 : 0) : 0;
   }
 };
@@ -381,48 +394,45 @@ __device__ __forceinline__ uint32_t positive_bits(const Raw8<float>& y) {
   return b;
 }
 
-// y (and the gate's bits, and x in 8 bits) of a thread's pixels, one at a time.  ACT < 0: p.act; EXTRA: res, gate and codes may
-// be asked for.  Lanes that share a block of 32 channels have the same pixels, and take their turns together.  Offsets inside a
-// CTA's pixels fit 32 bits.
-template <typename T, bool VEC, int ACT, bool EXTRA> struct Emitter {
+// y (and the gate's bits, and x in 8 bits) of a thread's pixels.  ACT < 0: p.act.  EXTRA 1: res and gate may be asked for; 2: and
+// codes.  Offsets inside a CTA's pixels fit 32 bits.
+enum { PLAIN = 0, WITH_RES_GATE = 1, WITH_CODES = 2 };
+template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
   T* y;
   const T* res;
   int8_t* codes;
   uint8_t *gate, *scales;
-  uint32_t step, gate_step, scale_step, all, tail;
-  int act, left, lanes, whole;
-  bool leads, has_gate, has_codes;
+  uint32_t gate_step, scale_step;
+  int act, left, lanes;
+  bool leads;
   __device__ __forceinline__ Emitter(const Forward<T>& p, const Place& at, const Share& sh) {
     const Geom& g = p.g;
     const size_t row = sh.row0 + at.r, off = row * g.C + at.c0;
     act = ACT < 0 ? p.act : ACT;
-    left = at.left; whole = sh.whole;
+    left = at.left;
     y = p.y + off;
-    step = (uint32_t)g.rp * g.C;
-    if constexpr (EXTRA) {
-      const int all_cols = (g.C + 7) >> 3, per_row = (g.C + kCkptBlock - 1) / kCkptBlock;
-      res = p.res ? p.res + off : nullptr;
-      has_gate = p.gate != nullptr; has_codes = p.codes != nullptr;
-      codes = p.codes + off;
-      gate = p.gate + (row * all_cols + (at.c0 >> 3));
-      scales = p.scales + (row * per_row + at.c0 / kCkptBlock);
+    res = nullptr; gate = nullptr; codes = nullptr;
+    if constexpr (EXTRA >= WITH_RES_GATE) {
+      const int all_cols = (g.C + 7) >> 3;
+      if (p.res) res = p.res + off;
+      if (p.gate) gate = p.gate + (row * all_cols + (at.c0 >> 3));
       gate_step = (uint32_t)g.rp * all_cols;
+    }
+    if constexpr (EXTRA == WITH_CODES) {
+      const int per_row = (g.C + kCkptBlock - 1) / kCkptBlock;
+      if (VEC || p.codes) codes = p.codes + off;             // the form for any alignment is compiled once, for all options
+      scales = p.scales + (row * per_row + at.c0 / kCkptBlock);
       scale_step = (uint32_t)g.rp * per_row;
       lanes = p.ckpt_lanes;
       leads = (at.col & (lanes - 1)) == 0;
-      all = __ballot_sync(0xffffffffu, at.active);
-      tail = __ballot_sync(0xffffffffu, sh.mine > sh.whole);
-    } else {
-      res = nullptr;
     }
   }
-  // `turn`: how many of its pixels the thread has had; k: which of them this one is.
-  __device__ __forceinline__ void one(int turn, uint32_t k, const Affine<T>& affine, const Raw8<T>& raw, const Raw8<T>& raw_res) const {
-    const F8 x = raw8_to_f8(raw);
+  // Pixel k of the thread, at element offset o = k * rp * C.
+  __device__ __forceinline__ void value(uint32_t k, uint32_t o, const Affine<T>& affine, const F8& x, const Raw8<T>& raw_res) const {
     F8 z;
 #pragma unroll
     for (int j = 0; j < 4; ++j) z.p[j] = affine.of(j, x.p[j]);
-    if constexpr (EXTRA)
+    if constexpr (EXTRA >= WITH_RES_GATE)
       if (res) {
         const F8 r = raw8_to_f8(raw_res);
 #pragma unroll
@@ -430,9 +440,9 @@ template <typename T, bool VEC, int ACT, bool EXTRA> struct Emitter {
       }
     if (act == ACT_RELU) {
       const Raw8<T> out = f8_to_raw8<T, true>(z);
-      raw8_put<T, VEC>(y + k * step, left, out);
-      if constexpr (EXTRA)
-        if (has_gate) gate[k * gate_step] = (uint8_t)(positive_bits(out) & (VEC ? 0xFFu : (1u << left) - 1));
+      raw8_put<T, VEC>(y + o, left, out);
+      if constexpr (EXTRA >= WITH_RES_GATE)
+        if (gate) gate[k * gate_step] = (uint8_t)(positive_bits(out) & (VEC ? 0xFFu : (1u << left) - 1));
     } else {
       if (act == ACT_SILU) {
 #pragma unroll
@@ -441,30 +451,59 @@ template <typename T, bool VEC, int ACT, bool EXTRA> struct Emitter {
           z.p[j] = mul2(z.p[j], pair(sigmoid<T>(h.x), sigmoid<T>(h.y)));
         }
       }
-      raw8_put<T, VEC>(y + k * step, left, f8_to_raw8<T>(z));
+      raw8_put<T, VEC>(y + o, left, f8_to_raw8<T>(z));
     }
-    if constexpr (EXTRA)
-      if (has_codes) {
-        const CkptScale s = ckpt_scale(ckpt_top_of_lanes(ckpt_top(raw), lanes, turn < whole ? all : tail));
-        store_codes<VEC>(codes + k * step, 0, left, ckpt_codes(x, s));
-        if (leads) scales[k * scale_step] = (uint8_t)s.byte;
+  }
+  // A turn of B pixels, raw, k counting from the thread's first pixel or (back) its last; for the whole warp where codes are
+  // formed, since the lanes that share a block of 32 channels (they have the same pixels) exchange its maximum.
+  template <int B>
+  __device__ __forceinline__ void turn(int k, int mine, bool back, uint32_t step, const Affine<T>& affine, const Raw8<T> (&raw)[B], const Raw8<T>* raw_res) const {
+    uint32_t top[B];
+    if constexpr (EXTRA == WITH_CODES)
+      if (VEC || codes) block_tops<B>(raw, top);
+#pragma unroll
+    for (int u = 0; u < B; ++u)
+      if (k + u < mine) {
+        const uint32_t kk = (uint32_t)(back ? mine - 1 - (k + u) : k + u), o = kk * step;
+        const F8 x = raw8_to_f8(raw[u]);
+        value(kk, o, affine, x, raw_res[EXTRA >= WITH_RES_GATE ? u : 0]);
+        if constexpr (EXTRA == WITH_CODES)
+          if (VEC || codes) {
+            const CkptScale s = ckpt_scale(top[u]);
+            store_codes<VEC>(codes + o, 0, left, ckpt_codes(x, s));
+            if (leads) scales[kk * scale_step] = (uint8_t)s.byte;
+          }
       }
+  }
+  // The largest magnitudes of the blocks of B vectors: 16-bit ones travel two to a word.
+  template <int B> __device__ __forceinline__ void block_tops(const Raw8<T> (&raw)[B], uint32_t (&top)[B]) const {
+    if constexpr (sizeof(T) == 2 && B == 2) {
+      const uint32_t a = ckpt_top2(raw[0]), b = ckpt_top2(raw[1]);
+      uint32_t m = max_u16x2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+      if (lanes >= 2) m = max_u16x2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+      if (lanes >= 4) m = max_u16x2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+      top[0] = m << 16;
+      top[1] = m & 0xFFFF0000u;
+    } else {
+#pragma unroll
+      for (int u = 0; u < B; ++u) top[u] = ckpt_top_of_lanes(ckpt_top(raw[u]), lanes);
+    }
   }
 };
 // The constants of a thread's channels from their groups' statistics.
 template <typename T, typename Stat>
 __device__ __forceinline__ void load_affine(const Forward<T>& p, const Place& at, const float (&gamma)[8], const float (&beta)[8], Stat stat, Affine<T>& affine) {
   float2 m[8];
-  each_channel(at, p.g.Cg, [&](int i, int, int s) { m[i] = stat(s); });
+  each_channel(p.g, at, [&](int i, int, int s) { m[i] = stat(s); });
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     affine.set(j, make_float2(m[2 * j].x, m[2 * j + 1].x), make_float2(gamma[2 * j] * m[2 * j].y, gamma[2 * j + 1] * m[2 * j + 1].y),
                make_float2(beta[2 * j], beta[2 * j + 1]));
 }
 
-// The resident form: blockIdx.x = image * parts + share of its pixels, a cluster per image.
-template <typename T, bool VEC, int ACT, bool EXTRA>
-__global__ void __launch_bounds__(kThreads, 2) forward_kernel(const __grid_constant__ Forward<T> p) {
+// The resident form: blockIdx = image, share of its pixels, tile of columns: a cluster per image.
+template <typename T, bool VEC, int ACT, int EXTRA>
+__global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_constant__ Forward<T> p) {
   constexpr int kBatch = 2;
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
@@ -473,7 +512,7 @@ __global__ void __launch_bounds__(kThreads, 2) forward_kernel(const __grid_const
   float2* chan = reinterpret_cast<float2*>(common + kThreads * 8);                               // [C]
   float* own = reinterpret_cast<float*>(chan + g.C);      // mean [G], squared deviations [G] of this CTA's pixels
   float2* mom = reinterpret_cast<float2*>(own + 2 * g.G);                                        // mean, rstd [G] of the image
-  const int rank = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
+  const int rank = blockIdx.y, n = blockIdx.x;
   const Place at(g, 0);
   const Share sh(g, at, n, rank);
   const Slots<T> slots(smem);
@@ -483,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 2) forward_kernel(const __grid_const
 #pragma unroll 4
   for (int k = 0; k < sh.mine; ++k) slots.template fetch<VEC>(k, src + (uint32_t)k * step, at.left);
   const Emitter<T, VEC, ACT, EXTRA> out(p, at, sh);
-  if constexpr (EXTRA)
+  if constexpr (EXTRA >= WITH_RES_GATE)
     if (out.res)
       for (int k = 0; k < sh.mine; ++k) prefetch_l2(out.res + (uint32_t)k * step);
   float gamma[8], beta[8];
@@ -509,18 +548,15 @@ __global__ void __launch_bounds__(kThreads, 2) forward_kernel(const __grid_const
   __syncthreads();
   Affine<T> affine;
   load_affine(p, at, gamma, beta, [&](int s) { return mom[s]; }, affine);
-  for (int k = 0; k < sh.mine; k += kBatch) {
-    Raw8<T> xs[kBatch], rs[EXTRA ? kBatch : 1];
+  for (int k = 0; k < (EXTRA == WITH_CODES ? sh.turns : sh.mine); k += kBatch) {
+    Raw8<T> xs[kBatch], rs[EXTRA >= WITH_RES_GATE ? kBatch : 1];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (k + u < sh.mine) {
-        xs[u] = slots.get(k + u);
-        if constexpr (EXTRA)
-          if (out.res) rs[u] = raw8_load<T, VEC>(out.res + (uint32_t)(k + u) * step, at.left);
-      }
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (k + u < sh.mine) out.one(k + u, k + u, affine, xs[u], rs[EXTRA ? u : 0]);
+    for (int u = 0; u < kBatch; ++u) {
+      if (EXTRA == WITH_CODES || k + u < sh.mine) xs[u] = slots.get(min(k + u, g.iters - 1));
+      if constexpr (EXTRA >= WITH_RES_GATE)
+        if (out.res && k + u < sh.mine) rs[u] = raw8_load<T, VEC>(out.res + (uint32_t)(k + u) * step, at.left);
+    }
+    out.turn(k, sh.mine, false, step, affine, xs, rs);
   }
   cluster.barrier_wait(std::move(token));                                 // nor do they read its own
 }
@@ -534,29 +570,36 @@ __global__ void __launch_bounds__(kThreads, 3) moments_kernel(const __grid_const
   float* red = reinterpret_cast<float*>(smem + kRing * Slots<T>::Q * kThreads);   // [4096]
   float* common = red + 2 * kThreads * 8;                                      // [2048]
   float2* chan = reinterpret_cast<float2*>(common + kThreads * 8);             // [8 * cols]
-  const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
-  Place at(g, blockIdx.y);
+  const int part = blockIdx.y, n = blockIdx.x;
+  Place at(g, blockIdx.z);
   at.active = at.active && at.left > 0;
   const Share sh(g, at, n, part);
+  // The next kernel may start once every CTA is past the wait: what this kernel's inputs come from is complete then, so the
+  // next one copies from them (and from nothing that this kernel writes) before its own wait.
   grid_dependency_wait();
   grid_dependency_release();
   const T* src = p.x + (sh.row0 + at.r) * g.C + at.c0;
   const uint32_t step = (uint32_t)g.rp * g.C;
   const Slots<T> ring(smem);
   Moments m;
-  stream<kBatch>(sh.mine, [&](int k) { ring.template fetch<VEC>(k % kRing, src + (uint32_t)k * step, at.left); }, [&](int k) {
-    if (k == 0) m.start(raw8_to_f8(ring.get(0)));
+  auto issue = [&](int slot) {
+    ring.template fetch<VEC>(slot, src, at.left);
+    src += step;
+  };
+  Stream<kBatch>::start(sh.mine, issue);
+  Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot) {
+    if (k == 0) m.start(raw8_to_f8(ring.get(slot)));
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      if (k + u < sh.mine) m.add(raw8_to_f8(ring.get((k + u) % kRing)));
+      if (k + u < sh.mine) m.add(raw8_to_f8(ring.get(slot + u)));
   });
-  const int c_first = blockIdx.y * kMaxCols * 8, sets = min(g.cols * 8, g.C - c_first);
+  const int c_first = blockIdx.z * kMaxCols * 8, sets = min(g.cols * 8, g.C - c_first);
   cta_moments(g, at, m, sh.mine, sh.count, sets, red, common, chan);
   if (g.tiles == 1) {
-    float* out = p.partial + (size_t)blockIdx.x * 2 * g.G;
+    float* out = p.partial + ((size_t)n * g.parts + part) * 2 * g.G;
     group_moments(g, sh.count, chan, [&](int s, float mu, float q) { out[s] = mu; out[g.G + s] = q; });
   } else {
-    float* out = p.partial + (size_t)blockIdx.x * 2 * g.C + c_first;
+    float* out = p.partial + ((size_t)n * g.parts + part) * 2 * g.C + c_first;
     for (int c = threadIdx.x; c < sets; c += kThreads) { out[c] = chan[c].x; out[g.C + c] = chan[c].y; }
   }
 }
@@ -612,21 +655,33 @@ __global__ void __launch_bounds__(1024) combine_kernel(const __grid_constant__ F
 
 // Streamed, second pass: y from x and the statistics, which every CTA of an image forms from the rows of sums itself (the same
 // bits everywhere; its first CTA writes them out) unless combine_kernel has.
-template <typename T, bool VEC, int ACT, bool EXTRA>
-__global__ void __launch_bounds__(kThreads, 2) apply_kernel(const __grid_constant__ Forward<T> p) {
+template <typename T, bool VEC, int ACT, int EXTRA>
+__global__ void __launch_bounds__(kThreads, 3) apply_kernel(const __grid_constant__ Forward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
   const Slots<T> ring(smem), res_ring(smem + kRing * Slots<T>::Q * kThreads);
-  float2* mom = reinterpret_cast<float2*>(smem + (EXTRA && p.res ? 2 : 1) * kRing * Slots<T>::Q * kThreads);    // [G], unless combined
-  const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
-  Place at(g, blockIdx.y);
+  float2* mom = reinterpret_cast<float2*>(smem + (EXTRA >= WITH_RES_GATE && p.res ? 2 : 1) * kRing * Slots<T>::Q * kThreads);    // [G], unless combined
+  const int part = blockIdx.y, n = blockIdx.x;
+  Place at(g, blockIdx.z);
   at.active = at.active && at.left > 0;
   if (at.left <= 0) { at.c0 = 0; at.left = 1; }
   const Share sh(g, at, n, part);
+  const Emitter<T, VEC, ACT, EXTRA> out(p, at, sh);
+  const uint32_t step = (uint32_t)g.rp * g.C;
+  const T* x = p.x + (sh.row0 + at.r) * g.C + at.c0 + (uint32_t)max(sh.mine - 1, 0) * step;
+  const T* res = out.res + (uint32_t)max(sh.mine - 1, 0) * step;
+  auto issue = [&](int slot) {
+    ring.template fetch<VEC>(slot, x, at.left);
+    x -= step;
+    if constexpr (EXTRA >= WITH_RES_GATE)
+      if (out.res) { res_ring.template fetch<VEC>(slot, res, at.left); res -= step; }
+  };
   float gamma[8], beta[8];
+  if constexpr (VEC) Stream<kBatch>::start(sh.mine, issue);      // see grid_dependency_release in moments_kernel
   grid_dependency_wait();
   grid_dependency_release();
+  if constexpr (!VEC) Stream<kBatch>::start(sh.mine, issue);
 #pragma unroll
   for (int i = 0; i < 8; ++i) { gamma[i] = p.gamma[at.channel(i)]; beta[i] = p.beta[at.channel(i)]; }
   if (!p.combined) {
@@ -645,23 +700,15 @@ __global__ void __launch_bounds__(kThreads, 2) apply_kernel(const __grid_constan
     load_affine(p, at, gamma, beta, [&](int s) { return make_float2(p.stats[(size_t)n * g.G + s], p.stats[(size_t)(g.N + n) * g.G + s]); }, affine);
   else
     load_affine(p, at, gamma, beta, [&](int s) { return mom[s]; }, affine);
-  const T* x = p.x + (sh.row0 + at.r) * g.C + at.c0;
-  const Emitter<T, VEC, ACT, EXTRA> out(p, at, sh);
-  const int last = sh.mine - 1;
-  stream<kBatch>(sh.mine, [&](int k) {
-    const uint32_t o = (uint32_t)(last - k) * out.step;
-    ring.template fetch<VEC>(k % kRing, x + o, at.left);
-    if constexpr (EXTRA)
-      if (out.res) res_ring.template fetch<VEC>(k % kRing, out.res + o, at.left);
-  }, [&](int k) {
+  Stream<kBatch>::run(EXTRA == WITH_CODES ? sh.turns : sh.mine, sh.mine, issue, [&](int k, int slot) {
+    Raw8<T> xs[kBatch], rs[EXTRA >= WITH_RES_GATE ? kBatch : 1];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (k + u < sh.mine) {
-        Raw8<T> r;
-        if constexpr (EXTRA)
-          if (out.res) r = res_ring.get((k + u) % kRing);
-        out.one(k + u, last - (k + u), affine, ring.get((k + u) % kRing), r);
-      }
+    for (int u = 0; u < kBatch; ++u) {
+      if (EXTRA == WITH_CODES || k + u < sh.mine) xs[u] = ring.get(slot + u);
+      if constexpr (EXTRA >= WITH_RES_GATE)
+        if (out.res && k + u < sh.mine) rs[u] = res_ring.get(slot + u);
+    }
+    out.turn(k, sh.mine, true, step, affine, xs, rs);
   });
 }
 
@@ -795,6 +842,7 @@ template <typename T, bool VEC, bool CK> struct Feed {
   int left, slope, n;
   bool reverse;
   uint32_t scale[3][kBatch], open[3][kBatch];     // of this turn, the next, and the one after
+  uint32_t next, step;                            // element offset of the next vector to be copied
   static constexpr int kVec = kRing * Slots<T>::Q * kThreads;        // 16-byte words of a ring
   // words of shared memory of a pass, in 16 bytes
   static __host__ __device__ __forceinline__ int words(bool mask, bool res) {
@@ -804,8 +852,8 @@ template <typename T, bool VEC, bool CK> struct Feed {
       : from(p, at, sh), dys(smem), xs(smem + kVec), masks(smem + kVec + (CK ? kRing * kThreads / 2 : kVec)),
         ress(smem + words(slope_ == SLOPE_MASK, false)), codes(reinterpret_cast<uint2*>(smem + kVec) + threadIdx.x),
         res(res_ ? res_ + (sh.row0 + at.r) * p.g.C + at.c0 : nullptr), left(at.left), slope(slope_), n(sh.mine), reverse(reverse_) {
-    bytes(0, 1);
-    bytes(kBatch, 2);
+    step = reverse ? 0u - from.step : from.step;
+    next = reverse && n > 0 ? (uint32_t)(n - 1) * from.step : 0u;
   }
   __device__ __forceinline__ uint32_t at(int k) const { return (uint32_t)(reverse ? n - 1 - k : k); }
   __device__ __forceinline__ void bytes(int k, int to) {
@@ -816,9 +864,9 @@ template <typename T, bool VEC, bool CK> struct Feed {
         if (slope == SLOPE_BITS) open[to][u] = from.gate[at(k + u) * from.gate_step];
       }
   }
-  __device__ __forceinline__ void issue(int k) const {
-    const uint32_t o = at(k) * from.step;
-    const int s = k % kRing;
+  __device__ __forceinline__ void issue(int s) {
+    const uint32_t o = next;
+    next += step;
     dys.template fetch<VEC>(s, from.dy + o, left);
     if constexpr (CK) {
       if constexpr (VEC) copy8_async(codes + s * kThreads, from.codes + o); else codes[s * kThreads] = load_codes<false>(from.codes + o, 0, left);
@@ -837,9 +885,9 @@ template <typename T, bool VEC, bool CK> struct Feed {
     }
     bytes(k + 2 * kBatch, 2);
   }
-  __device__ __forceinline__ Held<T, CK> get(int k, int u) const {
+  __device__ __forceinline__ Held<T, CK> get(int slot, int u) const {
     Held<T, CK> h;
-    const int s = (k + u) % kRing;
+    const int s = slot + u;
     h.dy = dys.get(s);
     if constexpr (CK) { h.codes = codes[s * kThreads]; h.scale = scale[0][u]; } else { h.x = xs.get(s); }
     if (slope == SLOPE_MASK) h.mask = masks.get(s);
@@ -853,7 +901,7 @@ template <typename T>
 __device__ __forceinline__ void load_channels(const Backward<T>& p, const Place& at, int n, int slope, Channels& ch, float (&rstd)[8]) {
   const Geom& g = p.g;
   float mean[8], scale[8], shift[8];
-  each_channel(at, g.Cg, [&](int i, int c, int s) {
+  each_channel(g, at, [&](int i, int c, int s) {
     mean[i] = p.stats[(size_t)n * g.G + s];
     rstd[i] = p.stats[(size_t)(g.N + n) * g.G + s];
     scale[i] = p.gamma[c] * rstd[i];
@@ -867,9 +915,9 @@ __device__ __forceinline__ void load_channels(const Backward<T>& p, const Place&
   }
 }
 // k1, k2 of a thread's channels from those of the groups, the first of which is `first`.
-__device__ __forceinline__ void load_coefficients(const Place& at, int Cg, const float* c1, const float* c2, int first, f32x2 (&k1)[4], f32x2 (&k2)[4]) {
+__device__ __forceinline__ void load_coefficients(const Geom& g, const Place& at, const float* c1, const float* c2, int first, f32x2 (&k1)[4], f32x2 (&k2)[4]) {
   float a[8], b[8];
-  each_channel(at, Cg, [&](int i, int, int s) { a[i] = -c1[s - first]; b[i] = -c2[s - first]; });
+  each_channel(g, at, [&](int i, int, int s) { a[i] = -c1[s - first]; b[i] = -c2[s - first]; });
 #pragma unroll
   for (int j = 0; j < 4; ++j) { k1[j] = pair(a[2 * j], a[2 * j + 1]); k2[j] = pair(b[2 * j], b[2 * j + 1]); }
 }
@@ -915,7 +963,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
   float* coef = own + 2 * g.G;                // [2][G]
   uint8_t* open = reinterpret_cast<uint8_t*>(coef + 2 * g.G);
   uint8_t* scale_bytes = open + vecs;
-  const int rank = blockIdx.x % g.parts, n = blockIdx.x / g.parts, tid = threadIdx.x;
+  const int rank = blockIdx.y, n = blockIdx.x, tid = threadIdx.x;
   const Place at(g, 0);
   const Share sh(g, at, n, rank);
   const Slots<T> dys(smem), xslots(xs);
@@ -1012,7 +1060,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
   cg::cluster_group::arrival_token token = cluster.barrier_arrive();
   __syncthreads();
   f32x2 k1[4], k2[4];
-  load_coefficients(at, g.Cg, coef, coef + g.G, 0, k1, k2);
+  load_coefficients(g, at, coef, coef + g.G, 0, k1, k2);
   T* const dx = p.dx + (sh.row0 + at.r) * g.C + at.c0;
   for (int k = 0; k < sh.mine; k += kBatch) {
     Raw8<T> rs[kBatch];
@@ -1036,24 +1084,28 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
   const int slope = SLOPE < 0 ? p.slope : SLOPE;
-  const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
-  Place at(g, blockIdx.y);
+  const int part = blockIdx.y, n = blockIdx.x;
+  Place at(g, blockIdx.z);
   at.active = at.active && at.left > 0;
-  if (at.left <= 0) { at.c0 = blockIdx.y * kMaxCols * 8; at.left = 1; }
+  if (at.left <= 0) { at.c0 = blockIdx.z * kMaxCols * 8; at.left = 1; }
   const Share sh(g, at, n, part);
   grid_dependency_wait();
   grid_dependency_release();
   Feed<T, VEC, CK> feed(p, at, sh, slope, nullptr, false, smem);
+  feed.bytes(0, 1);
+  feed.bytes(kBatch, 2);
   Channels ch;
   float rstd[8];
-  load_channels(p, at, n, slope, ch, rstd);
   Sums sums;
-  stream<kBatch>(sh.mine, [&](int k) { feed.issue(k); }, [&](int k) {
+  auto issue = [&](int slot) { feed.issue(slot); };
+  Stream<kBatch>::start(sh.mine, issue);
+  load_channels(p, at, n, slope, ch, rstd);
+  Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot) {
     feed.turn(k);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (k + u < sh.mine) {
-        const Held<T, CK> h = feed.get(k, u);
+        const Held<T, CK> h = feed.get(slot, u);
         F8 dz, d;
         operands<T, CK>(passed<T, CK>(h, slope), h, slope, ch, dz, d);
         sums.add(dz, d);
@@ -1063,8 +1115,8 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
   float* red = reinterpret_cast<float*>(smem);
   sums.put(red, g, at, rstd);
   __syncthreads();
-  const int c_first = blockIdx.y * kMaxCols * 8, sets = min(g.cols * 8, g.C - c_first);
-  float* out = p.partial + (size_t)blockIdx.x * 2 * g.C + c_first;
+  const int c_first = blockIdx.z * kMaxCols * 8, sets = min(g.cols * 8, g.C - c_first);
+  float* out = p.partial + ((size_t)n * g.parts + part) * 2 * g.C + c_first;
   channel_sums(red, g, sets, g.lanes_c, [&](int c, float a, float b) { out[c] = a; out[g.C + c] = b; });
 }
 
@@ -1103,17 +1155,22 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   const Geom& g = p.g;
   float* coef = reinterpret_cast<float*>(smem + Feed<T, VEC, CK>::words((SLOPE < 0 ? p.slope : SLOPE) == SLOPE_MASK, p.res != nullptr));   // [2][sets]
   const int slope = SLOPE < 0 ? p.slope : SLOPE;
-  const int part = blockIdx.x % g.parts, n = blockIdx.x / g.parts;
-  const int c_first = blockIdx.y * kMaxCols * 8;
-  Place at(g, blockIdx.y);
+  const int part = blockIdx.y, n = blockIdx.x;
+  const int c_first = blockIdx.z * kMaxCols * 8;
+  Place at(g, blockIdx.z);
   at.active = at.active && at.left > 0;
   if (at.left <= 0) { at.c0 = c_first; at.left = 1; }
   const Share sh(g, at, n, part);
   const int c_last = min(g.C, c_first + g.cols * 8) - 1;
   const int g_first = c_first / g.Cg, sets = c_last / g.Cg - g_first + 1, c_base = g_first * g.Cg;
+  Feed<T, VEC, CK> feed(p, at, sh, slope, p.res, true, smem);
+  if constexpr (VEC) Stream<kBatch>::start(sh.mine, [&](int slot) { feed.issue(slot); });
   grid_dependency_wait();
   grid_dependency_release();
-  Feed<T, VEC, CK> feed(p, at, sh, slope, p.res, true, smem);
+  auto issue = [&](int slot) { feed.issue(slot); };
+  if constexpr (!VEC) Stream<kBatch>::start(sh.mine, issue);
+  feed.bytes(0, 1);
+  feed.bytes(kBatch, 2);
   Channels ch;
   float rstd[8];
   load_channels(p, at, n, slope, ch, rstd);
@@ -1133,16 +1190,16 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   });
   __syncthreads();
   f32x2 k1[4], k2[4];
-  load_coefficients(at, g.Cg, coef, coef + sets, g_first, k1, k2);
+  load_coefficients(g, at, coef, coef + sets, g_first, k1, k2);
   T* const dx = p.dx + (sh.row0 + at.r) * g.C + at.c0;
-  stream<kBatch>(sh.mine, [&](int k) { feed.issue(k); }, [&](int k) {
+  Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot) {
     feed.turn(k);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (k + u < sh.mine) {
-        const Held<T, CK> h = feed.get(k, u);
+        const Held<T, CK> h = feed.get(slot, u);
         Raw8<T> r;
-        if (feed.res) r = feed.ress.get((k + u) % kRing);
+        if (feed.res) r = feed.ress.get(slot + u);
         raw8_put<T, VEC>(dx + feed.at(k + u) * feed.from.step, at.left,
                          dx_of<T, CK>(passed<T, CK>(h, slope), h, slope, ch, k1, k2, feed.res ? &r : nullptr));
       }
@@ -1174,8 +1231,15 @@ inline Plan plan(int N, int P, int C, int G, size_t vec_bytes, size_t fixed, int
   g.cols = std::min(all_cols, kMaxCols);
   g.tiles = (all_cols + kMaxCols - 1) / kMaxCols;
   g.rp = kThreads / g.cols;
+  g.col_mul = (65536 + g.cols - 1) / g.cols;              // exact for tid < 256: the excess is below 256 / 65536 <= 1 / cols
+  g.cg_mul = g.Cg == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + g.Cg - 1) / g.Cg);      // exact for c * Cg < 2^32 (C <= 2^16)
   g.lanes_g = pow2_up_to(kThreads / std::min(G, kThreads), 32);
   g.lanes_c = pow2_up_to(kThreads / std::min(g.cols * 8, kThreads), 32);
+  auto shares = [&]() {
+    g.whole = g.pix / g.rp;
+    const int last = P % g.pix;
+    g.whole_last = last ? last / g.rp : g.whole;
+  };
   auto split = [&](int parts) {
     g.pix = P / parts + (P % parts != 0);
     g.parts = parts;
@@ -1189,13 +1253,14 @@ inline Plan plan(int N, int P, int C, int G, size_t vec_bytes, size_t fixed, int
     // few images: more SMs, while every thread keeps two pixels
     while (parts < kMaxCluster && (int64_t)N * parts * 2 <= 2 * kSms && (split(parts), g.iters) >= 4) parts *= 2;
     pl.smem = split(parts);
-    pl.resident = pl.smem <= kSmemMost && (int64_t)N * g.parts <= INT32_MAX;
-    if (f_ && f_[0] == 'o') pl.resident = pl.resident && (int64_t)N * g.parts <= 2 * kSms;
+    pl.resident = pl.smem <= kSmemMost && (int64_t)N * g.parts <= 2 * kSms;
+    shares();
     if (pl.resident) return pl;
   }
   // one wave of CTAs, each with at least one batch of pixels in flight
   split((int)std::max<int64_t>(1, std::min<int64_t>((int64_t)per_sm * kSms / N, P / (4 * g.rp))));
   g.parts = P / g.pix + (P % g.pix != 0);         // none without pixels
+  shares();
   return pl;
 }
 inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G) {
@@ -1208,7 +1273,7 @@ inline Plan plan_backward(int elem_bytes, int N, int P, int C, int G, bool ckpt)
 // Whether every launch's grid can be given.
 inline bool grid_ok(const Plan& pl) {
   const Geom& g = pl.g;
-  return pl.resident || ((int64_t)g.N * g.parts <= INT32_MAX && (int64_t)g.N * g.G <= INT32_MAX && g.tiles <= 65535 &&
+  return pl.resident || ((int64_t)g.N * g.parts <= INT32_MAX && (int64_t)g.N * g.G <= INT32_MAX &&
                          (int64_t)g.N * ((2 * (int64_t)g.C + 31) / 32) <= INT32_MAX);
 }
 inline size_t partial_floats(const Plan& pl) { return pl.resident ? 0 : (size_t)pl.g.N * pl.g.parts * 2 * pl.g.C; }
@@ -1217,24 +1282,24 @@ inline bool merges(const Geom& g) { return g.tiles == 1 && g.parts <= kMergePart
 
 // ---- host side: launches ---------------------------------------------------------------------------------------
 template <typename Kernel, typename Params>
-inline cudaError_t launch_cluster(Kernel kernel, int blocks, int cluster, size_t smem, cudaStream_t st, const Params& p) {
+inline cudaError_t launch_cluster(Kernel kernel, int images, int cluster, size_t smem, cudaStream_t st, const Params& p) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.gridDim = dim3((unsigned)images, (unsigned)cluster); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = (unsigned)cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  at[1].val.clusterDim.x = 1; at[1].val.clusterDim.y = (unsigned)cluster; at[1].val.clusterDim.z = 1;
   cfg.attrs = at; cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-template <typename T, bool VEC, int ACT, bool EXTRA> inline cudaError_t launch_forward_as(cudaStream_t st, const Plan& pl, Forward<T> p) {
+template <typename T, bool VEC, int ACT, int EXTRA> inline cudaError_t launch_forward_as(cudaStream_t st, const Plan& pl, Forward<T> p) {
   const Geom& g = pl.g;
   if (pl.resident) {
     static OncePerDevice once;
     const cudaError_t e = once_per_device(&once, []() { return set_smem_limit(forward_kernel<T, VEC, ACT, EXTRA>, kSmemMost); });
-    return e != cudaSuccess ? e : launch_cluster(forward_kernel<T, VEC, ACT, EXTRA>, g.N * g.parts, g.parts, pl.smem, st, p);
+    return e != cudaSuccess ? e : launch_cluster(forward_kernel<T, VEC, ACT, EXTRA>, g.N, g.parts, pl.smem, st, p);
   }
   static OncePerDevice once;
   cudaError_t e = once_per_device(&once, []() {
@@ -1242,7 +1307,7 @@ template <typename T, bool VEC, int ACT, bool EXTRA> inline cudaError_t launch_f
     return f != cudaSuccess ? f : set_smem_limit(apply_kernel<T, VEC, ACT, EXTRA>, kSmemMost);
   });
   if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)(g.N * g.parts), (unsigned)g.tiles);
+  const dim3 grid((unsigned)g.N, (unsigned)g.parts, (unsigned)g.tiles);
   const size_t ring = (size_t)ring_of<T>() * kThreads * 8 * sizeof(T);
   e = launch_chained(moments_kernel<T, VEC>, grid, dim3(kThreads), ring + 3 * kThreads * 8 * 4 + 64 * (size_t)g.cols, st, p);
   p.combined = !merges(g);
@@ -1255,6 +1320,10 @@ template <typename T, bool VEC, int ACT, bool EXTRA> inline cudaError_t launch_f
   return e;
 }
 
+template <typename T, int ACT> inline cudaError_t launch_forward_act(cudaStream_t st, const Plan& pl, const Forward<T>& p) {
+  return p.codes ? launch_forward_as<T, true, ACT, WITH_CODES>(st, pl, p)
+                 : p.res || p.gate ? launch_forward_as<T, true, ACT, WITH_RES_GATE>(st, pl, p) : launch_forward_as<T, true, ACT, PLAIN>(st, pl, p);
+}
 template <typename T>
 inline cudaError_t launch_forward(cudaStream_t st, const Plan& pl, Forward<T> p) {
   p.g = pl.g;
@@ -1263,12 +1332,9 @@ inline cudaError_t launch_forward(cudaStream_t st, const Plan& pl, Forward<T> p)
   int8_t* codes = p.codes;
   if (p.ckpt_lanes == 0) p.codes = nullptr;       // blocks that do not fall on groups of lanes: a pass of their own
   const bool vec = C % 8 == 0 && aligned_to(p.x, 16) && aligned_to(p.y, 16) && aligned_to(p.res, 16) && aligned_to(p.codes, 8);
-  const bool extra = p.res || p.gate || p.codes;
-  cudaError_t e;
-  if (!vec) e = launch_forward_as<T, false, -1, true>(st, pl, p);
-  else if (p.act == ACT_RELU) e = extra ? launch_forward_as<T, true, ACT_RELU, true>(st, pl, p) : launch_forward_as<T, true, ACT_RELU, false>(st, pl, p);
-  else if (p.act == ACT_SILU) e = extra ? launch_forward_as<T, true, ACT_SILU, true>(st, pl, p) : launch_forward_as<T, true, ACT_SILU, false>(st, pl, p);
-  else e = extra ? launch_forward_as<T, true, ACT_NONE, true>(st, pl, p) : launch_forward_as<T, true, ACT_NONE, false>(st, pl, p);
+  cudaError_t e = !vec ? launch_forward_as<T, false, -1, WITH_CODES>(st, pl, p)
+                         : p.act == ACT_RELU ? launch_forward_act<T, ACT_RELU>(st, pl, p)
+                         : p.act == ACT_SILU ? launch_forward_act<T, ACT_SILU>(st, pl, p) : launch_forward_act<T, ACT_NONE>(st, pl, p);
   if (e == cudaSuccess && codes && !p.codes) e = launch_ckpt_encode<T>(st, p.x, (size_t)p.g.N * p.g.P, C, codes, p.scales);
   return e;
 }
@@ -1281,14 +1347,14 @@ inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<
   if (pl.resident) {
     static OncePerDevice once;
     e = once_per_device(&once, []() { return set_smem_limit(backward_kernel<T, VEC, CK, SLOPE>, kSmemMost); });
-    if (e == cudaSuccess) e = launch_cluster(backward_kernel<T, VEC, CK, SLOPE>, g.N * g.parts, g.parts, pl.smem, st, p);
+    if (e == cudaSuccess) e = launch_cluster(backward_kernel<T, VEC, CK, SLOPE>, g.N, g.parts, pl.smem, st, p);
   } else {
     static OncePerDevice once;
     e = once_per_device(&once, []() {
       const cudaError_t f = set_smem_limit(backward_sums_kernel<T, VEC, CK, SLOPE>, kSmemMost);
       return f != cudaSuccess ? f : set_smem_limit(backward_apply_kernel<T, VEC, CK, SLOPE>, kSmemMost);
     });
-    const dim3 grid((unsigned)(g.N * g.parts), (unsigned)g.tiles);
+    const dim3 grid((unsigned)g.N, (unsigned)g.parts, (unsigned)g.tiles);
     auto rings = [&](bool res) { return 16 * (size_t)Feed<T, VEC, CK>::words(p.slope == SLOPE_MASK, res); };
     if (e == cudaSuccess)
       e = launch_chained(backward_sums_kernel<T, VEC, CK, SLOPE>, grid, dim3(kThreads), std::max(rings(false), (size_t)2 * kThreads * 8 * 4), st, p);

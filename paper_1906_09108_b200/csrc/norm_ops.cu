@@ -15,7 +15,7 @@ static fdg_status status_of(cudaError_t e) { return e == cudaSuccess ? FDG_OK : 
 static bool rows_ok(size_t rows, int C) { return C >= 1 && rows >= 1 && rows <= ((size_t)1 << 40) / (size_t)C; }
 static bool gn_shape_ok(int precision, const fdg_gn_shape* s) {
   if (!s || !precision_ok(precision) || s->N < 1 || s->HW < 1 || s->C < 1 || s->groups < 1 || s->C % s->groups) return false;
-  if (s->C > 1 << 24 || !rows_ok((size_t)s->N * (size_t)s->HW, s->C)) return false;
+  if (s->C > 1 << 16 || !rows_ok((size_t)s->N * (size_t)s->HW, s->C)) return false;
   const int b = (int)elem_bytes(precision);
   return gn::grid_ok(gn::plan_forward(b, s->N, s->HW, s->C, s->groups)) && gn::grid_ok(gn::plan_backward(b, s->N, s->HW, s->C, s->groups, false)) &&
          gn::grid_ok(gn::plan_backward(b, s->N, s->HW, s->C, s->groups, true));
