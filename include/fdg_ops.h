@@ -184,8 +184,8 @@ fdg_status fdg_ckpt_decode(int precision, const int8_t* codes, const uint8_t* sc
  * [g*C/groups, (g+1)*C/groups) at all of its pixels (groups = 1: layer norm over an image, groups = C: instance norm).
  * `groups` divides C; any C up to 65536, any alignment that the storage type has (multiples of 8 channels on 16-byte aligned tensors are
  * fastest).  gamma, beta, dgamma, dbeta [C], stats [2][N][groups] (mean, then 1/sqrt(var + eps), biased variance) are fp32.
- * `scratch`: fdg_gn_scratch_bytes bytes of device memory, 256-byte aligned, any contents; it serves both calls, and is not
- * to be shared by calls that may run at the same time.  The result of a call does not depend on scheduling.  No output
+ * `scratch`: fdg_gn_scratch_bytes bytes of device memory for that pass (0 for a forward pass that needs none: scratch may then
+ * be NULL), 256-byte aligned, any contents; not to be shared by calls that may run at the same time.  The result of a call does not depend on scheduling.  No output
  * overlaps an input or another output.  Errors: FDG_ERR_INVALID_ARG (null pointer, bad shape, precision or activation, a
  * combination named below), FDG_ERR_WORKSPACE_TOO_SMALL, FDG_ERR_CUDA; nothing is launched after the first two. */
 typedef struct {
@@ -195,7 +195,7 @@ typedef struct {
   int groups;
 } fdg_gn_shape;
 enum { FDG_ACT_NONE = 0, FDG_ACT_RELU = 1, FDG_ACT_SILU = 2 };       /* z, max(z, 0), z/(1 + exp(-z)) */
-fdg_status fdg_gn_scratch_bytes(int precision, const fdg_gn_shape* shape, size_t* bytes);
+fdg_status fdg_gn_scratch_bytes(int precision, const fdg_gn_shape* shape, int backward, size_t* bytes);
 /* y = act(gamma*(x - mean)*rstd + beta [+ res]), and the statistics.  Optional outputs:
  *   gate            [N][HW][ceil(C/8)] bytes, FDG_ACT_RELU only: bit i of byte j = [y > 0] at channel 8j + i (unused bits 0)
  *   codes, scales   x held in 8 bits (both or neither), formed in the same pass over x where blocks fall on whole columns

@@ -162,7 +162,7 @@ def load_library(path=LIB_PATH):
                             C.c_int, C.c_int, vp, sz, vp],
         "fdg_ckpt_encode": [C.c_int, vp, sz, C.c_int, vp, vp, vp],
         "fdg_ckpt_decode": [C.c_int, vp, vp, sz, C.c_int, vp, vp],
-        "fdg_gn_scratch_bytes": [C.c_int, P(fdg_gn_shape), P(sz)],
+        "fdg_gn_scratch_bytes": [C.c_int, P(fdg_gn_shape), C.c_int, P(sz)],
         "fdg_gn_forward": [C.c_int, P(fdg_gn_shape), vp, vp, vp, vp, C.c_int, C.c_float, vp, vp, vp, vp, vp, vp, sz, vp],
         "fdg_gn_backward": [C.c_int, P(fdg_gn_shape), vp, vp, vp, vp, vp, vp, vp, C.c_int, vp, vp, vp, vp, vp, vp, vp, sz, vp],
         "fdg_shrink": [C.c_int, vp, vp, C.c_float, sz, vp],
@@ -555,7 +555,7 @@ class EwOps:
         self.lib = load_library()
         self.precision = precision
         self.dtype = torch.bfloat16 if precision == FDG_BF16_TC else torch.float32
-        self._gn_shapes = {}                     # (N, HW, C, groups) -> (fdg_gn_shape, scratch bytes)
+        self._gn_shapes = {}                     # (N, HW, C, groups, backward) -> (fdg_gn_shape by reference, scratch bytes)
 
     def _stream(self):
         return self.torch.cuda.current_stream().cuda_stream
@@ -610,103 +610,130 @@ class EwOps:
         return (dx, dg, db, dx2, dg2, db2) if second else (dx, dg, db)
 
     # -- group norm, and tensors held in 8 bits.  The library sees addresses only, so what it cannot check is checked here.
-    def _take(self, t, shape, dtype, what):
-        """The address of a contiguous tensor of the current device with this shape and type."""
-        if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device.index != self.torch.cuda.current_device():
-            raise FDGError(1, "%s: expected a contiguous %s tensor of shape %s on the current device, got %s %s on %s"
-                           % (what, dtype, tuple(shape), t.dtype, tuple(t.shape), t.device))
-        return t.data_ptr()
+    def _take(self, t, shape, dtype, what, dev):
+        """The address of a contiguous tensor of device `dev`, the current one, with this shape and type."""
+        if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev:
+            return t.data_ptr()
+        raise FDGError(1, "%s: expected a contiguous %s tensor of shape %s on the current device, got %s %s on %s"
+                       % (what, dtype, tuple(shape), t.dtype, tuple(t.shape), t.device))
 
-    def _gn(self, t, groups):
-        """(shape structure, scratch bytes) of a group norm of tensors like t [N, pixels.., C]."""
-        if t.dim() < 2:
-            raise FDGError(1, "group norm: expected [N, pixels.., C], got %s" % (tuple(t.shape),))
-        n, ch = t.shape[0], t.shape[-1]
-        key = (n, t.numel() // max(n * ch, 1), ch, groups)
+    def _here(self):
+        """(current device, its current stream)."""
+        dev = self.torch._C._cuda_getDevice()
+        return dev, self.torch._C._cuda_getCurrentRawStream(dev)
+
+    def _gn(self, shape, groups, backward):
+        """(shape structure, scratch bytes) of a group norm of tensors [N, pixels.., C]."""
+        key = (shape, groups, backward)
         got = self._gn_shapes.get(key)
         if got is None:
-            s, need = fdg_gn_shape(*key), C.c_size_t()
-            self._chk(self.lib.fdg_gn_scratch_bytes(self.precision, C.byref(s), C.byref(need)))
+            if len(shape) < 2 or not isinstance(groups, int):
+                raise FDGError(1, "group norm: expected [N, pixels.., C] and a number of groups, got %s and %r" % (tuple(shape), groups))
+            hw = 1
+            for v in shape[1:-1]:
+                hw *= v
+            if max(shape[0], hw, shape[-1], groups) >= 2 ** 31:
+                raise FDGError(1, "group norm: %s is too large" % (tuple(shape),))
+            s, need = fdg_gn_shape(shape[0], hw, shape[-1], groups), C.c_size_t()
+            self._chk(self.lib.fdg_gn_scratch_bytes(self.precision, C.byref(s), backward, C.byref(need)))
             if len(self._gn_shapes) >= 4096:
                 self._gn_shapes.clear()
-            got = self._gn_shapes[key] = (s, need.value)
+            got = self._gn_shapes[key] = (C.byref(s), need.value)
         return got
 
-    @staticmethod
-    def _act(name):
-        if name not in ("none", "relu", "silu"):
-            raise FDGError(1, "activation %r: none, relu or silu" % (name,))
-        return {"none": FDG_ACT_NONE, "relu": FDG_ACT_RELU, "silu": FDG_ACT_SILU}[name]
+    _ACTS = {"none": FDG_ACT_NONE, "relu": FDG_ACT_RELU, "silu": FDG_ACT_SILU}
 
-    def _held_shapes(self, shape):
-        return shape, shape[:-1] + (-(-shape[-1] // FDG_CKPT_BLOCK),)
+    def _act(self, name):
+        if name not in self._ACTS:
+            raise FDGError(1, "activation %r: none, relu or silu" % (name,))
+        return self._ACTS[name]
+
+    @staticmethod
+    def _scale_shape(shape):
+        return shape[:-1] + (-(-shape[-1] // FDG_CKPT_BLOCK),)
+
+    def _empty_held(self, x):
+        torch = self.torch
+        return torch.empty_like(x, dtype=torch.int8), x.new_empty(self._scale_shape(x.shape), dtype=torch.uint8)
 
     def ckpt_encode(self, x):
         """(codes, scales): x [.., C] held in 8 bits."""
-        torch = self.torch
-        cs, ss = self._held_shapes(x.shape)
-        px = self._take(x, x.shape, self.dtype, "x")
-        codes = torch.empty(cs, dtype=torch.int8, device=x.device)
-        scales = torch.empty(ss, dtype=torch.uint8, device=x.device)
-        self._chk(self.lib.fdg_ckpt_encode(self.precision, px, x.numel() // max(cs[-1], 1), cs[-1], codes.data_ptr(), scales.data_ptr(),
-                                           self._stream()))
+        dev, stream = self._here()
+        px = self._take(x, x.shape, self.dtype, "x", dev)
+        codes, scales = self._empty_held(x)
+        ch = x.shape[-1]
+        rc = self.lib.fdg_ckpt_encode(self.precision, px, x.numel() // ch if ch else 0, ch, codes.data_ptr(), scales.data_ptr(), stream)
+        if rc:
+            self._chk(rc)
         return codes, scales
 
     def ckpt_decode(self, held):
         """The tensor that held = (codes, scales) stands for."""
         torch = self.torch
+        dev, stream = self._here()
         codes, scales = held
-        cs, ss = self._held_shapes(codes.shape)
-        pc, ps = self._take(codes, cs, torch.int8, "codes"), self._take(scales, ss, torch.uint8, "scales")
-        x = torch.empty(cs, dtype=self.dtype, device=codes.device)
-        self._chk(self.lib.fdg_ckpt_decode(self.precision, pc, ps, codes.numel() // max(cs[-1], 1), cs[-1], x.data_ptr(), self._stream()))
+        shape = codes.shape
+        pc = self._take(codes, shape, torch.int8, "codes", dev)
+        ps = self._take(scales, self._scale_shape(shape), torch.uint8, "scales", dev)
+        x = torch.empty_like(codes, dtype=self.dtype)
+        ch = shape[-1]
+        rc = self.lib.fdg_ckpt_decode(self.precision, pc, ps, codes.numel() // ch if ch else 0, ch, x.data_ptr(), stream)
+        if rc:
+            self._chk(rc)
         return x
 
     def gn_forward(self, x, groups, gamma, beta, act="none", res=None, eps=1e-5, gate=False, checkpoint=False):
         """y = act(group norm of x [N, pixels.., C] [+ res]).  Returns (y, stats [2, N, groups], gate, (codes, scales)); the last
         two are None unless asked for: the bits of [y > 0] (relu only), and x held in 8 bits, for gn_backward."""
         torch = self.torch
-        s, need = self._gn(x, groups)
-        vec = (s.C,)
-        args = [self._take(x, x.shape, self.dtype, "x"), self._take(gamma, vec, torch.float32, "gamma"),
-                self._take(beta, vec, torch.float32, "beta"), None if res is None else self._take(res, x.shape, self.dtype, "res")]
+        dev, stream = self._here()
+        shape = x.shape
+        s, need = self._gn(shape, groups, 0)
+        vec, f32 = shape[-1:], torch.float32
+        px, pg, pb = self._take(x, shape, self.dtype, "x", dev), self._take(gamma, vec, f32, "gamma", dev), self._take(beta, vec, f32, "beta", dev)
+        pr = None if res is None else self._take(res, shape, self.dtype, "res", dev)
         y = torch.empty_like(x)
-        stats = torch.empty((2, s.N, groups), dtype=torch.float32, device=x.device)
-        bits = torch.empty(x.shape[:-1] + ((s.C + 7) // 8,), dtype=torch.uint8, device=x.device) if gate else None
-        held = None
-        if checkpoint:
-            cs, ss = self._held_shapes(x.shape)
-            held = torch.empty(cs, dtype=torch.int8, device=x.device), torch.empty(ss, dtype=torch.uint8, device=x.device)
-        sc = torch.empty(need, dtype=torch.uint8, device=x.device)
-        self._chk(self.lib.fdg_gn_forward(self.precision, C.byref(s), *args, self._act(act), eps, y.data_ptr(), stats.data_ptr(),
-                                          _ptr(bits), *((None, None) if held is None else (held[0].data_ptr(), held[1].data_ptr())),
-                                          sc.data_ptr(), need, self._stream()))
+        stats = x.new_empty((2, shape[0], groups), dtype=f32)
+        bits = x.new_empty(shape[:-1] + ((shape[-1] + 7) // 8,), dtype=torch.uint8) if gate else None
+        held = self._empty_held(x) if checkpoint else None
+        sc = x.new_empty(need, dtype=torch.uint8) if need else None
+        rc = self.lib.fdg_gn_forward(self.precision, s, px, pg, pb, pr, self._act(act), eps, y.data_ptr(), stats.data_ptr(), _ptr(bits),
+                                     None if held is None else held[0].data_ptr(), None if held is None else held[1].data_ptr(),
+                                     _ptr(sc), need, stream)
+        if rc:
+            self._chk(rc)
         return y, stats, bits, held
 
     def gn_backward(self, dy, x, stats, groups, gamma, beta=None, act="none", mask=None, gate=None, res=None):
         """(dx, dgamma, dbeta).  `x`: the input of gn_forward, or (codes, scales) as it left them; relu: `mask` = y or `gate` = its
         bits; silu: `beta`; `res` is added to dx."""
         torch = self.torch
-        s, need = self._gn(dy, groups)
-        vec = (s.C,)
-        pdy = self._take(dy, dy.shape, self.dtype, "dy")
+        dev, stream = self._here()
+        shape = dy.shape
+        s, need = self._gn(shape, groups, 1)
+        vec, f32 = shape[-1:], torch.float32
+        pdy = self._take(dy, shape, self.dtype, "dy", dev)
+        px = pc = ps = None
         if isinstance(x, (tuple, list)):
-            cs, ss = self._held_shapes(dy.shape)
-            px, pc, ps = None, self._take(x[0], cs, torch.int8, "codes"), self._take(x[1], ss, torch.uint8, "scales")
+            pc = self._take(x[0], shape, torch.int8, "codes", dev)
+            ps = self._take(x[1], self._scale_shape(shape), torch.uint8, "scales", dev)
         else:
-            px, pc, ps = self._take(x, dy.shape, self.dtype, "x"), None, None
-        args = [self._take(stats, (2, s.N, groups), torch.float32, "stats"), self._take(gamma, vec, torch.float32, "gamma"),
-                None if beta is None else self._take(beta, vec, torch.float32, "beta")]
-        masks = [None if mask is None else self._take(mask, dy.shape, self.dtype, "mask"),
-                 None if gate is None else self._take(gate, dy.shape[:-1] + ((s.C + 7) // 8,), torch.uint8, "gate"),
-                 None if res is None else self._take(res, dy.shape, self.dtype, "res")]
+            px = self._take(x, shape, self.dtype, "x", dev)
+        pst, pg = self._take(stats, (2, shape[0], groups), f32, "stats", dev), self._take(gamma, vec, f32, "gamma", dev)
+        pb = None if beta is None else self._take(beta, vec, f32, "beta", dev)
+        pm = None if mask is None else self._take(mask, shape, self.dtype, "mask", dev)
+        pgate = None if gate is None else self._take(gate, shape[:-1] + ((shape[-1] + 7) // 8,), torch.uint8, "gate", dev)
+        pr = None if res is None else self._take(res, shape, self.dtype, "res", dev)
         dx = torch.empty_like(dy)
-        dparam = torch.empty((2, s.C), dtype=torch.float32, device=dy.device)
+        dparam = dy.new_empty((2, shape[-1]), dtype=f32)
+        sc = dy.new_empty(need, dtype=torch.uint8)
         dg = dparam.data_ptr()
-        sc = torch.empty(need, dtype=torch.uint8, device=dy.device)
-        self._chk(self.lib.fdg_gn_backward(self.precision, C.byref(s), pdy, px, pc, ps, *args, self._act(act), *masks, dx.data_ptr(),
-                                           dg, dg + 4 * s.C, sc.data_ptr(), need, self._stream()))
-        return dx, dparam[0], dparam[1]
+        rc = self.lib.fdg_gn_backward(self.precision, s, pdy, px, pc, ps, pst, pg, pb, self._act(act), pm, pgate, pr, dx.data_ptr(), dg,
+                                      dg + 4 * shape[-1], sc.data_ptr(), need, stream)
+        if rc:
+            self._chk(rc)
+        dgamma, dbeta = dparam.unbind()
+        return dx, dgamma, dbeta
 
     def shrink(self, x, beta):
         out = self.torch.empty_like(x)

@@ -11,38 +11,30 @@ static bool precision_ok(int precision) { return precision == FDG_FP32_CUDACORE 
 static unsigned elem_bytes(int precision) { return precision == FDG_BF16_TC ? 2 : 4; }
 static fdg_status status_of(cudaError_t e) { return e == cudaSuccess ? FDG_OK : FDG_ERR_CUDA; }
 
-// rows * C values whose bytes can be counted, and grids that can be given.
-static bool rows_ok(size_t rows, int C) { return C >= 1 && rows >= 1 && rows <= ((size_t)1 << 40) / (size_t)C; }
+// rows * C values whose bytes can be counted, and whose share of a CTA can be in 32 bits.
+static bool rows_ok(size_t rows, int C) { return C >= 1 && rows >= 1 && rows <= ((size_t)1 << 38) / (size_t)C; }
 static bool gn_shape_ok(int precision, const fdg_gn_shape* s) {
-  if (!s || !precision_ok(precision) || s->N < 1 || s->HW < 1 || s->C < 1 || s->groups < 1 || s->C % s->groups) return false;
-  if (s->C > 1 << 16 || !rows_ok((size_t)s->N * (size_t)s->HW, s->C)) return false;
-  const int b = (int)elem_bytes(precision);
-  return gn::grid_ok(gn::plan_forward(b, s->N, s->HW, s->C, s->groups)) && gn::grid_ok(gn::plan_backward(b, s->N, s->HW, s->C, s->groups, false)) &&
-         gn::grid_ok(gn::plan_backward(b, s->N, s->HW, s->C, s->groups, true));
+  return s && precision_ok(precision) && s->N >= 1 && s->HW >= 1 && s->C >= 1 && s->groups >= 1 && s->C % s->groups == 0 &&
+         s->C <= 1 << 16 && rows_ok((size_t)s->N * (size_t)s->HW, s->C);
 }
 static size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Scratch: the backward pass's per-image totals [N][2][C], then the streamed forms' rows of sums.
+// Scratch: the forward pass's rows of sums; the backward pass's per-image totals [N][2][C] and then its rows of sums.
+static size_t forward_need(const gn::Plan& pl) { return align256(gn::partial_floats(pl) * sizeof(float)); }
 static size_t totals_bytes(const fdg_gn_shape* s) { return align256((size_t)s->N * 2 * s->C * sizeof(float)); }
-static size_t gn_scratch_need(int precision, const fdg_gn_shape* s) {
-  const int b = (int)elem_bytes(precision);
-  const size_t rows = std::max({gn::partial_floats(gn::plan_forward(b, s->N, s->HW, s->C, s->groups)),
-                                gn::partial_floats(gn::plan_backward(b, s->N, s->HW, s->C, s->groups, false)),
-                                gn::partial_floats(gn::plan_backward(b, s->N, s->HW, s->C, s->groups, true))});
-  return totals_bytes(s) + align256(rows * sizeof(float));
-}
+static size_t backward_need(const fdg_gn_shape* s, const gn::Plan& pl) { return totals_bytes(s) + align256(gn::partial_floats(pl) * sizeof(float)); }
 
 template <typename T>
-static cudaError_t gn_forward_as(const fdg_gn_shape* s, const void* x, const float* gamma, const float* beta, const void* res, int act, float eps,
+static cudaError_t gn_forward_as(const gn::Plan& pl, const void* x, const float* gamma, const float* beta, const void* res, int act, float eps,
                                  void* y, float* stats, uint8_t* gate, int8_t* codes, uint8_t* scales, void* scratch, cudaStream_t st) {
   gn::Forward<T> p{};
   p.x = (const T*)x; p.gamma = gamma; p.beta = beta; p.res = (const T*)res; p.y = (T*)y; p.stats = stats; p.gate = gate;
   p.codes = codes; p.scales = scales; p.eps = eps; p.act = act;
-  p.partial = reinterpret_cast<float*>(static_cast<char*>(scratch) + totals_bytes(s));
-  return gn::launch_forward<T>(st, gn::plan_forward(sizeof(T), s->N, s->HW, s->C, s->groups), p);
+  p.partial = static_cast<float*>(scratch);
+  return gn::launch_forward<T>(st, pl, p);
 }
 template <typename T>
-static cudaError_t gn_backward_as(const fdg_gn_shape* s, const void* dy, const void* x, const int8_t* codes, const uint8_t* scales,
+static cudaError_t gn_backward_as(const fdg_gn_shape* s, const gn::Plan& pl, const void* dy, const void* x, const int8_t* codes, const uint8_t* scales,
                                   const float* stats, const float* gamma, const float* beta, int act, const void* mask, const uint8_t* gate,
                                   const void* res, void* dx, float* dgamma, float* dbeta, void* scratch, cudaStream_t st) {
   gn::Backward<T> p{};
@@ -51,7 +43,7 @@ static cudaError_t gn_backward_as(const fdg_gn_shape* s, const void* dy, const v
   p.slope = act == FDG_ACT_SILU ? gn::SLOPE_SILU : mask ? gn::SLOPE_MASK : gate ? gn::SLOPE_BITS : gn::SLOPE_ONE;
   p.totals = static_cast<float*>(scratch);
   p.partial = reinterpret_cast<float*>(static_cast<char*>(scratch) + totals_bytes(s));
-  return gn::launch_backward<T>(st, gn::plan_backward(sizeof(T), s->N, s->HW, s->C, s->groups, codes != nullptr), p, dgamma, dbeta);
+  return gn::launch_backward<T>(st, pl, p, dgamma, dbeta);
 }
 }  // namespace fdg
 
@@ -73,9 +65,18 @@ fdg_status fdg_ckpt_decode(int precision, const int8_t* codes, const uint8_t* sc
                                             : launch_ckpt_decode<float>(st, codes, scales, rows, C, (float*)x));
 }
 
-fdg_status fdg_gn_scratch_bytes(int precision, const fdg_gn_shape* s, size_t* bytes) {
+fdg_status fdg_gn_scratch_bytes(int precision, const fdg_gn_shape* s, int backward, size_t* bytes) {
   if (!bytes || !gn_shape_ok(precision, s)) return FDG_ERR_INVALID_ARG;
-  *bytes = gn_scratch_need(precision, s);
+  const int b = (int)elem_bytes(precision);
+  if (!backward) {
+    const gn::Plan pl = gn::plan_forward(b, s->N, s->HW, s->C, s->groups);
+    if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
+    *bytes = forward_need(pl);
+    return FDG_OK;
+  }
+  const gn::Plan of_x = gn::plan_backward(b, s->N, s->HW, s->C, s->groups, false), of_codes = gn::plan_backward(b, s->N, s->HW, s->C, s->groups, true);
+  if (!gn::grid_ok(of_x) || !gn::grid_ok(of_codes)) return FDG_ERR_INVALID_ARG;
+  *bytes = std::max(backward_need(s, of_x), backward_need(s, of_codes));
   return FDG_OK;
 }
 
@@ -87,10 +88,13 @@ fdg_status fdg_gn_forward(int precision, const fdg_gn_shape* s, const void* x, c
   if ((act == FDG_ACT_SILU && res) || (gate && act != FDG_ACT_RELU) || (codes != nullptr) != (scales != nullptr)) return FDG_ERR_INVALID_ARG;
   const unsigned b = elem_bytes(precision);
   if (!aligned_to(x, b) || !aligned_to(y, b) || !aligned_to(res, b) || !aligned_to(scratch, 256)) return FDG_ERR_INVALID_ARG;
-  if (!scratch || scratch_bytes < gn_scratch_need(precision, s)) return FDG_ERR_WORKSPACE_TOO_SMALL;
+  const gn::Plan pl = gn::plan_forward((int)b, s->N, s->HW, s->C, s->groups);
+  if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
+  const size_t need = forward_need(pl);
+  if (need > 0 && (!scratch || scratch_bytes < need)) return FDG_ERR_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return status_of(precision == FDG_BF16_TC ? gn_forward_as<bf16>(s, x, gamma, beta, res, act, eps, y, stats, gate, codes, scales, scratch, st)
-                                            : gn_forward_as<float>(s, x, gamma, beta, res, act, eps, y, stats, gate, codes, scales, scratch, st));
+  return status_of(precision == FDG_BF16_TC ? gn_forward_as<bf16>(pl, x, gamma, beta, res, act, eps, y, stats, gate, codes, scales, scratch, st)
+                                            : gn_forward_as<float>(pl, x, gamma, beta, res, act, eps, y, stats, gate, codes, scales, scratch, st));
 }
 
 fdg_status fdg_gn_backward(int precision, const fdg_gn_shape* s, const void* dy, const void* x, const int8_t* codes, const uint8_t* scales,
@@ -103,11 +107,13 @@ fdg_status fdg_gn_backward(int precision, const fdg_gn_shape* s, const void* dy,
   const unsigned b = elem_bytes(precision);
   if (!aligned_to(dy, b) || !aligned_to(x, b) || !aligned_to(mask, b) || !aligned_to(res, b) || !aligned_to(dx, b) || !aligned_to(scratch, 256))
     return FDG_ERR_INVALID_ARG;
-  if (!scratch || scratch_bytes < gn_scratch_need(precision, s)) return FDG_ERR_WORKSPACE_TOO_SMALL;
+  const gn::Plan pl = gn::plan_backward((int)b, s->N, s->HW, s->C, s->groups, codes != nullptr);
+  if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
+  if (!scratch || scratch_bytes < backward_need(s, pl)) return FDG_ERR_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return status_of(precision == FDG_BF16_TC
-                       ? gn_backward_as<bf16>(s, dy, x, codes, scales, stats, gamma, beta, act, mask, gate, res, dx, dgamma, dbeta, scratch, st)
-                       : gn_backward_as<float>(s, dy, x, codes, scales, stats, gamma, beta, act, mask, gate, res, dx, dgamma, dbeta, scratch, st));
+                       ? gn_backward_as<bf16>(s, pl, dy, x, codes, scales, stats, gamma, beta, act, mask, gate, res, dx, dgamma, dbeta, scratch, st)
+                       : gn_backward_as<float>(s, pl, dy, x, codes, scales, stats, gamma, beta, act, mask, gate, res, dx, dgamma, dbeta, scratch, st));
 }
 
 }  // extern "C"

@@ -261,10 +261,11 @@ def test_nothing_is_written_past_the_outputs(prec_name, shape):
     n, p, c, groups = shape
     lib, prec = ew.lib, ew.precision
     b = 2 if prec_name == "bf16" else 4
-    need, s = C.c_size_t(), B.fdg_gn_shape(n, p, c, groups)
-    assert lib.fdg_gn_scratch_bytes(prec, C.byref(s), C.byref(need)) == 0
+    need, back, s = C.c_size_t(), C.c_size_t(), B.fdg_gn_shape(n, p, c, groups)
+    assert lib.fdg_gn_scratch_bytes(prec, C.byref(s), 0, C.byref(need)) == 0
+    assert lib.fdg_gn_scratch_bytes(prec, C.byref(s), 1, C.byref(back)) == 0
     sizes = dict(y=n * p * c * b, stats=2 * n * groups * 4, gate=n * p * -(-c // 8), codes=n * p * c, scales=n * p * -(-c // 32),
-                 scratch=need.value, dx=n * p * c * b, dgamma=4 * c, dbeta=4 * c)
+                 scratch=need.value, scratch_b=back.value, dx=n * p * c * b, dgamma=4 * c, dbeta=4 * c)
     pad = 512
     bufs = {k: torch.full((v + 2 * pad,), 0x5A, dtype=torch.uint8, device="cuda") for k, v in sizes.items()}
     at = {k: v.data_ptr() + pad for k, v in bufs.items()}
@@ -277,7 +278,7 @@ def test_nothing_is_written_past_the_outputs(prec_name, shape):
         assert lib.fdg_gn_backward(prec, C.byref(s), dy.data_ptr(), None if held else x.data_ptr(), at["codes"] if held else None,
                                    at["scales"] if held else None, at["stats"], gamma.data_ptr(), beta.data_ptr(), B.FDG_ACT_RELU,
                                    None if held else at["y"], at["gate"] if held else None, None, at["dx"], at["dgamma"], at["dbeta"],
-                                   at["scratch"], need.value, st) == 0
+                                   at["scratch_b"], back.value, st) == 0
     torch.cuda.synchronize()
     for k, v in bufs.items():
         assert (v[:pad] == 0x5A).all() and (v[pad + sizes[k]:] == 0x5A).all(), k

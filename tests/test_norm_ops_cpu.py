@@ -17,9 +17,9 @@ def lib():
     return B.load_library()
 
 
-def _scratch(lib, prec, *shape):
+def _scratch(lib, prec, *shape, backward=1):
     n, s = C.c_size_t(), B.fdg_gn_shape(*shape)
-    rc = lib.fdg_gn_scratch_bytes(prec, C.byref(s), C.byref(n))
+    rc = lib.fdg_gn_scratch_bytes(prec, C.byref(s), backward, C.byref(n))
     return rc, n.value
 
 
@@ -27,20 +27,22 @@ def _scratch(lib, prec, *shape):
 def test_scratch(lib, prec):
     rc, small = _scratch(lib, prec, 8, 256, 8, 4)
     assert rc == 0 and 8 * 2 * 8 * 4 <= small <= 8192            # totals of the backward pass only: images fit a cluster
-    rc, large = _scratch(lib, prec, 8, 65536, 128, 32)
-    assert rc == 0 and large < 8 * 65536 * 128 * 2 // 20          # sums of chunks: a small part of the tensor
+    assert _scratch(lib, prec, 8, 256, 8, 4, backward=0) == (0, 0)
+    for backward in (0, 1):
+        rc, large = _scratch(lib, prec, 8, 65536, 128, 32, backward=backward)
+        assert rc == 0 and 0 < large < 8 * 65536 * 128 * 2 // 20      # sums of chunks: a small part of the tensor
     for bad in ((0, 4, 8, 4), (4, 0, 8, 4), (4, 4, 0, 1), (4, 4, 8, 0), (4, 4, 8, 3), (4, 4, 8, 16), (-1, 4, 8, 4),
-                (2 ** 31 - 1, 2 ** 31 - 1, 1024, 4), (1, 1, 2 ** 25, 1)):
-        assert _scratch(lib, prec, *bad)[0] == INVALID, bad
+                (2 ** 31 - 1, 2 ** 31 - 1, 1024, 4), (1, 1, 2 ** 16 + 1, 1), (2 ** 20, 2 ** 19, 1, 1)):
+        assert _scratch(lib, prec, *bad)[0] == INVALID and _scratch(lib, prec, *bad, backward=0)[0] == INVALID, bad
     assert _scratch(lib, 7, 8, 256, 8, 4)[0] == INVALID
     s = B.fdg_gn_shape(8, 256, 8, 4)
-    assert lib.fdg_gn_scratch_bytes(prec, None, C.byref(C.c_size_t())) == INVALID
-    assert lib.fdg_gn_scratch_bytes(prec, C.byref(s), None) == INVALID
+    assert lib.fdg_gn_scratch_bytes(prec, None, 1, C.byref(C.c_size_t())) == INVALID
+    assert lib.fdg_gn_scratch_bytes(prec, C.byref(s), 1, None) == INVALID
 
 
 def test_gn_forward_refusals(lib):
-    s = B.fdg_gn_shape(8, 256, 8, 4)
-    need = _scratch(lib, B.FDG_BF16_TC, 8, 256, 8, 4)[1]
+    s = B.fdg_gn_shape(8, 65536, 128, 4)                       # large enough to need scratch
+    need = _scratch(lib, B.FDG_BF16_TC, 8, 65536, 128, 4, backward=0)[1]
     good = dict(precision=B.FDG_BF16_TC, shape=C.byref(s), x=P, gamma=P, beta=P, res=None, act=B.FDG_ACT_RELU, eps=1e-5, y=P, stats=P,
                 gate=None, codes=None, scales=None, scratch=P, bytes=need, stream=None)
 
