@@ -729,6 +729,8 @@ template <typename T> struct Backward {
   T* dx;
   float* partial;             // streamed: [N][parts][2][C]: A, B of each CTA
   float* totals;              // [N][2][C]: A, B of each image; streamed: null if the second pass adds up the rows itself
+  float* dgamma;
+  float* dbeta;
   int slope;
 };
 
@@ -841,8 +843,8 @@ template <typename T, bool VEC, bool CK> struct Feed {
   const T* res;
   int left, slope, n;
   bool reverse;
-  uint32_t scale[3][kBatch], open[3][kBatch];     // of this turn, the next, and the one after
-  uint32_t next, step;                            // element offset of the next vector to be copied
+  uint32_t scale[kAhead + 1][kBatch], open[kAhead + 1][kBatch];     // by turn, as the ring
+  uint32_t next, next_scale, next_gate, step, scale_step, gate_step;       // offsets of the next vector and bytes to be fetched
   static constexpr int kVec = kRing * Slots<T>::Q * kThreads;        // 16-byte words of a ring
   // words of shared memory of a pass, in 16 bytes
   static __host__ __device__ __forceinline__ int words(bool mask, bool res) {
@@ -853,15 +855,20 @@ template <typename T, bool VEC, bool CK> struct Feed {
         ress(smem + words(slope_ == SLOPE_MASK, false)), codes(reinterpret_cast<uint2*>(smem + kVec) + threadIdx.x),
         res(res_ ? res_ + (sh.row0 + at.r) * p.g.C + at.c0 : nullptr), left(at.left), slope(slope_), n(sh.mine), reverse(reverse_) {
     step = reverse ? 0u - from.step : from.step;
-    next = reverse && n > 0 ? (uint32_t)(n - 1) * from.step : 0u;
+    scale_step = reverse ? 0u - from.scale_step : from.scale_step;
+    gate_step = reverse ? 0u - from.gate_step : from.gate_step;
+    const uint32_t first = reverse && n > 0 ? (uint32_t)(n - 1) : 0u;
+    next = first * from.step; next_scale = first * from.scale_step; next_gate = first * from.gate_step;
   }
   __device__ __forceinline__ uint32_t at(int k) const { return (uint32_t)(reverse ? n - 1 - k : k); }
-  __device__ __forceinline__ void bytes(int k, int to) {
+  // The bytes of the turn that begins with vector k, to be used two turns later.
+  __device__ __forceinline__ void bytes(int k, int slot) {
+    const int to = slot / kBatch % (kAhead + 1);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (k + u < n) {
-        if constexpr (CK) scale[to][u] = from.scales[at(k + u) * from.scale_step];
-        if (slope == SLOPE_BITS) open[to][u] = from.gate[at(k + u) * from.gate_step];
+        if constexpr (CK) { scale[to][u] = from.scales[next_scale]; next_scale += scale_step; }
+        if (slope == SLOPE_BITS) { open[to][u] = from.gate[next_gate]; next_gate += gate_step; }
       }
   }
   __device__ __forceinline__ void issue(int s) {
@@ -876,22 +883,13 @@ template <typename T, bool VEC, bool CK> struct Feed {
     if (slope == SLOPE_MASK) masks.template fetch<VEC>(s, from.mask + o, left);
     if (res) ress.template fetch<VEC>(s, res + o, left);
   }
-  // At the start of turn k: moves the bytes on.
-  __device__ __forceinline__ void turn(int k) {
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      scale[0][u] = scale[1][u]; scale[1][u] = scale[2][u];
-      open[0][u] = open[1][u]; open[1][u] = open[2][u];
-    }
-    bytes(k + 2 * kBatch, 2);
-  }
   __device__ __forceinline__ Held<T, CK> get(int slot, int u) const {
     Held<T, CK> h;
     const int s = slot + u;
     h.dy = dys.get(s);
-    if constexpr (CK) { h.codes = codes[s * kThreads]; h.scale = scale[0][u]; } else { h.x = xs.get(s); }
+    if constexpr (CK) { h.codes = codes[s * kThreads]; h.scale = scale[slot / kBatch][u]; } else { h.x = xs.get(s); }
     if (slope == SLOPE_MASK) h.mask = masks.get(s);
-    if (slope == SLOPE_BITS) h.open = open[0][u];
+    if (slope == SLOPE_BITS) h.open = open[slot / kBatch][u];
     return h;
   }
 };
@@ -959,7 +957,8 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
   uint2* cs = reinterpret_cast<uint2*>(xs);
   float* red = reinterpret_cast<float*>(CK ? reinterpret_cast<uint4*>(cs + vecs) : xs + vecs * Slots<T>::Q);   // [2][2048]
   float* chan = red + 2 * kThreads * 8;       // [2][C]
-  float* own = chan + 2 * g.C;                // [2][G]
+  float* gamma = chan + 2 * g.C;              // [C]
+  float* own = gamma + g.C;                   // [2][G]
   float* coef = own + 2 * g.G;                // [2][G]
   uint8_t* open = reinterpret_cast<uint8_t*>(coef + 2 * g.G);
   uint8_t* scale_bytes = open + vecs;
@@ -1009,6 +1008,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
   float rstd[8];
   load_channels(p, at, n, slope, ch, rstd);
   copies_done();
+  for (int c = tid; c < g.C; c += kThreads) gamma[c] = p.gamma[c];
   auto held = [&](uint32_t k) {
     Held<T, CK> h;
     h.dy = dys.get(k);
@@ -1036,7 +1036,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
   __syncthreads();
   channel_sums(red, g, g.C, g.lanes_c, [&](int c, float a, float b) { chan[c] = a; chan[g.C + c] = b; });
   __syncthreads();
-  group_sums(g.G, g.Cg, g.lanes_g, [&](int c) { const float w = p.gamma[c]; return make_float2(w * chan[g.C + c], w * chan[c]); },
+  group_sums(g.G, g.Cg, g.lanes_g, [&](int c) { const float w = gamma[c]; return make_float2(w * chan[g.C + c], w * chan[c]); },
              [&](int s, float s1, float s2) { own[s] = s1; own[g.G + s] = s2; });
   cg::cluster_group cluster = cg::this_cluster();
   cluster.sync();
@@ -1092,8 +1092,8 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
   grid_dependency_wait();
   grid_dependency_release();
   Feed<T, VEC, CK> feed(p, at, sh, slope, nullptr, false, smem);
-  feed.bytes(0, 1);
-  feed.bytes(kBatch, 2);
+  feed.bytes(0, 0);
+  feed.bytes(kBatch, kBatch);
   Channels ch;
   float rstd[8];
   Sums sums;
@@ -1101,7 +1101,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
   Stream<kBatch>::start(sh.mine, issue);
   load_channels(p, at, n, slope, ch, rstd);
   Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot) {
-    feed.turn(k);
+    feed.bytes(k + 2 * kBatch, slot + 2 * kBatch);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (k + u < sh.mine) {
@@ -1120,34 +1120,39 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
   channel_sums(red, g, sets, g.lanes_c, [&](int c, float a, float b) { out[c] = a; out[g.C + c] = b; });
 }
 
-// out[j][i] = the sum of `rows` rows of `width` floats from in[j * rows] on, j = blockIdx.x / blocks; a block takes 32 of
-// the width, its warps every 32nd row, and adds in fp64.  Streamed, between the passes where an image has many rows, and, for
-// all forms, the parameter gradients (`split` > 0: values from there on go to out2).
+// Sums of `rows` rows of `width` floats, 32 of the width from `first` on: done(i, sum).  The CTA's warps take every `warps`-th
+// row and add in fp64; fin: [warps][33].
+template <typename Done>
+__device__ __forceinline__ void add_rows(const float* __restrict__ in, int rows, int width, int first, double (*fin)[33], Done done) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int i = first + lane;
+  double t = 0.0;
+  if (i < width)
+#pragma unroll 8
+    for (int r = warp; r < rows; r += warps) t += (double)in[(size_t)r * width + i];
+  fin[warp][lane] = t;
+  __syncthreads();
+  if (warp == 0 && i < width) {
+    for (int w = 1; w < warps; ++w) t += fin[w][lane];
+    done(i, (float)t);
+  }
+  __syncthreads();
+}
+// out[j][i] = the sum of `rows` rows of `width` floats from in[j * rows] on, j = blockIdx.x / blocks.  Streamed, between the passes
+// where an image has many rows; resident, the parameter gradients (`split` > 0: values from there on go to out2).
 __global__ void __launch_bounds__(1024) add_rows_kernel(const float* __restrict__ in, int rows, int width, float* __restrict__ out,
                                                         float* __restrict__ out2, int split) {
   __shared__ double fin[32][33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int blocks = (width + 31) / 32, j = blockIdx.x / blocks, first = (blockIdx.x - j * blocks) * 32;
-  const int i = first + lane;
-  in += (size_t)j * rows * width;
-  out += (size_t)j * width;
+  const int blocks = (width + 31) / 32, j = blockIdx.x / blocks;
   grid_dependency_wait();
   grid_dependency_release();
-  double t = 0.0;
-  if (i < width)
-#pragma unroll 4
-    for (int r = warp; r < rows; r += 32) t += (double)in[(size_t)r * width + i];
-  fin[warp][lane] = t;
-  __syncthreads();
-  const int ii = first + warp;
-  t = fin[lane][warp];
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-  if (lane != 0 || ii >= width) return;
-  if (split > 0 && ii >= split) out2[ii - split] = (float)t; else out[ii] = (float)t;
+  add_rows(in + (size_t)j * rows * width, rows, width, (blockIdx.x - j * blocks) * 32, fin, [&](int i, float v) {
+    if (split > 0 && i >= split) out2[i - split] = v; else out[(size_t)j * width + i] = v;
+  });
 }
 
 // Streamed, second pass: dx.  Every CTA forms S1 and S2 of its tile's groups from the image's totals, or from its rows of sums.
+// The CTAs behind the last share of an image (blockIdx.y = parts) add up the parameter gradients.
 template <typename T, bool VEC, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __grid_constant__ Backward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
@@ -1157,6 +1162,14 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   const int slope = SLOPE < 0 ? p.slope : SLOPE;
   const int part = blockIdx.y, n = blockIdx.x;
   const int c_first = blockIdx.z * kMaxCols * 8;
+  if (part == g.parts) {
+    grid_dependency_wait();
+    if (blockIdx.z == 0)
+      for (int first = n * 32; first < 2 * g.C; first += g.N * 32)
+        add_rows(p.partial, g.N * g.parts, 2 * g.C, first, reinterpret_cast<double(*)[33]>(smem),
+                 [&](int i, float v) { (i < g.C ? p.dgamma + i : p.dbeta + (i - g.C))[0] = v; });
+    return;
+  }
   Place at(g, blockIdx.z);
   at.active = at.active && at.left > 0;
   if (at.left <= 0) { at.c0 = c_first; at.left = 1; }
@@ -1169,39 +1182,49 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   grid_dependency_release();
   auto issue = [&](int slot) { feed.issue(slot); };
   if constexpr (!VEC) Stream<kBatch>::start(sh.mine, issue);
-  feed.bytes(0, 1);
-  feed.bytes(kBatch, 2);
+  feed.bytes(0, 0);
+  feed.bytes(kBatch, kBatch);
   Channels ch;
   float rstd[8];
   load_channels(p, at, n, slope, ch, rstd);
   const int rows = p.totals ? 1 : g.parts;
   const float* src = p.totals ? p.totals + (size_t)n * 2 * g.C : p.partial + (size_t)n * g.parts * 2 * g.C;
   const float* rs = p.stats + (size_t)(g.N + n) * g.G + g_first;
-  group_sums(sets, g.Cg, g.lanes_g, [&](int c) {
-    c += c_base;
+  auto weighted = [&](int c) {
     float a = 0.f, b = 0.f;
 #pragma unroll 4
     for (int j = 0; j < rows; ++j) { a += src[(size_t)j * 2 * g.C + c]; b += src[(size_t)j * 2 * g.C + g.C + c]; }
     const float w = p.gamma[c];
     return make_float2(w * b, w * a);
-  }, [&](int s, float s1, float s2) {
+  };
+  auto done = [&](int s, float s1, float s2) {
     coef[s] = rs[s] * s1 * g.inv_m;
     coef[sets + s] = rs[s] * rs[s] * s2 * g.inv_m;
-  });
+  };
+  if (g.tiles == 1) {
+    float2* chan = reinterpret_cast<float2*>(coef + 2 * sets);                // [C]
+    for (int c = threadIdx.x; c < g.C; c += kThreads) chan[c] = weighted(c);
+    __syncthreads();
+    group_sums(sets, g.Cg, g.lanes_g, [&](int c) { return chan[c]; }, done);
+  } else {
+    group_sums(sets, g.Cg, g.lanes_g, [&](int c) { return weighted(c_base + c); }, done);
+  }
   __syncthreads();
   f32x2 k1[4], k2[4];
   load_coefficients(g, at, coef, coef + sets, g_first, k1, k2);
+  uint32_t o = feed.at(0) * feed.from.step;
   T* const dx = p.dx + (sh.row0 + at.r) * g.C + at.c0;
   Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot) {
-    feed.turn(k);
+    feed.bytes(k + 2 * kBatch, slot + 2 * kBatch);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (k + u < sh.mine) {
         const Held<T, CK> h = feed.get(slot, u);
         Raw8<T> r;
         if (feed.res) r = feed.ress.get(slot + u);
-        raw8_put<T, VEC>(dx + feed.at(k + u) * feed.from.step, at.left,
+        raw8_put<T, VEC>(dx + o, at.left,
                          dx_of<T, CK>(passed<T, CK>(h, slope), h, slope, ch, k1, k2, feed.res ? &r : nullptr));
+        o += feed.step;
       }
   });
 }
@@ -1217,8 +1240,8 @@ inline int pow2_up_to(int64_t most, int cap) {
   while (2 * v <= cap && 2 * (int64_t)v <= most) v *= 2;
   return v;
 }
-constexpr size_t kSmemMost = 220 * 1024;        // of 227 KB
-constexpr size_t kSmemShare = 110 * 1024;       // two CTAs on an SM: one's copies run beside another's arithmetic
+constexpr size_t kSmemMost = 220 * 1024;        // of 227 KB that a CTA can have
+constexpr size_t kSmemOfSm = 227 * 1024;
 
 // `vec_bytes`: shared memory per vector of 8 channels in the resident form; `fixed`: besides the vectors; `per_sm`: CTAs of the
 // streamed form on an SM.
@@ -1248,14 +1271,17 @@ inline Plan plan(int N, int P, int C, int G, size_t vec_bytes, size_t fixed, int
   };
   const char* f_ = getenv("GN_FORM");
   if (g.tiles == 1 && !(f_ && f_[0] == 's')) {
-    int parts = 1;
-    while (parts < kMaxCluster && split(parts) > kSmemShare) parts *= 2;
-    // few images: more SMs, while every thread keeps two pixels
-    while (parts < kMaxCluster && (int64_t)N * parts * 2 <= 2 * kSms && (split(parts), g.iters) >= 4) parts *= 2;
-    pl.smem = split(parts);
-    pl.resident = pl.smem <= kSmemMost && (int64_t)N * g.parts <= 2 * kSms;
-    shares();
-    if (pl.resident) return pl;
+    // as many CTAs per image as all run at once, while every thread keeps two pixels
+    for (int parts = kMaxCluster; parts >= 1; parts /= 2) {
+      pl.smem = split(parts);
+      if (parts > 1 && g.iters < 2) continue;
+      const int per = (int)std::min<size_t>(kSmemOfSm / (pl.smem + 1024), 2);
+      if (pl.smem <= kSmemMost && (int64_t)N * parts <= (int64_t)per * kSms) {
+        pl.resident = true;
+        shares();
+        return pl;
+      }
+    }
   }
   // one wave of CTAs, each with at least one batch of pixels in flight
   split((int)std::max<int64_t>(1, std::min<int64_t>((int64_t)per_sm * kSms / N, P / (4 * g.rp))));
@@ -1268,7 +1294,7 @@ inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G) {
 }
 inline Plan plan_backward(int elem_bytes, int N, int P, int C, int G, bool ckpt) {
   const size_t vec = 8 * (size_t)elem_bytes + (ckpt ? 8 : 8 * (size_t)elem_bytes) + 2;      // dy, x, a byte each for gate and scale
-  return plan(N, P, C, G, vec, 2 * kThreads * 8 * 4 + 8 * (size_t)C + 16 * (size_t)G, 2);
+  return plan(N, P, C, G, vec, 2 * kThreads * 8 * 4 + 12 * (size_t)C + 16 * (size_t)G, 2);
 }
 // Whether every launch's grid can be given.
 inline bool grid_ok(const Plan& pl) {
@@ -1340,51 +1366,53 @@ inline cudaError_t launch_forward(cudaStream_t st, const Plan& pl, Forward<T> p)
 }
 
 template <typename T, bool VEC, bool CK, int SLOPE>
-inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<T> p, float* dgamma, float* dbeta) {
+inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<T> p) {
   const Geom& g = pl.g;
   const int width = 2 * g.C, blocks = (width + 31) / 32;
-  cudaError_t e;
   if (pl.resident) {
     static OncePerDevice once;
-    e = once_per_device(&once, []() { return set_smem_limit(backward_kernel<T, VEC, CK, SLOPE>, kSmemMost); });
+    cudaError_t e = once_per_device(&once, []() { return set_smem_limit(backward_kernel<T, VEC, CK, SLOPE>, kSmemMost); });
     if (e == cudaSuccess) e = launch_cluster(backward_kernel<T, VEC, CK, SLOPE>, g.N, g.parts, pl.smem, st, p);
-  } else {
-    static OncePerDevice once;
-    e = once_per_device(&once, []() {
-      const cudaError_t f = set_smem_limit(backward_sums_kernel<T, VEC, CK, SLOPE>, kSmemMost);
-      return f != cudaSuccess ? f : set_smem_limit(backward_apply_kernel<T, VEC, CK, SLOPE>, kSmemMost);
-    });
-    const dim3 grid((unsigned)g.N, (unsigned)g.parts, (unsigned)g.tiles);
-    auto rings = [&](bool res) { return 16 * (size_t)Feed<T, VEC, CK>::words(p.slope == SLOPE_MASK, res); };
     if (e == cudaSuccess)
-      e = launch_chained(backward_sums_kernel<T, VEC, CK, SLOPE>, grid, dim3(kThreads), std::max(rings(false), (size_t)2 * kThreads * 8 * 4), st, p);
-    if (merges(g)) p.totals = nullptr;
-    else if (e == cudaSuccess)
-      e = launch_chained(add_rows_kernel, dim3((unsigned)(g.N * blocks)), dim3(1024), 0, st, (const float*)p.partial, g.parts, width, p.totals,
-                         (float*)nullptr, 0);
-    if (e == cudaSuccess) e = launch_chained(backward_apply_kernel<T, VEC, CK, SLOPE>, grid, dim3(kThreads), rings(p.res != nullptr) + 8 * (size_t)g.cols * 8, st, p);
+      e = launch_chained(add_rows_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, (const float*)p.totals, g.N, width, p.dgamma, p.dbeta, g.C);
+    return e;
   }
+  static OncePerDevice once;
+  cudaError_t e = once_per_device(&once, []() {
+    const cudaError_t f = set_smem_limit(backward_sums_kernel<T, VEC, CK, SLOPE>, kSmemMost);
+    return f != cudaSuccess ? f : set_smem_limit(backward_apply_kernel<T, VEC, CK, SLOPE>, kSmemMost);
+  });
+  auto rings = [&](bool res) { return 16 * (size_t)Feed<T, VEC, CK>::words(p.slope == SLOPE_MASK, res); };
   if (e == cudaSuccess)
-    e = launch_chained(add_rows_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, (const float*)(p.totals ? p.totals : p.partial),
-                       p.totals ? g.N : g.N * g.parts, width, dgamma, dbeta, g.C);
+    e = launch_chained(backward_sums_kernel<T, VEC, CK, SLOPE>, dim3((unsigned)g.N, (unsigned)g.parts, (unsigned)g.tiles), dim3(kThreads),
+                       std::max(rings(false), (size_t)2 * kThreads * 8 * 4), st, p);
+  if (merges(g)) p.totals = nullptr;
+  else if (e == cudaSuccess)
+    e = launch_chained(add_rows_kernel, dim3((unsigned)(g.N * blocks)), dim3(1024), 0, st, (const float*)p.partial, g.parts, width, p.totals,
+                       (float*)nullptr, 0);
+  // coefficients of the tile's groups; with one tile also the channels' sums
+  const size_t own = 8 * (size_t)std::min(g.G, g.cols * 8) + (g.tiles == 1 ? 8 * (size_t)g.C : 0);
+  if (e == cudaSuccess)
+    e = launch_chained(backward_apply_kernel<T, VEC, CK, SLOPE>, dim3((unsigned)g.N, (unsigned)g.parts + 1, (unsigned)g.tiles), dim3(kThreads),
+                       rings(p.res != nullptr) + own, st, p);
   return e;
 }
 template <typename T, bool CK>
-inline cudaError_t launch_backward_of(cudaStream_t st, const Plan& pl, const Backward<T>& p, bool vec, float* dgamma, float* dbeta) {
-  if (!vec) return launch_backward_as<T, false, CK, -1>(st, pl, p, dgamma, dbeta);
+inline cudaError_t launch_backward_of(cudaStream_t st, const Plan& pl, const Backward<T>& p, bool vec) {
+  if (!vec) return launch_backward_as<T, false, CK, -1>(st, pl, p);
   switch (p.slope) {
-    case SLOPE_MASK: return launch_backward_as<T, true, CK, SLOPE_MASK>(st, pl, p, dgamma, dbeta);
-    case SLOPE_BITS: return launch_backward_as<T, true, CK, SLOPE_BITS>(st, pl, p, dgamma, dbeta);
-    case SLOPE_SILU: return launch_backward_as<T, true, CK, SLOPE_SILU>(st, pl, p, dgamma, dbeta);
-    default: return launch_backward_as<T, true, CK, SLOPE_ONE>(st, pl, p, dgamma, dbeta);
+    case SLOPE_MASK: return launch_backward_as<T, true, CK, SLOPE_MASK>(st, pl, p);
+    case SLOPE_BITS: return launch_backward_as<T, true, CK, SLOPE_BITS>(st, pl, p);
+    case SLOPE_SILU: return launch_backward_as<T, true, CK, SLOPE_SILU>(st, pl, p);
+    default: return launch_backward_as<T, true, CK, SLOPE_ONE>(st, pl, p);
   }
 }
 template <typename T>
-inline cudaError_t launch_backward(cudaStream_t st, const Plan& pl, Backward<T> p, float* dgamma, float* dbeta) {
+inline cudaError_t launch_backward(cudaStream_t st, const Plan& pl, Backward<T> p) {
   p.g = pl.g;
   const bool vec = p.g.C % 8 == 0 && aligned_to(p.dy, 16) && aligned_to(p.x, 16) && aligned_to(p.codes, 8) && aligned_to(p.mask, 16) &&
                    aligned_to(p.res, 16) && aligned_to(p.dx, 16);
-  return p.codes ? launch_backward_of<T, true>(st, pl, p, vec, dgamma, dbeta) : launch_backward_of<T, false>(st, pl, p, vec, dgamma, dbeta);
+  return p.codes ? launch_backward_of<T, true>(st, pl, p, vec) : launch_backward_of<T, false>(st, pl, p, vec);
 }
 
 }  // namespace gn

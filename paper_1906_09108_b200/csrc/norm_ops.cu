@@ -43,7 +43,8 @@ static cudaError_t gn_backward_as(const fdg_gn_shape* s, const gn::Plan& pl, con
   p.slope = act == FDG_ACT_SILU ? gn::SLOPE_SILU : mask ? gn::SLOPE_MASK : gate ? gn::SLOPE_BITS : gn::SLOPE_ONE;
   p.totals = static_cast<float*>(scratch);
   p.partial = reinterpret_cast<float*>(static_cast<char*>(scratch) + totals_bytes(s));
-  return gn::launch_backward<T>(st, pl, p, dgamma, dbeta);
+  p.dgamma = dgamma; p.dbeta = dbeta;
+  return gn::launch_backward<T>(st, pl, p);
 }
 }  // namespace fdg
 
