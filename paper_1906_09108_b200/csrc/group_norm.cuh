@@ -113,12 +113,13 @@ template <typename T> struct Slots {
 
 // The streamed passes copy to shared memory ahead of what they use, every thread its own vectors, B of them to a commit group
 // (32 bytes) and kAhead groups under way: 96 to 128 bytes per thread are on their way at any time, which costs no registers and
-// needs no barrier.  start(mine, issue) begins; run() calls turn(k, slot) for k = 0, B, ... < n once vectors k .. k + B - 1 have
+// needs no barrier.  start(mine, issue) begins; run() calls turn(k, slot, full) for k = 0, B, ... < n once vectors k .. k + B - 1 have
 // come to slots slot .. slot + B - 1; issue(slot) starts the copy of the thread's next vector (of `mine`) into a slot.  The loop is
 // unrolled over the ring, so that slots are constants.
 constexpr int kAhead = 3;
 template <typename T> __host__ __device__ constexpr int batch_of() { return sizeof(T) == 2 ? 2 : 1; }
 template <typename T> __host__ __device__ constexpr int ring_of() { return batch_of<T>() * (kAhead + 1); }
+template <bool FULL> struct Full { static constexpr bool value = FULL; };      // whether every vector of a turn exists
 template <int B> struct Stream {
   static constexpr int R = B * (kAhead + 1);
   template <typename Issue> static __device__ __forceinline__ void start(int mine, Issue issue) {
@@ -129,17 +130,24 @@ template <int B> struct Stream {
     }
   }
   template <typename Issue, typename Turn> static __device__ __forceinline__ void run(int n, int mine, Issue issue, Turn turn) {
-    for (int k0 = 0; k0 < n; k0 += R) {
+    int k0 = 0;
+    // whole rounds of the ring ask nothing of a single vector
+    for (; k0 + R + B * kAhead <= mine; k0 += R) round<true>(k0, n, mine, issue, turn);
+    for (; k0 < n; k0 += R) round<false>(k0, n, mine, issue, turn);
+  }
+
+ private:
+  template <bool FULL, typename Issue, typename Turn>
+  static __device__ __forceinline__ void round(int k0, int n, int mine, Issue& issue, Turn& turn) {
 #pragma unroll
-      for (int b = 0; b < R; b += B) {
-        if (k0 + b < n) {
+    for (int b = 0; b < R; b += B) {
+      if (FULL || k0 + b < n) {
 #pragma unroll
-          for (int u = 0; u < B; ++u)
-            if (k0 + b + B * kAhead + u < mine) issue((b + B * kAhead + u) % R);
-          asm volatile("cp.async.commit_group;" ::: "memory");
-          asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
-          turn(k0 + b, b);
-        }
+        for (int u = 0; u < B; ++u)
+          if (FULL || k0 + b + B * kAhead + u < mine) issue((b + B * kAhead + u) % R);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+        turn(k0 + b, b, Full<FULL>());
       }
     }
   }
@@ -397,6 +405,7 @@ __device__ __forceinline__ uint32_t positive_bits(const Raw8<float>& y) {
 // y (and the gate's bits, and x in 8 bits) of a thread's pixels.  ACT < 0: p.act.  EXTRA 1: res and gate may be asked for; 2: and
 // codes.  Offsets inside a CTA's pixels fit 32 bits.
 enum { PLAIN = 0, WITH_RES_GATE = 1, WITH_CODES = 2 };
+constexpr int kPlainPerSm = 3, kCodesPerSm = 2;       // CTAs on an SM that the registers allow (80 spill where codes are formed)
 template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
   T* y;
   const T* res;
@@ -456,14 +465,14 @@ template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
   }
   // A turn of B pixels, raw, k counting from the thread's first pixel or (back) its last; for the whole warp where codes are
   // formed, since the lanes that share a block of 32 channels (they have the same pixels) exchange its maximum.
-  template <int B>
+  template <bool FULL, int B>
   __device__ __forceinline__ void turn(int k, int mine, bool back, uint32_t step, const Affine<T>& affine, const Raw8<T> (&raw)[B], const Raw8<T>* raw_res) const {
     uint32_t top[B];
     if constexpr (EXTRA == WITH_CODES)
       if (VEC || codes) block_tops<B>(raw, top);
 #pragma unroll
     for (int u = 0; u < B; ++u)
-      if (k + u < mine) {
+      if (FULL || k + u < mine) {
         const uint32_t kk = (uint32_t)(back ? mine - 1 - (k + u) : k + u), o = kk * step;
         const F8 x = raw8_to_f8(raw[u]);
         value(kk, o, affine, x, raw_res[EXTRA >= WITH_RES_GATE ? u : 0]);
@@ -503,7 +512,7 @@ __device__ __forceinline__ void load_affine(const Forward<T>& p, const Place& at
 
 // The resident form: blockIdx = image, share of its pixels, tile of columns: a cluster per image.
 template <typename T, bool VEC, int ACT, int EXTRA>
-__global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_constant__ Forward<T> p) {
+__global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : kPlainPerSm) forward_kernel(const __grid_constant__ Forward<T> p) {
   constexpr int kBatch = 2;
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
@@ -556,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_const
       if constexpr (EXTRA >= WITH_RES_GATE)
         if (out.res && k + u < sh.mine) rs[u] = raw8_load<T, VEC>(out.res + (uint32_t)(k + u) * step, at.left);
     }
-    out.turn(k, sh.mine, false, step, affine, xs, rs);
+    out.template turn<false>(k, sh.mine, false, step, affine, xs, rs);
   }
   cluster.barrier_wait(std::move(token));                                 // nor do they read its own
 }
@@ -586,12 +595,14 @@ __global__ void __launch_bounds__(kThreads, 3) moments_kernel(const __grid_const
     ring.template fetch<VEC>(slot, src, at.left);
     src += step;
   };
+  Raw8<T> first{};
+  if (sh.mine > 0) first = raw8_load<T, VEC>(src, at.left);
   Stream<kBatch>::start(sh.mine, issue);
-  Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot) {
-    if (k == 0) m.start(raw8_to_f8(ring.get(slot)));
+  m.start(raw8_to_f8(first));
+  Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot, auto full) {
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      if (k + u < sh.mine) m.add(raw8_to_f8(ring.get(slot + u)));
+      if (full.value || k + u < sh.mine) m.add(raw8_to_f8(ring.get(slot + u)));
   });
   const int c_first = blockIdx.z * kMaxCols * 8, sets = min(g.cols * 8, g.C - c_first);
   cta_moments(g, at, m, sh.mine, sh.count, sets, red, common, chan);
@@ -656,7 +667,7 @@ __global__ void __launch_bounds__(1024) combine_kernel(const __grid_constant__ F
 // Streamed, second pass: y from x and the statistics, which every CTA of an image forms from the rows of sums itself (the same
 // bits everywhere; its first CTA writes them out) unless combine_kernel has.
 template <typename T, bool VEC, int ACT, int EXTRA>
-__global__ void __launch_bounds__(kThreads, 3) apply_kernel(const __grid_constant__ Forward<T> p) {
+__global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : kPlainPerSm) apply_kernel(const __grid_constant__ Forward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
@@ -700,15 +711,15 @@ __global__ void __launch_bounds__(kThreads, 3) apply_kernel(const __grid_constan
     load_affine(p, at, gamma, beta, [&](int s) { return make_float2(p.stats[(size_t)n * g.G + s], p.stats[(size_t)(g.N + n) * g.G + s]); }, affine);
   else
     load_affine(p, at, gamma, beta, [&](int s) { return mom[s]; }, affine);
-  Stream<kBatch>::run(EXTRA == WITH_CODES ? sh.turns : sh.mine, sh.mine, issue, [&](int k, int slot) {
+  Stream<kBatch>::run(EXTRA == WITH_CODES ? sh.turns : sh.mine, sh.mine, issue, [&](int k, int slot, auto full) {
     Raw8<T> xs[kBatch], rs[EXTRA >= WITH_RES_GATE ? kBatch : 1];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      if (EXTRA == WITH_CODES || k + u < sh.mine) xs[u] = ring.get(slot + u);
+      if (EXTRA == WITH_CODES || full.value || k + u < sh.mine) xs[u] = ring.get(slot + u);
       if constexpr (EXTRA >= WITH_RES_GATE)
-        if (out.res && k + u < sh.mine) rs[u] = res_ring.get(slot + u);
+        if (out.res && (full.value || k + u < sh.mine)) rs[u] = res_ring.get(slot + u);
     }
-    out.turn(k, sh.mine, true, step, affine, xs, rs);
+    out.template turn<full.value>(k, sh.mine, true, step, affine, xs, rs);
   });
 }
 
@@ -862,11 +873,11 @@ template <typename T, bool VEC, bool CK> struct Feed {
   }
   __device__ __forceinline__ uint32_t at(int k) const { return (uint32_t)(reverse ? n - 1 - k : k); }
   // The bytes of the turn that begins with vector k, to be used two turns later.
-  __device__ __forceinline__ void bytes(int k, int slot) {
+  template <bool FULL> __device__ __forceinline__ void bytes(int k, int slot) {
     const int to = slot / kBatch % (kAhead + 1);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      if (k + u < n) {
+      if (FULL || k + u < n) {
         if constexpr (CK) { scale[to][u] = from.scales[next_scale]; next_scale += scale_step; }
         if (slope == SLOPE_BITS) { open[to][u] = from.gate[next_gate]; next_gate += gate_step; }
       }
@@ -1092,19 +1103,19 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
   grid_dependency_wait();
   grid_dependency_release();
   Feed<T, VEC, CK> feed(p, at, sh, slope, nullptr, false, smem);
-  feed.bytes(0, 0);
-  feed.bytes(kBatch, kBatch);
+  feed.template bytes<false>(0, 0);
+  feed.template bytes<false>(kBatch, kBatch);
   Channels ch;
   float rstd[8];
   Sums sums;
   auto issue = [&](int slot) { feed.issue(slot); };
   Stream<kBatch>::start(sh.mine, issue);
   load_channels(p, at, n, slope, ch, rstd);
-  Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot) {
-    feed.bytes(k + 2 * kBatch, slot + 2 * kBatch);
+  Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot, auto full) {
+    feed.template bytes<full.value>(k + 2 * kBatch, slot + 2 * kBatch);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      if (k + u < sh.mine) {
+      if (full.value || k + u < sh.mine) {
         const Held<T, CK> h = feed.get(slot, u);
         F8 dz, d;
         operands<T, CK>(passed<T, CK>(h, slope), h, slope, ch, dz, d);
@@ -1182,8 +1193,8 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   grid_dependency_release();
   auto issue = [&](int slot) { feed.issue(slot); };
   if constexpr (!VEC) Stream<kBatch>::start(sh.mine, issue);
-  feed.bytes(0, 0);
-  feed.bytes(kBatch, kBatch);
+  feed.template bytes<false>(0, 0);
+  feed.template bytes<false>(kBatch, kBatch);
   Channels ch;
   float rstd[8];
   load_channels(p, at, n, slope, ch, rstd);
@@ -1214,11 +1225,11 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   load_coefficients(g, at, coef, coef + sets, g_first, k1, k2);
   uint32_t o = feed.at(0) * feed.from.step;
   T* const dx = p.dx + (sh.row0 + at.r) * g.C + at.c0;
-  Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot) {
-    feed.bytes(k + 2 * kBatch, slot + 2 * kBatch);
+  Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot, auto full) {
+    feed.template bytes<full.value>(k + 2 * kBatch, slot + 2 * kBatch);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      if (k + u < sh.mine) {
+      if (full.value || k + u < sh.mine) {
         const Held<T, CK> h = feed.get(slot, u);
         Raw8<T> r;
         if (feed.res) r = feed.ress.get(slot + u);
@@ -1289,8 +1300,8 @@ inline Plan plan(int N, int P, int C, int G, size_t vec_bytes, size_t fixed, int
   shares();
   return pl;
 }
-inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G) {
-  return plan(N, P, C, G, 8 * (size_t)elem_bytes, 3 * kThreads * 8 * 4 + 8 * (size_t)C + 16 * (size_t)G, 3);
+inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G, bool codes) {
+  return plan(N, P, C, G, 8 * (size_t)elem_bytes, 3 * kThreads * 8 * 4 + 8 * (size_t)C + 16 * (size_t)G, codes ? kCodesPerSm : kPlainPerSm);
 }
 inline Plan plan_backward(int elem_bytes, int N, int P, int C, int G, bool ckpt) {
   const size_t vec = 8 * (size_t)elem_bytes + (ckpt ? 8 : 8 * (size_t)elem_bytes) + 2;      // dy, x, a byte each for gate and scale

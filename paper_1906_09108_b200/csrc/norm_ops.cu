@@ -70,9 +70,9 @@ fdg_status fdg_gn_scratch_bytes(int precision, const fdg_gn_shape* s, int backwa
   if (!bytes || !gn_shape_ok(precision, s)) return FDG_ERR_INVALID_ARG;
   const int b = (int)elem_bytes(precision);
   if (!backward) {
-    const gn::Plan pl = gn::plan_forward(b, s->N, s->HW, s->C, s->groups);
-    if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
-    *bytes = forward_need(pl);
+    const gn::Plan plain = gn::plan_forward(b, s->N, s->HW, s->C, s->groups, false), codes = gn::plan_forward(b, s->N, s->HW, s->C, s->groups, true);
+    if (!gn::grid_ok(plain) || !gn::grid_ok(codes)) return FDG_ERR_INVALID_ARG;
+    *bytes = std::max(forward_need(plain), forward_need(codes));
     return FDG_OK;
   }
   const gn::Plan of_x = gn::plan_backward(b, s->N, s->HW, s->C, s->groups, false), of_codes = gn::plan_backward(b, s->N, s->HW, s->C, s->groups, true);
@@ -89,7 +89,7 @@ fdg_status fdg_gn_forward(int precision, const fdg_gn_shape* s, const void* x, c
   if ((act == FDG_ACT_SILU && res) || (gate && act != FDG_ACT_RELU) || (codes != nullptr) != (scales != nullptr)) return FDG_ERR_INVALID_ARG;
   const unsigned b = elem_bytes(precision);
   if (!aligned_to(x, b) || !aligned_to(y, b) || !aligned_to(res, b) || !aligned_to(scratch, 256)) return FDG_ERR_INVALID_ARG;
-  const gn::Plan pl = gn::plan_forward((int)b, s->N, s->HW, s->C, s->groups);
+  const gn::Plan pl = gn::plan_forward((int)b, s->N, s->HW, s->C, s->groups, codes != nullptr);
   if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
   const size_t need = forward_need(pl);
   if (need > 0 && (!scratch || scratch_bytes < need)) return FDG_ERR_WORKSPACE_TOO_SMALL;
