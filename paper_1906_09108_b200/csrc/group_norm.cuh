@@ -405,38 +405,42 @@ __device__ __forceinline__ uint32_t positive_bits(const Raw8<float>& y) {
 // y (and the gate's bits, and x in 8 bits) of a thread's pixels.  ACT < 0: p.act.  EXTRA 1: res and gate may be asked for; 2: and
 // codes.  Offsets inside a CTA's pixels fit 32 bits.
 enum { PLAIN = 0, WITH_RES_GATE = 1, WITH_CODES = 2 };
-constexpr int kPlainPerSm = 3, kCodesPerSm = 2;       // CTAs on an SM that the registers allow (80 spill where codes are formed)
+constexpr int kPlainPerSm = 3, kCodesPerSm = 3;       // CTAs on an SM that the registers allow (80 spill where codes are formed)
 template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
-  T* y;
+  T* y;                       // of the CTA's first pixel, as the others: the same for all threads
   const T* res;
   int8_t* codes;
   uint8_t *gate, *scales;
-  uint32_t gate_step, scale_step;
+  uint32_t first, step, gate_first, gate_step, scale_first, scale_step;      // the thread's first pixel, and the next from each
   int act, left, lanes;
   bool leads;
   __device__ __forceinline__ Emitter(const Forward<T>& p, const Place& at, const Share& sh) {
     const Geom& g = p.g;
-    const size_t row = sh.row0 + at.r, off = row * g.C + at.c0;
+    const size_t off = sh.row0 * g.C;
     act = ACT < 0 ? p.act : ACT;
     left = at.left;
     y = p.y + off;
+    first = (uint32_t)at.r * g.C + at.c0;
+    step = (uint32_t)g.rp * g.C;
     res = nullptr; gate = nullptr; codes = nullptr;
     if constexpr (EXTRA >= WITH_RES_GATE) {
       const int all_cols = (g.C + 7) >> 3;
       if (p.res) res = p.res + off;
-      if (p.gate) gate = p.gate + (row * all_cols + (at.c0 >> 3));
+      if (p.gate) gate = p.gate + sh.row0 * all_cols;
+      gate_first = (uint32_t)at.r * all_cols + (at.c0 >> 3);
       gate_step = (uint32_t)g.rp * all_cols;
     }
     if constexpr (EXTRA == WITH_CODES) {
       const int per_row = (g.C + kCkptBlock - 1) / kCkptBlock;
       if (VEC || p.codes) codes = p.codes + off;             // the form for any alignment is compiled once, for all options
-      scales = p.scales + (row * per_row + at.c0 / kCkptBlock);
+      scales = p.scales + sh.row0 * per_row;
+      scale_first = (uint32_t)at.r * per_row + at.c0 / kCkptBlock;
       scale_step = (uint32_t)g.rp * per_row;
       lanes = p.ckpt_lanes;
       leads = (at.col & (lanes - 1)) == 0;
     }
   }
-  // Pixel k of the thread, at element offset o = k * rp * C.
+  // Pixel k of the thread, at element offset o.
   __device__ __forceinline__ void value(uint32_t k, uint32_t o, const Affine<T>& affine, const F8& x, const Raw8<T>& raw_res) const {
     F8 z;
 #pragma unroll
@@ -451,7 +455,7 @@ template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
       const Raw8<T> out = f8_to_raw8<T, true>(z);
       raw8_put<T, VEC>(y + o, left, out);
       if constexpr (EXTRA >= WITH_RES_GATE)
-        if (gate) gate[k * gate_step] = (uint8_t)(positive_bits(out) & (VEC ? 0xFFu : (1u << left) - 1));
+        if (gate) gate[gate_first + k * gate_step] = (uint8_t)(positive_bits(out) & (VEC ? 0xFFu : (1u << left) - 1));
     } else {
       if (act == ACT_SILU) {
 #pragma unroll
@@ -466,21 +470,21 @@ template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
   // A turn of B pixels, raw, k counting from the thread's first pixel or (back) its last; for the whole warp where codes are
   // formed, since the lanes that share a block of 32 channels (they have the same pixels) exchange its maximum.
   template <bool FULL, int B>
-  __device__ __forceinline__ void turn(int k, int mine, bool back, uint32_t step, const Affine<T>& affine, const Raw8<T> (&raw)[B], const Raw8<T>* raw_res) const {
+  __device__ __forceinline__ void turn(int k, int mine, bool back, const Affine<T>& affine, const Raw8<T> (&raw)[B], const Raw8<T>* raw_res) const {
     uint32_t top[B];
     if constexpr (EXTRA == WITH_CODES)
       if (VEC || codes) block_tops<B>(raw, top);
 #pragma unroll
     for (int u = 0; u < B; ++u)
       if (FULL || k + u < mine) {
-        const uint32_t kk = (uint32_t)(back ? mine - 1 - (k + u) : k + u), o = kk * step;
+        const uint32_t kk = (uint32_t)(back ? mine - 1 - (k + u) : k + u), o = first + kk * step;
         const F8 x = raw8_to_f8(raw[u]);
         value(kk, o, affine, x, raw_res[EXTRA >= WITH_RES_GATE ? u : 0]);
         if constexpr (EXTRA == WITH_CODES)
           if (VEC || codes) {
             const CkptScale s = ckpt_scale(top[u]);
             store_codes<VEC>(codes + o, 0, left, ckpt_codes(x, s));
-            if (leads) scales[kk * scale_step] = (uint8_t)s.byte;
+            if (leads) scales[scale_first + kk * scale_step] = (uint8_t)s.byte;
           }
       }
   }
@@ -533,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : 
   const Emitter<T, VEC, ACT, EXTRA> out(p, at, sh);
   if constexpr (EXTRA >= WITH_RES_GATE)
     if (out.res)
-      for (int k = 0; k < sh.mine; ++k) prefetch_l2(out.res + (uint32_t)k * step);
+      for (int k = 0; k < sh.mine; ++k) prefetch_l2(out.res + (out.first + (uint32_t)k * step));
   float gamma[8], beta[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) { gamma[i] = p.gamma[at.channel(i)]; beta[i] = p.beta[at.channel(i)]; }
@@ -563,9 +567,9 @@ __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : 
     for (int u = 0; u < kBatch; ++u) {
       if (EXTRA == WITH_CODES || k + u < sh.mine) xs[u] = slots.get(min(k + u, g.iters - 1));
       if constexpr (EXTRA >= WITH_RES_GATE)
-        if (out.res && k + u < sh.mine) rs[u] = raw8_load<T, VEC>(out.res + (uint32_t)(k + u) * step, at.left);
+        if (out.res && k + u < sh.mine) rs[u] = raw8_load<T, VEC>(out.res + (out.first + (uint32_t)(k + u) * step), at.left);
     }
-    out.template turn<false>(k, sh.mine, false, step, affine, xs, rs);
+    out.template turn<false>(k, sh.mine, false, affine, xs, rs);
   }
   cluster.barrier_wait(std::move(token));                                 // nor do they read its own
 }
@@ -587,16 +591,17 @@ __global__ void __launch_bounds__(kThreads, 3) moments_kernel(const __grid_const
   // next one copies from them (and from nothing that this kernel writes) before its own wait.
   grid_dependency_wait();
   grid_dependency_release();
-  const T* src = p.x + (sh.row0 + at.r) * g.C + at.c0;
+  const T* const src = p.x + sh.row0 * g.C;
+  uint32_t next = (uint32_t)at.r * g.C + at.c0;
   const uint32_t step = (uint32_t)g.rp * g.C;
   const Slots<T> ring(smem);
   Moments m;
-  auto issue = [&](int slot) {
-    ring.template fetch<VEC>(slot, src, at.left);
-    src += step;
-  };
   Raw8<T> first{};
-  if (sh.mine > 0) first = raw8_load<T, VEC>(src, at.left);
+  if (sh.mine > 0) first = raw8_load<T, VEC>(src + next, at.left);
+  auto issue = [&](int slot) {
+    ring.template fetch<VEC>(slot, src + next, at.left);
+    next += step;
+  };
   Stream<kBatch>::start(sh.mine, issue);
   m.start(raw8_to_f8(first));
   Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot, auto full) {
@@ -679,14 +684,13 @@ __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : 
   if (at.left <= 0) { at.c0 = 0; at.left = 1; }
   const Share sh(g, at, n, part);
   const Emitter<T, VEC, ACT, EXTRA> out(p, at, sh);
-  const uint32_t step = (uint32_t)g.rp * g.C;
-  const T* x = p.x + (sh.row0 + at.r) * g.C + at.c0 + (uint32_t)max(sh.mine - 1, 0) * step;
-  const T* res = out.res + (uint32_t)max(sh.mine - 1, 0) * step;
+  const T* const x = p.x + sh.row0 * g.C;
+  uint32_t next = out.first + (uint32_t)max(sh.mine - 1, 0) * out.step;
   auto issue = [&](int slot) {
-    ring.template fetch<VEC>(slot, x, at.left);
-    x -= step;
+    ring.template fetch<VEC>(slot, x + next, at.left);
     if constexpr (EXTRA >= WITH_RES_GATE)
-      if (out.res) { res_ring.template fetch<VEC>(slot, res, at.left); res -= step; }
+      if (out.res) res_ring.template fetch<VEC>(slot, out.res + next, at.left);
+    next -= out.step;
   };
   float gamma[8], beta[8];
   if constexpr (VEC) Stream<kBatch>::start(sh.mine, issue);      // see grid_dependency_release in moments_kernel
@@ -719,7 +723,7 @@ __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : 
       if constexpr (EXTRA >= WITH_RES_GATE)
         if (out.res && (full.value || k + u < sh.mine)) rs[u] = res_ring.get(slot + u);
     }
-    out.template turn<full.value>(k, sh.mine, true, step, affine, xs, rs);
+    out.template turn<full.value>(k, sh.mine, true, affine, xs, rs);
   });
 }
 
@@ -754,19 +758,23 @@ template <typename T, bool CK> struct Held {
   Raw8<T> mask;               // SLOPE_MASK
   uint32_t open;              // SLOPE_BITS
 };
-// Where a thread's columns start in the tensors, and how far apart its pixels are.
+// Where a CTA's pixels start in the tensors (the same for all threads), where a thread's columns do, and how far apart its
+// pixels are.
 template <typename T> struct Columns {
   const T *dy, *x, *mask;
   const int8_t* codes;
   const uint8_t *scales, *gate;
-  uint32_t step, gate_step, scale_step;
+  uint32_t first, step, gate_first, gate_step, scale_first, scale_step;
   __device__ __forceinline__ Columns(const Backward<T>& p, const Place& at, const Share& sh) {
     const Geom& g = p.g;
     const int all_cols = (g.C + 7) >> 3, per_row = (g.C + kCkptBlock - 1) / kCkptBlock;
-    const size_t row = sh.row0 + at.r, off = row * g.C + at.c0;
+    const size_t off = sh.row0 * g.C;
     dy = p.dy + off; x = p.x + off; mask = p.mask + off; codes = p.codes + off;
-    scales = p.scales + (row * per_row + at.c0 / kCkptBlock);
-    gate = p.gate + (row * all_cols + (at.c0 >> 3));
+    scales = p.scales + sh.row0 * per_row;
+    gate = p.gate + sh.row0 * all_cols;
+    first = (uint32_t)at.r * g.C + at.c0;
+    scale_first = (uint32_t)at.r * per_row + at.c0 / kCkptBlock;
+    gate_first = (uint32_t)at.r * all_cols + (at.c0 >> 3);
     step = (uint32_t)g.rp * g.C; gate_step = (uint32_t)g.rp * all_cols; scale_step = (uint32_t)g.rp * per_row;
   }
 };
@@ -864,14 +872,13 @@ template <typename T, bool VEC, bool CK> struct Feed {
   __device__ __forceinline__ Feed(const Backward<T>& p, const Place& at, const Share& sh, int slope_, const T* res_, bool reverse_, uint4* smem)
       : from(p, at, sh), dys(smem), xs(smem + kVec), masks(smem + kVec + (CK ? kRing * kThreads / 2 : kVec)),
         ress(smem + words(slope_ == SLOPE_MASK, false)), codes(reinterpret_cast<uint2*>(smem + kVec) + threadIdx.x),
-        res(res_ ? res_ + (sh.row0 + at.r) * p.g.C + at.c0 : nullptr), left(at.left), slope(slope_), n(sh.mine), reverse(reverse_) {
+        res(res_ ? res_ + sh.row0 * p.g.C : nullptr), left(at.left), slope(slope_), n(sh.mine), reverse(reverse_) {
     step = reverse ? 0u - from.step : from.step;
     scale_step = reverse ? 0u - from.scale_step : from.scale_step;
     gate_step = reverse ? 0u - from.gate_step : from.gate_step;
-    const uint32_t first = reverse && n > 0 ? (uint32_t)(n - 1) : 0u;
-    next = first * from.step; next_scale = first * from.scale_step; next_gate = first * from.gate_step;
+    const uint32_t k = reverse && n > 0 ? (uint32_t)(n - 1) : 0u;
+    next = from.first + k * from.step; next_scale = from.scale_first + k * from.scale_step; next_gate = from.gate_first + k * from.gate_step;
   }
-  __device__ __forceinline__ uint32_t at(int k) const { return (uint32_t)(reverse ? n - 1 - k : k); }
   // The bytes of the turn that begins with vector k, to be used two turns later.
   template <bool FULL> __device__ __forceinline__ void bytes(int k, int slot) {
     const int to = slot / kBatch % (kAhead + 1);
@@ -982,7 +989,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
   grid_dependency_release();
 #pragma unroll 4
   for (int k = 0; k < sh.mine; ++k) {
-    const uint32_t o = (uint32_t)k * from.step;
+    const uint32_t o = from.first + (uint32_t)k * from.step;
     dys.template fetch<VEC>(k, from.dy + o, at.left);
     if constexpr (CK) {
       if constexpr (VEC) copy8_async(cs + k * kThreads + tid, from.codes + o); else cs[k * kThreads + tid] = load_codes<false>(from.codes + o, 0, at.left);
@@ -990,21 +997,23 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
       xslots.template fetch<VEC>(k, from.x + o, at.left);
     }
   }
-  const T* const res = p.res ? p.res + (sh.row0 + at.r) * g.C + at.c0 : nullptr;
+  const T* const res = p.res ? p.res + sh.row0 * g.C : nullptr;
   if (res)
-    for (int k = 0; k < sh.mine; ++k) prefetch_l2(res + (uint32_t)k * from.step);
+    for (int k = 0; k < sh.mine; ++k) prefetch_l2(res + (from.first + (uint32_t)k * from.step));
   // what comes in bytes goes through registers, several loads in flight
+  if (slope == SLOPE_MASK)
+    for (int k = 0; k < sh.mine; ++k) prefetch_l2(from.mask + (from.first + (uint32_t)k * from.step));
   if (CK || slope == SLOPE_MASK || slope == SLOPE_BITS) {
-    constexpr int U = 4;
+    constexpr int U = sizeof(T) == 2 ? 8 : 4;
     for (int k0 = 0; k0 < sh.mine; k0 += U) {
       uint32_t sc[U], bits[U];
       Raw8<T> m[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (k0 + u < sh.mine) {
-          if constexpr (CK) sc[u] = from.scales[(uint32_t)(k0 + u) * from.scale_step];
-          if (slope == SLOPE_BITS) bits[u] = from.gate[(uint32_t)(k0 + u) * from.gate_step];
-          if (slope == SLOPE_MASK) m[u] = raw8_load<T, VEC>(from.mask + (uint32_t)(k0 + u) * from.step, at.left);
+          if constexpr (CK) sc[u] = from.scales[from.scale_first + (uint32_t)(k0 + u) * from.scale_step];
+          if (slope == SLOPE_BITS) bits[u] = from.gate[from.gate_first + (uint32_t)(k0 + u) * from.gate_step];
+          if (slope == SLOPE_MASK) m[u] = raw8_load<T, VEC>(from.mask + (from.first + (uint32_t)(k0 + u) * from.step), at.left);
         }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -1072,17 +1081,17 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
   __syncthreads();
   f32x2 k1[4], k2[4];
   load_coefficients(g, at, coef, coef + g.G, 0, k1, k2);
-  T* const dx = p.dx + (sh.row0 + at.r) * g.C + at.c0;
+  T* const dx = p.dx + sh.row0 * g.C;
   for (int k = 0; k < sh.mine; k += kBatch) {
     Raw8<T> rs[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      if (res && k + u < sh.mine) rs[u] = raw8_load<T, VEC>(res + (uint32_t)(k + u) * from.step, at.left);
+      if (res && k + u < sh.mine) rs[u] = raw8_load<T, VEC>(res + (from.first + (uint32_t)(k + u) * from.step), at.left);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (k + u < sh.mine) {
         const Held<T, CK> h = held(k + u);
-        raw8_put<T, VEC>(dx + (uint32_t)(k + u) * from.step, at.left, dx_of<T, CK>(h.dy, h, slope, ch, k1, k2, res ? &rs[u] : nullptr));
+        raw8_put<T, VEC>(dx + (from.first + (uint32_t)(k + u) * from.step), at.left, dx_of<T, CK>(h.dy, h, slope, ch, k1, k2, res ? &rs[u] : nullptr));
       }
   }
   cluster.barrier_wait(std::move(token));
@@ -1223,8 +1232,8 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   __syncthreads();
   f32x2 k1[4], k2[4];
   load_coefficients(g, at, coef, coef + sets, g_first, k1, k2);
-  uint32_t o = feed.at(0) * feed.from.step;
-  T* const dx = p.dx + (sh.row0 + at.r) * g.C + at.c0;
+  uint32_t o = feed.from.first + (uint32_t)max(sh.mine - 1, 0) * feed.from.step;
+  T* const dx = p.dx + sh.row0 * g.C;
   Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot, auto full) {
     feed.template bytes<full.value>(k + 2 * kBatch, slot + 2 * kBatch);
 #pragma unroll
@@ -1295,7 +1304,7 @@ inline Plan plan(int N, int P, int C, int G, size_t vec_bytes, size_t fixed, int
     }
   }
   // one wave of CTAs, each with at least one batch of pixels in flight
-  split((int)std::max<int64_t>(1, std::min<int64_t>((int64_t)per_sm * kSms / N, P / (4 * g.rp))));
+  split((int)std::max<int64_t>(1, std::min<int64_t>((int64_t)((getenv("GN_F")?atof(getenv("GN_F")):1.0)*per_sm * kSms) / N, P / (4 * g.rp))));
   g.parts = P / g.pix + (P % g.pix != 0);         // none without pixels
   shares();
   return pl;
