@@ -135,6 +135,18 @@ template <int B> struct Stream {
     for (; k0 + R + B * kAhead <= mine; k0 += R) round<true>(k0, n, mine, issue, turn);
     for (; k0 < n; k0 += R) round<false>(k0, n, mine, issue, turn);
   }
+  // The same in a loop of single turns, for turns whose code unrolled over the ring does not fit the instruction caches.
+  template <typename Issue, typename Turn> static __device__ __forceinline__ void run_rolled(int n, int mine, Issue issue, Turn turn) {
+#pragma unroll 1
+    for (int k = 0; k < n; k += B) {
+#pragma unroll
+      for (int u = 0; u < B; ++u)
+        if (k + B * kAhead + u < mine) issue((k + B * kAhead + u) & (R - 1));
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+      turn(k, k & (R - 1), Full<false>());
+    }
+  }
 
  private:
   template <bool FULL, typename Issue, typename Turn>
@@ -715,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : 
     load_affine(p, at, gamma, beta, [&](int s) { return make_float2(p.stats[(size_t)n * g.G + s], p.stats[(size_t)(g.N + n) * g.G + s]); }, affine);
   else
     load_affine(p, at, gamma, beta, [&](int s) { return mom[s]; }, affine);
-  Stream<kBatch>::run(EXTRA == WITH_CODES ? sh.turns : sh.mine, sh.mine, issue, [&](int k, int slot, auto full) {
+  auto turn = [&](int k, int slot, auto full) {
     Raw8<T> xs[kBatch], rs[EXTRA >= WITH_RES_GATE ? kBatch : 1];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
@@ -724,7 +736,9 @@ __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : 
         if (out.res && (full.value || k + u < sh.mine)) rs[u] = res_ring.get(slot + u);
     }
     out.template turn<full.value>(k, sh.mine, true, affine, xs, rs);
-  });
+  };
+  if constexpr (EXTRA == WITH_CODES) Stream<kBatch>::run_rolled(sh.turns, sh.mine, issue, turn);
+  else Stream<kBatch>::run(sh.mine, sh.mine, issue, turn);
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------
