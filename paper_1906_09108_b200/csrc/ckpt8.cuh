@@ -117,23 +117,31 @@ __device__ __forceinline__ F8 ckpt_values(uint2 codes, float step) {
   return f;
 }
 
-// Bytes of 8 codes at element offset `off`; VEC: one 8-byte access, else the first `left`.
-template <bool VEC> __device__ __forceinline__ uint2 load_codes(const int8_t* codes, size_t off, int left) {
-  if constexpr (VEC) {
-    return *reinterpret_cast<const uint2*>(codes + off);
+// 8 codes in pieces of CW bytes (8, 4, 2, 1), the first `left` of them.
+template <int CW> struct CodePiece;
+template <> struct CodePiece<4> { typedef uint32_t Type; };
+template <> struct CodePiece<2> { typedef uint16_t Type; };
+template <> struct CodePiece<1> { typedef uint8_t Type; };
+template <int CW> __device__ __forceinline__ uint2 load_codes(const int8_t* codes, int left) {
+  if constexpr (CW == 8) {
+    return *reinterpret_cast<const uint2*>(codes);
   } else {
+    typedef typename CodePiece<CW>::Type P;
     uint32_t w[2] = {0, 0};
-    for (int i = 0; i < 8; ++i)
-      if (i < left) w[i >> 2] |= (uint32_t)(uint8_t)codes[off + i] << (8 * (i & 3));
+#pragma unroll
+    for (int i = 0; i < 8 / CW; ++i)
+      if (i * CW < left) w[i * CW / 4] |= (uint32_t) reinterpret_cast<const P*>(codes)[i] << (8 * (i * CW % 4));
     return make_uint2(w[0], w[1]);
   }
 }
-template <bool VEC> __device__ __forceinline__ void store_codes(int8_t* codes, size_t off, int left, uint2 q) {
-  if constexpr (VEC) {
-    *reinterpret_cast<uint2*>(codes + off) = q;
+template <int CW> __device__ __forceinline__ void store_codes(int8_t* codes, int left, uint2 q) {
+  if constexpr (CW == 8) {
+    *reinterpret_cast<uint2*>(codes) = q;
   } else {
-    for (int i = 0; i < 8; ++i)
-      if (i < left) codes[off + i] = (int8_t)((i < 4 ? q.x : q.y) >> (8 * (i & 3)));
+    typedef typename CodePiece<CW>::Type P;
+#pragma unroll
+    for (int i = 0; i < 8 / CW; ++i)
+      if (i * CW < left) reinterpret_cast<P*>(codes)[i] = (P)((i * CW < 4 ? q.x : q.y) >> (8 * (i * CW % 4)));
   }
 }
 
@@ -163,7 +171,7 @@ __global__ void __launch_bounds__(kCkptThreads) ckpt_encode_kernel(const T* __re
 #pragma unroll
   for (int u = 0; u < kCkptUnroll; ++u) {
     const size_t i = first + (size_t)u * kCkptThreads;
-    raw[u] = i < vecs ? raw8_load<T, true>(x + i * 8, 8) : Raw8<T>{};
+    raw[u] = i < vecs ? raw8_load<T, kWhole>(x + i * 8, 8) : Raw8<T>{};
   }
 #pragma unroll
   for (int u = 0; u < kCkptUnroll; ++u) {
@@ -176,22 +184,62 @@ __global__ void __launch_bounds__(kCkptThreads) ckpt_encode_kernel(const T* __re
   }
 }
 
-// Encode, any row length and alignment: a warp takes a block, a lane a value.
+// Encode, rows of whole vectors of any number: a thread takes a block, up to 4 vectors.
+template <typename T>
+__global__ void __launch_bounds__(kCkptThreads) ckpt_encode_blocks_kernel(const T* __restrict__ x, size_t blocks, int cols, int per_row,
+                                                                          int8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  grid_dependency_wait();
+  const size_t b = (size_t)blockIdx.x * kCkptThreads + threadIdx.x;
+  if (b >= blocks) return;
+  const size_t row = b / (unsigned)per_row;
+  const int col = (int)(b - row * (unsigned)per_row) * 4, n = min(4, cols - col);
+  const size_t off = (row * (unsigned)cols + col) * 8;
+  Raw8<T> raw[4];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < n) raw[i] = raw8_load<T, kWhole>(x + off + 8 * i, 8);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < n) top = max(top, ckpt_top(raw[i]));
+  const CkptScale s = ckpt_scale(top);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < n) *reinterpret_cast<uint2*>(codes + off + 8 * i) = ckpt_codes(raw8_to_f8(raw[i]), s);
+  scales[b] = (uint8_t)s.byte;
+}
+
+// Encode, any row length and alignment: a lane takes a value, a warp a block, kCkptBlocks of them in flight.
+constexpr int kCkptBlocks = 8;
 template <typename T>
 __global__ void __launch_bounds__(kCkptThreads) ckpt_encode_any_kernel(const T* __restrict__ x, size_t blocks, int C, int per_row,
                                                                        int8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
   grid_dependency_wait();
   const int lane = threadIdx.x & 31;
-  const size_t stride = (size_t)gridDim.x * (kCkptThreads / 32);
-  for (size_t b = (size_t)blockIdx.x * (kCkptThreads / 32) + (threadIdx.x >> 5); b < blocks; b += stride) {
-    const size_t row = b / (unsigned)per_row;
-    const int c = (int)(b - row * (unsigned)per_row) * kCkptBlock + lane;
-    const size_t off = row * C + c;
-    const float v = c < C ? to_f(x[off]) : 0.f;
-    const CkptScale s = ckpt_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7FFFFFFFu));
-    if (c < C) codes[off] = (int8_t)ckpt_code(v, s);
-    if (lane == 0) scales[b] = (uint8_t)s.byte;
+  const size_t b0 = ((size_t)blockIdx.x * (kCkptThreads / 32) + (threadIdx.x >> 5)) * kCkptBlocks;
+  if (b0 >= blocks) return;
+  const size_t row0 = b0 / (unsigned)per_row;
+  const int first = (int)(b0 - row0 * (unsigned)per_row);
+  x += row0 * C; codes += row0 * C;                      // the same for the warp; what follows is a few rows on
+  const int n = (int)min((size_t)kCkptBlocks, blocks - b0);
+  float v[kCkptBlocks];
+  int off[kCkptBlocks];                                  // of the lane's value, -1 behind the row's end
+  int row = 0, in_row = first;
+#pragma unroll
+  for (int i = 0; i < kCkptBlocks; ++i) {
+    const int c = in_row * kCkptBlock + lane;
+    off[i] = i < n && c < C ? row * C + c : -1;
+    v[i] = off[i] >= 0 ? to_f(x[off[i]]) : 0.f;
+    if (++in_row == per_row) { in_row = 0; ++row; }
   }
+  uint32_t byte = 0;
+#pragma unroll
+  for (int i = 0; i < kCkptBlocks; ++i) {
+    const CkptScale s = ckpt_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(v[i]) & 0x7FFFFFFFu));
+    if (off[i] >= 0) codes[off[i]] = (int8_t)ckpt_code(v[i], s);
+    if (lane == i) byte = s.byte;
+  }
+  if (lane < n) scales[b0 + lane] = (uint8_t)byte;
 }
 
 // Decode, rows of whole vectors (C a multiple of 8): a thread takes vectors of 8 values.  `lanes` as in the encoder; 0: the
@@ -225,7 +273,7 @@ __global__ void __launch_bounds__(kCkptThreads) ckpt_decode_kernel(const int8_t*
   for (int u = 0; u < kCkptUnroll; ++u) {
     const size_t i = first + (size_t)u * kCkptThreads;
     if (i >= vecs) break;
-    raw8_put<T, true>(x + i * 8, 8, f8_to_raw8<T>(ckpt_values(q[u], ckpt_step(k[u]))));
+    raw8_put<T, kWhole>(x + i * 8, 8, f8_to_raw8<T>(ckpt_values(q[u], ckpt_step(k[u]))));
   }
 }
 // Decode, any row length and alignment: a thread takes values.
@@ -242,24 +290,27 @@ __global__ void __launch_bounds__(kCkptThreads) ckpt_decode_any_kernel(const int
 }
 
 // ---- host side -----------------------------------------------------------------------------------------
-inline bool aligned_to(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 constexpr size_t kCkptMaxGrid = (size_t)1 << 30;
 
 template <typename T>
 inline cudaError_t launch_ckpt_encode(cudaStream_t st, const T* x, size_t rows, int C, int8_t* codes, uint8_t* scales) {
-  const int lanes = C % 8 == 0 ? ckpt_block_lanes(C) : 0, per_row = (C + kCkptBlock - 1) / kCkptBlock;
-  if (lanes && aligned_to(x, 16) && aligned_to(codes, 8)) {
-    const size_t vecs = rows * (size_t)(C / 8), per = kCkptThreads * kCkptUnroll, grid = (vecs + per - 1) / per;
-    if (grid <= kCkptMaxGrid)
+  const int lanes = ckpt_block_lanes(C), per_row = (C + kCkptBlock - 1) / kCkptBlock;
+  const size_t blocks = rows * (size_t)per_row;
+  if (access_width<T>(C, {x}, codes) == kWhole) {
+    const size_t vecs = rows * (size_t)(C / 8), per = kCkptThreads * kCkptUnroll, grid = lanes ? (vecs + per - 1) / per : (blocks + kCkptThreads - 1) / kCkptThreads;
+    if (grid <= kCkptMaxGrid && lanes)
       return launch_chained(ckpt_encode_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, x, vecs, lanes, codes, scales);
+    if (grid <= kCkptMaxGrid)
+      return launch_chained(ckpt_encode_blocks_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, x, blocks, C / 8, per_row, codes, scales);
   }
-  const size_t blocks = rows * (size_t)per_row, grid = std::min<size_t>((blocks + 7) / 8, (size_t)kSms * 64);
+  const size_t per = kCkptThreads / 32 * kCkptBlocks, grid = (blocks + per - 1) / per;
+  if (grid > INT32_MAX) return cudaErrorInvalidValue;
   return launch_chained(ckpt_encode_any_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, x, blocks, C, per_row, codes, scales);
 }
 template <typename T>
 inline cudaError_t launch_ckpt_decode(cudaStream_t st, const int8_t* codes, const uint8_t* scales, size_t rows, int C, T* x) {
   const int per_row = (C + kCkptBlock - 1) / kCkptBlock;
-  if (C % 8 == 0 && aligned_to(x, 16) && aligned_to(codes, 8)) {
+  if (access_width<T>(C, {x}, codes) == kWhole) {
     const size_t vecs = rows * (size_t)(C / 8), per = kCkptThreads * kCkptUnroll, grid = (vecs + per - 1) / per;
     if (grid <= kCkptMaxGrid)
       return launch_chained(ckpt_decode_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, codes, scales, vecs, ckpt_block_lanes(C), C / 8, per_row,

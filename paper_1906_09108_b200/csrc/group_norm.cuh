@@ -83,6 +83,11 @@ __device__ __forceinline__ void copy16_async(void* smem, const void* gmem) {
 __device__ __forceinline__ void copy8_async(void* smem, const void* gmem) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem) : "memory");
 }
+// Through L1, for pieces of a sector: the accesses that follow to the same sector find it there.
+template <int W> __device__ __forceinline__ void copy_piece_async(void* smem, const void* gmem, bool exists) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem), "n"(W), "r"(exists ? W : 0)
+               : "memory");
+}
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void prefetch_l2(const void* gmem) { asm volatile("prefetch.global.L2 [%0];" ::"l"(gmem)); }
 
@@ -91,12 +96,16 @@ template <typename T> struct Slots {
   static constexpr int Q = sizeof(T) / 2;
   uint4* base;                // + threadIdx.x
   __device__ __forceinline__ Slots(void* smem) : base(static_cast<uint4*>(smem) + threadIdx.x) {}
-  template <bool VEC> __device__ __forceinline__ void fetch(int k, const T* __restrict__ p, int left) const {
-    if constexpr (VEC) {
+  template <int W> __device__ __forceinline__ void fetch(int k, const T* __restrict__ p, int left) const {
+    if constexpr (W == kWhole && sizeof(T) == 2) {
+      copy16_async(base + k * kThreads, p);
+    } else if constexpr (W >= 4) {
+      constexpr int B = W, PER = B / (int)sizeof(T);
 #pragma unroll
-      for (int j = 0; j < Q; ++j) copy16_async(base + (k * Q + j) * kThreads, reinterpret_cast<const uint4*>(p) + j);
+      for (int i = 0; i < 8 / PER; ++i)
+        copy_piece_async<B>(reinterpret_cast<char*>(base + (k * Q + i * B / 16) * kThreads) + i * B % 16, p + i * PER, W == kWhole || i * PER < left);
     } else {
-      put(k, raw8_load<T, false>(p, left));
+      put(k, raw8_load<T, W>(p, left));
     }
   }
   __device__ __forceinline__ Raw8<T> get(int k) const {
@@ -164,6 +173,11 @@ template <int B> struct Stream {
     }
   }
 };
+
+// Whether copies of these vectors may begin before a kernel's grid_dependency_wait(), see moments_kernel: those that go past L1.
+template <typename T, int W> constexpr bool kEarly = W == kWhole && sizeof(T) == 2;
+// Bytes of a piece of 8 codes.
+template <typename T, int W> constexpr int kCodeWidth = W == kWhole ? 8 : W / (int)sizeof(T);
 
 // This thread's place in a CTA's tile.
 struct Place {
@@ -418,7 +432,7 @@ __device__ __forceinline__ uint32_t positive_bits(const Raw8<float>& y) {
 // codes.  Offsets inside a CTA's pixels fit 32 bits.
 enum { PLAIN = 0, WITH_RES_GATE = 1, WITH_CODES = 2 };
 constexpr int kPlainPerSm = 3, kCodesPerSm = 3;       // CTAs on an SM that the registers allow (80 spill where codes are formed)
-template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
+template <typename T, int W, int ACT, int EXTRA> struct Emitter {
   T* y;                       // of the CTA's first pixel, as the others: the same for all threads
   const T* res;
   int8_t* codes;
@@ -444,7 +458,7 @@ template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
     }
     if constexpr (EXTRA == WITH_CODES) {
       const int per_row = (g.C + kCkptBlock - 1) / kCkptBlock;
-      if (VEC || p.codes) codes = p.codes + off;             // the form for any alignment is compiled once, for all options
+      if (W == kWhole || p.codes) codes = p.codes + off;             // the form for any alignment is compiled once, for all options
       scales = p.scales + sh.row0 * per_row;
       scale_first = (uint32_t)at.r * per_row + at.c0 / kCkptBlock;
       scale_step = (uint32_t)g.rp * per_row;
@@ -465,9 +479,9 @@ template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
       }
     if (act == ACT_RELU) {
       const Raw8<T> out = f8_to_raw8<T, true>(z);
-      raw8_put<T, VEC>(y + o, left, out);
+      raw8_put<T, W>(y + o, left, out);
       if constexpr (EXTRA >= WITH_RES_GATE)
-        if (gate) gate[gate_first + k * gate_step] = (uint8_t)(positive_bits(out) & (VEC ? 0xFFu : (1u << left) - 1));
+        if (gate) gate[gate_first + k * gate_step] = (uint8_t)(positive_bits(out) & (W == kWhole ? 0xFFu : (1u << left) - 1));
     } else {
       if (act == ACT_SILU) {
 #pragma unroll
@@ -476,7 +490,7 @@ template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
           z.p[j] = mul2(z.p[j], pair(sigmoid<T>(h.x), sigmoid<T>(h.y)));
         }
       }
-      raw8_put<T, VEC>(y + o, left, f8_to_raw8<T>(z));
+      raw8_put<T, W>(y + o, left, f8_to_raw8<T>(z));
     }
   }
   // A turn of B pixels, raw, k counting from the thread's first pixel or (back) its last; for the whole warp where codes are
@@ -485,7 +499,7 @@ template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
   __device__ __forceinline__ void turn(int k, int mine, bool back, const Affine<T>& affine, const Raw8<T> (&raw)[B], const Raw8<T>* raw_res) const {
     uint32_t top[B];
     if constexpr (EXTRA == WITH_CODES)
-      if (VEC || codes) block_tops<B>(raw, top);
+      if (W == kWhole || codes) block_tops<B>(raw, top);
 #pragma unroll
     for (int u = 0; u < B; ++u)
       if (FULL || k + u < mine) {
@@ -493,9 +507,9 @@ template <typename T, bool VEC, int ACT, int EXTRA> struct Emitter {
         const F8 x = raw8_to_f8(raw[u]);
         value(kk, o, affine, x, raw_res[EXTRA >= WITH_RES_GATE ? u : 0]);
         if constexpr (EXTRA == WITH_CODES)
-          if (VEC || codes) {
+          if (W == kWhole || codes) {
             const CkptScale s = ckpt_scale(top[u]);
-            store_codes<VEC>(codes + o, 0, left, ckpt_codes(x, s));
+            store_codes<kCodeWidth<T, W>>(codes + o, left, ckpt_codes(x, s));
             if (leads) scales[scale_first + kk * scale_step] = (uint8_t)s.byte;
           }
       }
@@ -527,7 +541,7 @@ __device__ __forceinline__ void load_affine(const Forward<T>& p, const Place& at
 }
 
 // The resident form: blockIdx = image, share of its pixels, tile of columns: a cluster per image.
-template <typename T, bool VEC, int ACT, int EXTRA>
+template <typename T, int W, int ACT, int EXTRA>
 __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : kPlainPerSm) forward_kernel(const __grid_constant__ Forward<T> p) {
   constexpr int kBatch = 2;
   extern __shared__ uint4 smem[];
@@ -545,8 +559,8 @@ __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : 
   const T* src = p.x + (sh.row0 + at.r) * g.C + at.c0;
   const uint32_t step = (uint32_t)g.rp * g.C;
 #pragma unroll 4
-  for (int k = 0; k < sh.mine; ++k) slots.template fetch<VEC>(k, src + (uint32_t)k * step, at.left);
-  const Emitter<T, VEC, ACT, EXTRA> out(p, at, sh);
+  for (int k = 0; k < sh.mine; ++k) slots.template fetch<W>(k, src + (uint32_t)k * step, at.left);
+  const Emitter<T, W, ACT, EXTRA> out(p, at, sh);
   if constexpr (EXTRA >= WITH_RES_GATE)
     if (out.res)
       for (int k = 0; k < sh.mine; ++k) prefetch_l2(out.res + (out.first + (uint32_t)k * step));
@@ -579,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : 
     for (int u = 0; u < kBatch; ++u) {
       if (EXTRA == WITH_CODES || k + u < sh.mine) xs[u] = slots.get(min(k + u, g.iters - 1));
       if constexpr (EXTRA >= WITH_RES_GATE)
-        if (out.res && k + u < sh.mine) rs[u] = raw8_load<T, VEC>(out.res + (out.first + (uint32_t)(k + u) * step), at.left);
+        if (out.res && k + u < sh.mine) rs[u] = raw8_load<T, W>(out.res + (out.first + (uint32_t)(k + u) * step), at.left);
     }
     out.template turn<false>(k, sh.mine, false, affine, xs, rs);
   }
@@ -587,7 +601,7 @@ __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : 
 }
 
 // Streamed, first pass: moments of each group (with tiles > 1: of each channel) over a CTA's pixels.
-template <typename T, bool VEC>
+template <typename T, int W>
 __global__ void __launch_bounds__(kThreads, 3) moments_kernel(const __grid_constant__ Forward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
@@ -609,9 +623,9 @@ __global__ void __launch_bounds__(kThreads, 3) moments_kernel(const __grid_const
   const Slots<T> ring(smem);
   Moments m;
   Raw8<T> first{};
-  if (sh.mine > 0) first = raw8_load<T, VEC>(src + next, at.left);
+  if (sh.mine > 0) first = raw8_load<T, W>(src + next, at.left);
   auto issue = [&](int slot) {
-    ring.template fetch<VEC>(slot, src + next, at.left);
+    ring.template fetch<W>(slot, src + next, at.left);
     next += step;
   };
   Stream<kBatch>::start(sh.mine, issue);
@@ -683,7 +697,7 @@ __global__ void __launch_bounds__(1024) combine_kernel(const __grid_constant__ F
 
 // Streamed, second pass: y from x and the statistics, which every CTA of an image forms from the rows of sums itself (the same
 // bits everywhere; its first CTA writes them out) unless combine_kernel has.
-template <typename T, bool VEC, int ACT, int EXTRA>
+template <typename T, int W, int ACT, int EXTRA>
 __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : kPlainPerSm) apply_kernel(const __grid_constant__ Forward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
@@ -695,20 +709,20 @@ __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : 
   at.active = at.active && at.left > 0;
   if (at.left <= 0) { at.c0 = 0; at.left = 1; }
   const Share sh(g, at, n, part);
-  const Emitter<T, VEC, ACT, EXTRA> out(p, at, sh);
+  const Emitter<T, W, ACT, EXTRA> out(p, at, sh);
   const T* const x = p.x + sh.row0 * g.C;
   uint32_t next = out.first + (uint32_t)max(sh.mine - 1, 0) * out.step;
   auto issue = [&](int slot) {
-    ring.template fetch<VEC>(slot, x + next, at.left);
+    ring.template fetch<W>(slot, x + next, at.left);
     if constexpr (EXTRA >= WITH_RES_GATE)
-      if (out.res) res_ring.template fetch<VEC>(slot, out.res + next, at.left);
+      if (out.res) res_ring.template fetch<W>(slot, out.res + next, at.left);
     next -= out.step;
   };
   float gamma[8], beta[8];
-  if constexpr (VEC) Stream<kBatch>::start(sh.mine, issue);      // see grid_dependency_release in moments_kernel
+  if constexpr (kEarly<T, W>) Stream<kBatch>::start(sh.mine, issue);      // see grid_dependency_release in moments_kernel
   grid_dependency_wait();
   grid_dependency_release();
-  if constexpr (!VEC) Stream<kBatch>::start(sh.mine, issue);
+  if constexpr (!kEarly<T, W>) Stream<kBatch>::start(sh.mine, issue);
 #pragma unroll
   for (int i = 0; i < 8; ++i) { gamma[i] = p.gamma[at.channel(i)]; beta[i] = p.beta[at.channel(i)]; }
   if (!p.combined) {
@@ -868,7 +882,7 @@ __device__ __forceinline__ Raw8<T> dx_of(const Raw8<T>& dy, const Held<T, CK>& h
 
 // The operands of the streamed passes: rings of dy, x (or its codes), the mask and res, as far as a pass has them; the bytes
 // (scales, gate bits) come through registers, two turns ahead.
-template <typename T, bool VEC, bool CK> struct Feed {
+template <typename T, int W, bool CK> struct Feed {
   static constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   const Columns<T> from;
   const Slots<T> dys, xs, masks, ress;
@@ -906,14 +920,14 @@ template <typename T, bool VEC, bool CK> struct Feed {
   __device__ __forceinline__ void issue(int s) {
     const uint32_t o = next;
     next += step;
-    dys.template fetch<VEC>(s, from.dy + o, left);
+    dys.template fetch<W>(s, from.dy + o, left);
     if constexpr (CK) {
-      if constexpr (VEC) copy8_async(codes + s * kThreads, from.codes + o); else codes[s * kThreads] = load_codes<false>(from.codes + o, 0, left);
+      if constexpr (W == kWhole) copy8_async(codes + s * kThreads, from.codes + o); else codes[s * kThreads] = load_codes<kCodeWidth<T, W>>(from.codes + o, left);
     } else {
-      xs.template fetch<VEC>(s, from.x + o, left);
+      xs.template fetch<W>(s, from.x + o, left);
     }
-    if (slope == SLOPE_MASK) masks.template fetch<VEC>(s, from.mask + o, left);
-    if (res) ress.template fetch<VEC>(s, res + o, left);
+    if (slope == SLOPE_MASK) masks.template fetch<W>(s, from.mask + o, left);
+    if (res) ress.template fetch<W>(s, res + o, left);
   }
   __device__ __forceinline__ Held<T, CK> get(int slot, int u) const {
     Held<T, CK> h;
@@ -978,7 +992,7 @@ struct Sums {
 
 // The resident form.  Shared memory: the thread's vectors of dy and x (or its codes), a byte per vector for the gate's bits and
 // one for the scale; then per-thread sums, per-channel sums A, B and per-group sums S1, S2 of this CTA, and k1, k2 of the image.
-template <typename T, bool VEC, bool CK, int SLOPE>
+template <typename T, int W, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_constant__ Backward<T> p) {
   constexpr int kBatch = 2;
   extern __shared__ uint4 smem[];
@@ -1004,11 +1018,11 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
 #pragma unroll 4
   for (int k = 0; k < sh.mine; ++k) {
     const uint32_t o = from.first + (uint32_t)k * from.step;
-    dys.template fetch<VEC>(k, from.dy + o, at.left);
+    dys.template fetch<W>(k, from.dy + o, at.left);
     if constexpr (CK) {
-      if constexpr (VEC) copy8_async(cs + k * kThreads + tid, from.codes + o); else cs[k * kThreads + tid] = load_codes<false>(from.codes + o, 0, at.left);
+      if constexpr (W == kWhole) copy8_async(cs + k * kThreads + tid, from.codes + o); else cs[k * kThreads + tid] = load_codes<kCodeWidth<T, W>>(from.codes + o, at.left);
     } else {
-      xslots.template fetch<VEC>(k, from.x + o, at.left);
+      xslots.template fetch<W>(k, from.x + o, at.left);
     }
   }
   const T* const res = p.res ? p.res + sh.row0 * g.C : nullptr;
@@ -1027,7 +1041,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
         if (k0 + u < sh.mine) {
           if constexpr (CK) sc[u] = from.scales[from.scale_first + (uint32_t)(k0 + u) * from.scale_step];
           if (slope == SLOPE_BITS) bits[u] = from.gate[from.gate_first + (uint32_t)(k0 + u) * from.gate_step];
-          if (slope == SLOPE_MASK) m[u] = raw8_load<T, VEC>(from.mask + (from.first + (uint32_t)(k0 + u) * from.step), at.left);
+          if (slope == SLOPE_MASK) m[u] = raw8_load<T, W>(from.mask + (from.first + (uint32_t)(k0 + u) * from.step), at.left);
         }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -1100,19 +1114,19 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
     Raw8<T> rs[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      if (res && k + u < sh.mine) rs[u] = raw8_load<T, VEC>(res + (from.first + (uint32_t)(k + u) * from.step), at.left);
+      if (res && k + u < sh.mine) rs[u] = raw8_load<T, W>(res + (from.first + (uint32_t)(k + u) * from.step), at.left);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (k + u < sh.mine) {
         const Held<T, CK> h = held(k + u);
-        raw8_put<T, VEC>(dx + (from.first + (uint32_t)(k + u) * from.step), at.left, dx_of<T, CK>(h.dy, h, slope, ch, k1, k2, res ? &rs[u] : nullptr));
+        raw8_put<T, W>(dx + (from.first + (uint32_t)(k + u) * from.step), at.left, dx_of<T, CK>(h.dy, h, slope, ch, k1, k2, res ? &rs[u] : nullptr));
       }
   }
   cluster.barrier_wait(std::move(token));
 }
 
 // Streamed, first pass: A and B of each channel over a CTA's pixels.
-template <typename T, bool VEC, bool CK, int SLOPE>
+template <typename T, int W, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid_constant__ Backward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
@@ -1125,7 +1139,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
   const Share sh(g, at, n, part);
   grid_dependency_wait();
   grid_dependency_release();
-  Feed<T, VEC, CK> feed(p, at, sh, slope, nullptr, false, smem);
+  Feed<T, W, CK> feed(p, at, sh, slope, nullptr, false, smem);
   feed.template bytes<false>(0, 0);
   feed.template bytes<false>(kBatch, kBatch);
   Channels ch;
@@ -1187,12 +1201,12 @@ __global__ void __launch_bounds__(1024) add_rows_kernel(const float* __restrict_
 
 // Streamed, second pass: dx.  Every CTA forms S1 and S2 of its tile's groups from the image's totals, or from its rows of sums.
 // The CTAs behind the last share of an image (blockIdx.y = parts) add up the parameter gradients.
-template <typename T, bool VEC, bool CK, int SLOPE>
+template <typename T, int W, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __grid_constant__ Backward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
-  float* coef = reinterpret_cast<float*>(smem + Feed<T, VEC, CK>::words((SLOPE < 0 ? p.slope : SLOPE) == SLOPE_MASK, p.res != nullptr));   // [2][sets]
+  float* coef = reinterpret_cast<float*>(smem + Feed<T, W, CK>::words((SLOPE < 0 ? p.slope : SLOPE) == SLOPE_MASK, p.res != nullptr));   // [2][sets]
   const int slope = SLOPE < 0 ? p.slope : SLOPE;
   const int part = blockIdx.y, n = blockIdx.x;
   const int c_first = blockIdx.z * kMaxCols * 8;
@@ -1210,12 +1224,12 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   const Share sh(g, at, n, part);
   const int c_last = min(g.C, c_first + g.cols * 8) - 1;
   const int g_first = c_first / g.Cg, sets = c_last / g.Cg - g_first + 1, c_base = g_first * g.Cg;
-  Feed<T, VEC, CK> feed(p, at, sh, slope, p.res, true, smem);
-  if constexpr (VEC) Stream<kBatch>::start(sh.mine, [&](int slot) { feed.issue(slot); });
+  Feed<T, W, CK> feed(p, at, sh, slope, p.res, true, smem);
+  if constexpr (kEarly<T, W>) Stream<kBatch>::start(sh.mine, [&](int slot) { feed.issue(slot); });
   grid_dependency_wait();
   grid_dependency_release();
   auto issue = [&](int slot) { feed.issue(slot); };
-  if constexpr (!VEC) Stream<kBatch>::start(sh.mine, issue);
+  if constexpr (!kEarly<T, W>) Stream<kBatch>::start(sh.mine, issue);
   feed.template bytes<false>(0, 0);
   feed.template bytes<false>(kBatch, kBatch);
   Channels ch;
@@ -1256,7 +1270,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
         const Held<T, CK> h = feed.get(slot, u);
         Raw8<T> r;
         if (feed.res) r = feed.ress.get(slot + u);
-        raw8_put<T, VEC>(dx + o, at.left,
+        raw8_put<T, W>(dx + o, at.left,
                          dx_of<T, CK>(passed<T, CK>(h, slope), h, slope, ch, k1, k2, feed.res ? &r : nullptr));
         o += feed.step;
       }
@@ -1354,35 +1368,35 @@ inline cudaError_t launch_cluster(Kernel kernel, int images, int cluster, size_t
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-template <typename T, bool VEC, int ACT, int EXTRA> inline cudaError_t launch_forward_as(cudaStream_t st, const Plan& pl, Forward<T> p) {
+template <typename T, int W, int ACT, int EXTRA> inline cudaError_t launch_forward_as(cudaStream_t st, const Plan& pl, Forward<T> p) {
   const Geom& g = pl.g;
   if (pl.resident) {
     static OncePerDevice once;
-    const cudaError_t e = once_per_device(&once, []() { return set_smem_limit(forward_kernel<T, VEC, ACT, EXTRA>, kSmemMost); });
-    return e != cudaSuccess ? e : launch_cluster(forward_kernel<T, VEC, ACT, EXTRA>, g.N, g.parts, pl.smem, st, p);
+    const cudaError_t e = once_per_device(&once, []() { return set_smem_limit(forward_kernel<T, W, ACT, EXTRA>, kSmemMost); });
+    return e != cudaSuccess ? e : launch_cluster(forward_kernel<T, W, ACT, EXTRA>, g.N, g.parts, pl.smem, st, p);
   }
   static OncePerDevice once;
   cudaError_t e = once_per_device(&once, []() {
-    const cudaError_t f = set_smem_limit(moments_kernel<T, VEC>, kSmemMost);
-    return f != cudaSuccess ? f : set_smem_limit(apply_kernel<T, VEC, ACT, EXTRA>, kSmemMost);
+    const cudaError_t f = set_smem_limit(moments_kernel<T, W>, kSmemMost);
+    return f != cudaSuccess ? f : set_smem_limit(apply_kernel<T, W, ACT, EXTRA>, kSmemMost);
   });
   if (e != cudaSuccess) return e;
   const dim3 grid((unsigned)g.N, (unsigned)g.parts, (unsigned)g.tiles);
   const size_t ring = (size_t)ring_of<T>() * kThreads * 8 * sizeof(T);
-  e = launch_chained(moments_kernel<T, VEC>, grid, dim3(kThreads), ring + 3 * kThreads * 8 * 4 + 64 * (size_t)g.cols, st, p);
+  e = launch_chained(moments_kernel<T, W>, grid, dim3(kThreads), ring + 3 * kThreads * 8 * 4 + 64 * (size_t)g.cols, st, p);
   p.combined = !merges(g);
   if (e == cudaSuccess && p.combined) {
     const int64_t entries = (int64_t)g.parts * (g.tiles == 1 ? 1 : g.Cg);
     e = launch_chained(combine_kernel<T>, dim3((unsigned)(g.N * g.G)), dim3(32 * pow2_up_to(entries / 64, 32)), 0, st, p);
   }
   if (e == cudaSuccess)
-    e = launch_chained(apply_kernel<T, VEC, ACT, EXTRA>, grid, dim3(kThreads), (p.res ? 2 : 1) * ring + (p.combined ? 0 : 8 * (size_t)g.G), st, p);
+    e = launch_chained(apply_kernel<T, W, ACT, EXTRA>, grid, dim3(kThreads), (p.res ? 2 : 1) * ring + (p.combined ? 0 : 8 * (size_t)g.G), st, p);
   return e;
 }
 
 template <typename T, int ACT> inline cudaError_t launch_forward_act(cudaStream_t st, const Plan& pl, const Forward<T>& p) {
-  return p.codes ? launch_forward_as<T, true, ACT, WITH_CODES>(st, pl, p)
-                 : p.res || p.gate ? launch_forward_as<T, true, ACT, WITH_RES_GATE>(st, pl, p) : launch_forward_as<T, true, ACT, PLAIN>(st, pl, p);
+  return p.codes ? launch_forward_as<T, kWhole, ACT, WITH_CODES>(st, pl, p)
+                 : p.res || p.gate ? launch_forward_as<T, kWhole, ACT, WITH_RES_GATE>(st, pl, p) : launch_forward_as<T, kWhole, ACT, PLAIN>(st, pl, p);
 }
 template <typename T>
 inline cudaError_t launch_forward(cudaStream_t st, const Plan& pl, Forward<T> p) {
@@ -1391,34 +1405,36 @@ inline cudaError_t launch_forward(cudaStream_t st, const Plan& pl, Forward<T> p)
   p.ckpt_lanes = p.codes ? ckpt_block_lanes(C) : 0;
   int8_t* codes = p.codes;
   if (p.ckpt_lanes == 0) p.codes = nullptr;       // blocks that do not fall on groups of lanes: a pass of their own
-  const bool vec = C % 8 == 0 && aligned_to(p.x, 16) && aligned_to(p.y, 16) && aligned_to(p.res, 16) && aligned_to(p.codes, 8);
-  cudaError_t e = !vec ? launch_forward_as<T, false, -1, WITH_CODES>(st, pl, p)
-                         : p.act == ACT_RELU ? launch_forward_act<T, ACT_RELU>(st, pl, p)
-                         : p.act == ACT_SILU ? launch_forward_act<T, ACT_SILU>(st, pl, p) : launch_forward_act<T, ACT_NONE>(st, pl, p);
+  const int w = access_width<T>(C, {p.x, p.y, p.res}, p.codes);
+  cudaError_t e = w == 8 ? launch_forward_as<T, 8, -1, WITH_CODES>(st, pl, p)
+                  : w == 4 ? launch_forward_as<T, 4, -1, WITH_CODES>(st, pl, p)
+                  : w != kWhole ? launch_forward_as<T, sizeof(T), -1, WITH_CODES>(st, pl, p)
+                  : p.act == ACT_RELU ? launch_forward_act<T, ACT_RELU>(st, pl, p)
+                  : p.act == ACT_SILU ? launch_forward_act<T, ACT_SILU>(st, pl, p) : launch_forward_act<T, ACT_NONE>(st, pl, p);
   if (e == cudaSuccess && codes && !p.codes) e = launch_ckpt_encode<T>(st, p.x, (size_t)p.g.N * p.g.P, C, codes, p.scales);
   return e;
 }
 
-template <typename T, bool VEC, bool CK, int SLOPE>
+template <typename T, int W, bool CK, int SLOPE>
 inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<T> p) {
   const Geom& g = pl.g;
   const int width = 2 * g.C, blocks = (width + 31) / 32;
   if (pl.resident) {
     static OncePerDevice once;
-    cudaError_t e = once_per_device(&once, []() { return set_smem_limit(backward_kernel<T, VEC, CK, SLOPE>, kSmemMost); });
-    if (e == cudaSuccess) e = launch_cluster(backward_kernel<T, VEC, CK, SLOPE>, g.N, g.parts, pl.smem, st, p);
+    cudaError_t e = once_per_device(&once, []() { return set_smem_limit(backward_kernel<T, W, CK, SLOPE>, kSmemMost); });
+    if (e == cudaSuccess) e = launch_cluster(backward_kernel<T, W, CK, SLOPE>, g.N, g.parts, pl.smem, st, p);
     if (e == cudaSuccess)
       e = launch_chained(add_rows_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, (const float*)p.totals, g.N, width, p.dgamma, p.dbeta, g.C);
     return e;
   }
   static OncePerDevice once;
   cudaError_t e = once_per_device(&once, []() {
-    const cudaError_t f = set_smem_limit(backward_sums_kernel<T, VEC, CK, SLOPE>, kSmemMost);
-    return f != cudaSuccess ? f : set_smem_limit(backward_apply_kernel<T, VEC, CK, SLOPE>, kSmemMost);
+    const cudaError_t f = set_smem_limit(backward_sums_kernel<T, W, CK, SLOPE>, kSmemMost);
+    return f != cudaSuccess ? f : set_smem_limit(backward_apply_kernel<T, W, CK, SLOPE>, kSmemMost);
   });
-  auto rings = [&](bool res) { return 16 * (size_t)Feed<T, VEC, CK>::words(p.slope == SLOPE_MASK, res); };
+  auto rings = [&](bool res) { return 16 * (size_t)Feed<T, W, CK>::words(p.slope == SLOPE_MASK, res); };
   if (e == cudaSuccess)
-    e = launch_chained(backward_sums_kernel<T, VEC, CK, SLOPE>, dim3((unsigned)g.N, (unsigned)g.parts, (unsigned)g.tiles), dim3(kThreads),
+    e = launch_chained(backward_sums_kernel<T, W, CK, SLOPE>, dim3((unsigned)g.N, (unsigned)g.parts, (unsigned)g.tiles), dim3(kThreads),
                        std::max(rings(false), (size_t)2 * kThreads * 8 * 4), st, p);
   if (merges(g)) p.totals = nullptr;
   else if (e == cudaSuccess)
@@ -1427,26 +1443,27 @@ inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<
   // coefficients of the tile's groups; with one tile also the channels' sums
   const size_t own = 8 * (size_t)std::min(g.G, g.cols * 8) + (g.tiles == 1 ? 8 * (size_t)g.C : 0);
   if (e == cudaSuccess)
-    e = launch_chained(backward_apply_kernel<T, VEC, CK, SLOPE>, dim3((unsigned)g.N, (unsigned)g.parts + 1, (unsigned)g.tiles), dim3(kThreads),
+    e = launch_chained(backward_apply_kernel<T, W, CK, SLOPE>, dim3((unsigned)g.N, (unsigned)g.parts + 1, (unsigned)g.tiles), dim3(kThreads),
                        rings(p.res != nullptr) + own, st, p);
   return e;
 }
-template <typename T, bool CK>
-inline cudaError_t launch_backward_of(cudaStream_t st, const Plan& pl, const Backward<T>& p, bool vec) {
-  if (!vec) return launch_backward_as<T, false, CK, -1>(st, pl, p);
+template <typename T, bool CK> inline cudaError_t launch_backward_of(cudaStream_t st, const Plan& pl, const Backward<T>& p) {
+  switch (access_width<T>(p.g.C, {p.dy, p.x, p.mask, p.res, p.dx}, p.codes)) {
+    case kWhole: break;
+    case 8: return launch_backward_as<T, 8, CK, -1>(st, pl, p);
+    case 4: return launch_backward_as<T, 4, CK, -1>(st, pl, p);
+    default: return launch_backward_as<T, sizeof(T), CK, -1>(st, pl, p);
+  }
   switch (p.slope) {
-    case SLOPE_MASK: return launch_backward_as<T, true, CK, SLOPE_MASK>(st, pl, p);
-    case SLOPE_BITS: return launch_backward_as<T, true, CK, SLOPE_BITS>(st, pl, p);
-    case SLOPE_SILU: return launch_backward_as<T, true, CK, SLOPE_SILU>(st, pl, p);
-    default: return launch_backward_as<T, true, CK, SLOPE_ONE>(st, pl, p);
+    case SLOPE_MASK: return launch_backward_as<T, kWhole, CK, SLOPE_MASK>(st, pl, p);
+    case SLOPE_BITS: return launch_backward_as<T, kWhole, CK, SLOPE_BITS>(st, pl, p);
+    case SLOPE_SILU: return launch_backward_as<T, kWhole, CK, SLOPE_SILU>(st, pl, p);
+    default: return launch_backward_as<T, kWhole, CK, SLOPE_ONE>(st, pl, p);
   }
 }
-template <typename T>
-inline cudaError_t launch_backward(cudaStream_t st, const Plan& pl, Backward<T> p) {
+template <typename T> inline cudaError_t launch_backward(cudaStream_t st, const Plan& pl, Backward<T> p) {
   p.g = pl.g;
-  const bool vec = p.g.C % 8 == 0 && aligned_to(p.dy, 16) && aligned_to(p.x, 16) && aligned_to(p.codes, 8) && aligned_to(p.mask, 16) &&
-                   aligned_to(p.res, 16) && aligned_to(p.dx, 16);
-  return p.codes ? launch_backward_of<T, true>(st, pl, p, vec) : launch_backward_of<T, false>(st, pl, p, vec);
+  return p.codes ? launch_backward_of<T, true>(st, pl, p) : launch_backward_of<T, false>(st, pl, p);
 }
 
 }  // namespace gn

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "once_per_device.h"
 
@@ -59,31 +60,54 @@ template <> __device__ __forceinline__ float from_f<float>(float x) { return x; 
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
 // Eight consecutive values of a row in the storage type (16 or 32 bytes), as the kernels on columns of 8 channels move them.
-// VEC: the row is a whole number of such vectors and 16-byte aligned; otherwise the first `left` values exist, one by one,
-// and the rest read as zero.
-template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };
-template <typename T, bool VEC> __device__ __forceinline__ Raw8<T> raw8_load(const T* __restrict__ p, int left) {
+// W = kWhole: rows are whole numbers of such vectors, aligned to their size.  Otherwise rows and bases are multiples of W bytes
+// (8, 4, or an element), the first `left` values exist, and the rest read as zero.
+constexpr int kWhole = 16;
+template <typename T> struct alignas(8 * sizeof(T)) Raw8 { uint4 q[sizeof(T) / 2]; };
+template <int W> struct Piece;
+template <> struct Piece<8> { typedef uint2 Type; };
+template <> struct Piece<4> { typedef uint32_t Type; };
+template <> struct Piece<2> { typedef uint16_t Type; };
+template <typename T, int W> __device__ __forceinline__ Raw8<T> raw8_load(const T* __restrict__ p, int left) {
   Raw8<T> r;
-  if constexpr (VEC) {
-#pragma unroll
-    for (int j = 0; j < (int)sizeof(T) / 2; ++j) r.q[j] = reinterpret_cast<const uint4*>(p)[j];
+  if constexpr (W == kWhole && sizeof(T) == 4) {         // one 256-bit access: two of 128 bits would each touch every sector
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r.q[0].x), "=r"(r.q[0].y), "=r"(r.q[0].z), "=r"(r.q[0].w), "=r"(r.q[1].x), "=r"(r.q[1].y), "=r"(r.q[1].z), "=r"(r.q[1].w)
+                 : "l"(p));
+  } else if constexpr (W == kWhole) {
+    r.q[0] = *reinterpret_cast<const uint4*>(p);
   } else {
-    T* e = reinterpret_cast<T*>(&r);
+    typedef typename Piece<W>::Type P;
+    constexpr int PER = W / (int)sizeof(T);
+    P* e = reinterpret_cast<P*>(&r);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] = i < left ? p[i] : from_f<T>(0.f);
+    for (int i = 0; i < 8 / PER; ++i) e[i] = i * PER < left ? reinterpret_cast<const P*>(p)[i] : P{};
   }
   return r;
 }
-template <typename T, bool VEC> __device__ __forceinline__ void raw8_put(T* __restrict__ p, int left, const Raw8<T>& r) {
-  if constexpr (VEC) {
-#pragma unroll
-    for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(p)[j] = r.q[j];
+template <typename T, int W> __device__ __forceinline__ void raw8_put(T* __restrict__ p, int left, const Raw8<T>& r) {
+  if constexpr (W == kWhole && sizeof(T) == 4) {
+    asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r.q[0].x), "r"(r.q[0].y), "r"(r.q[0].z), "r"(r.q[0].w),
+                 "r"(r.q[1].x), "r"(r.q[1].y), "r"(r.q[1].z), "r"(r.q[1].w), "l"(p)
+                 : "memory");
+  } else if constexpr (W == kWhole) {
+    *reinterpret_cast<uint4*>(p) = r.q[0];
   } else {
-    const T* e = reinterpret_cast<const T*>(&r);
+    typedef typename Piece<W>::Type P;
+    constexpr int PER = W / (int)sizeof(T);
+    const P* e = reinterpret_cast<const P*>(&r);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) p[i] = e[i];
+    for (int i = 0; i < 8 / PER; ++i)
+      if (i * PER < left) reinterpret_cast<P*>(p)[i] = e[i];
   }
+}
+inline bool aligned_to(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+// W for rows of C values and these tensors (null ones do not count); `bytes`: a tensor of rows of C bytes, which is moved in
+// pieces of W / sizeof(T).
+template <typename T> inline int access_width(int C, std::initializer_list<const void*> tensors, const void* bytes = nullptr) {
+  uintptr_t bits = (uintptr_t)C * sizeof(T) | reinterpret_cast<uintptr_t>(bytes) * sizeof(T);
+  for (const void* t : tensors) bits |= reinterpret_cast<uintptr_t>(t);
+  return bits % (8 * sizeof(T)) == 0 ? kWhole : bits % 8 == 0 ? 8 : bits % 4 == 0 ? 4 : (int)sizeof(T);
 }
 
 // Pairs of fp32 values in one 64-bit register pair.  sm_100a adds, multiplies and multiply-adds both halves with one
