@@ -15,14 +15,13 @@
 // and end anywhere inside a column (5 channels of 160, say): sums are formed per channel and thread and added per group from
 // shared memory.
 //
-// Two forms, chosen by plan():
-//   resident  a cluster of up to 8 CTAs takes an image, each a share of its pixels, which it copies to shared memory at once
-//             (cp.async, every thread its own vectors, so nothing but a thread's own wait stands between copy and use).  The
-//             sums are formed there, exchanged through distributed shared memory, and applied from there: one launch, one
-//             read, one write.
-//   streamed  as many CTAs as run at once, each a contiguous share of an image's pixels: one pass forms the sums, leaves a row
-//             of them per CTA in scratch, and a second pass adds the rows up and applies them, walking its pixels backwards, so
-//             that it starts with what L2 holds.
+// Streamed, both passes: as many CTAs as run at once, each a contiguous share of an image's pixels.  One kernel forms the sums
+// and leaves a row of them per CTA in scratch; a second adds the rows up and applies them, walking its pixels backwards, so that
+// it starts with what L2 holds, and starting its copies before the first has ended.  Vectors come through rings in shared memory.
+// Resident, forward only (plan_forward): a cluster of up to 8 CTAs takes an image, each a share of its pixels, which it copies to
+// shared memory at once (every thread its own vectors, so nothing but a thread's own wait stands between copy and use).  The
+// moments are formed there, exchanged through distributed shared memory, and applied from there: one launch, one read, one write.
+// (A resident backward pass was no faster anywhere: its parameter gradients need a second launch all the same.)
 //
 // Variance: a thread sums its values and their squares less its first value, brings them about a common value of the CTA (the
 // mean of the channel's first row of threads), then about the CTA's group mean, and CTAs are combined by Chan's formula.  The
@@ -31,7 +30,6 @@
 // All sums are fp32 within a CTA (a chain of a thread's values, then of rows of threads, then a tree), in a fixed order.
 #pragma once
 #include <cooperative_groups.h>
-#include <stdlib.h>
 
 #include "ckpt8.cuh"
 #include "kernel_common.cuh"
@@ -770,8 +768,8 @@ template <typename T> struct Backward {
   const uint8_t* gate;
   const T* res;
   T* dx;
-  float* partial;             // streamed: [N][parts][2][C]: A, B of each CTA
-  float* totals;              // [N][2][C]: A, B of each image; streamed: null if the second pass adds up the rows itself
+  float* partial;             // [N][parts][2][C]: A, B of each CTA
+  float* totals;              // [N][2][C]: A, B of each image, or null if the second pass adds up the rows itself
   float* dgamma;
   float* dbeta;
   int slope;
@@ -880,7 +878,7 @@ __device__ __forceinline__ Raw8<T> dx_of(const Raw8<T>& dy, const Held<T, CK>& h
   return f8_to_raw8<T>(dz);
 }
 
-// The operands of the streamed passes: rings of dy, x (or its codes), the mask and res, as far as a pass has them; the bytes
+// The operands of a pass: rings of dy, x (or its codes), the mask and res, as far as a pass has them; the bytes
 // (scales, gate bits) come through registers, two turns ahead.
 template <typename T, int W, bool CK> struct Feed {
   static constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
@@ -990,142 +988,7 @@ struct Sums {
   }
 };
 
-// The resident form.  Shared memory: the thread's vectors of dy and x (or its codes), a byte per vector for the gate's bits and
-// one for the scale; then per-thread sums, per-channel sums A, B and per-group sums S1, S2 of this CTA, and k1, k2 of the image.
-template <typename T, int W, bool CK, int SLOPE>
-__global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_constant__ Backward<T> p) {
-  constexpr int kBatch = 2;
-  extern __shared__ uint4 smem[];
-  const Geom& g = p.g;
-  const int slope = SLOPE < 0 ? p.slope : SLOPE;
-  const size_t vecs = (size_t)g.iters * kThreads;
-  uint4* xs = smem + vecs * Slots<T>::Q;
-  uint2* cs = reinterpret_cast<uint2*>(xs);
-  float* red = reinterpret_cast<float*>(CK ? reinterpret_cast<uint4*>(cs + vecs) : xs + vecs * Slots<T>::Q);   // [2][2048]
-  float* chan = red + 2 * kThreads * 8;       // [2][C]
-  float* gamma = chan + 2 * g.C;              // [C]
-  float* own = gamma + g.C;                   // [2][G]
-  float* coef = own + 2 * g.G;                // [2][G]
-  uint8_t* open = reinterpret_cast<uint8_t*>(coef + 2 * g.G);
-  uint8_t* scale_bytes = open + vecs;
-  const int rank = blockIdx.y, n = blockIdx.x, tid = threadIdx.x;
-  const Place at(g, 0);
-  const Share sh(g, at, n, rank);
-  const Slots<T> dys(smem), xslots(xs);
-  const Columns<T> from(p, at, sh);
-  grid_dependency_wait();
-  grid_dependency_release();
-#pragma unroll 4
-  for (int k = 0; k < sh.mine; ++k) {
-    const uint32_t o = from.first + (uint32_t)k * from.step;
-    dys.template fetch<W>(k, from.dy + o, at.left);
-    if constexpr (CK) {
-      if constexpr (W == kWhole) copy8_async(cs + k * kThreads + tid, from.codes + o); else cs[k * kThreads + tid] = load_codes<kCodeWidth<T, W>>(from.codes + o, at.left);
-    } else {
-      xslots.template fetch<W>(k, from.x + o, at.left);
-    }
-  }
-  const T* const res = p.res ? p.res + sh.row0 * g.C : nullptr;
-  if (res)
-    for (int k = 0; k < sh.mine; ++k) prefetch_l2(res + (from.first + (uint32_t)k * from.step));
-  // what comes in bytes goes through registers, several loads in flight
-  if (slope == SLOPE_MASK)
-    for (int k = 0; k < sh.mine; ++k) prefetch_l2(from.mask + (from.first + (uint32_t)k * from.step));
-  if (CK || slope == SLOPE_MASK || slope == SLOPE_BITS) {
-    constexpr int U = sizeof(T) == 2 ? 8 : 4;
-    for (int k0 = 0; k0 < sh.mine; k0 += U) {
-      uint32_t sc[U], bits[U];
-      Raw8<T> m[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (k0 + u < sh.mine) {
-          if constexpr (CK) sc[u] = from.scales[from.scale_first + (uint32_t)(k0 + u) * from.scale_step];
-          if (slope == SLOPE_BITS) bits[u] = from.gate[from.gate_first + (uint32_t)(k0 + u) * from.gate_step];
-          if (slope == SLOPE_MASK) m[u] = raw8_load<T, W>(from.mask + (from.first + (uint32_t)(k0 + u) * from.step), at.left);
-        }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (k0 + u < sh.mine) {
-          if constexpr (CK) scale_bytes[(k0 + u) * kThreads + tid] = (uint8_t)sc[u];
-          if (slope == SLOPE_BITS) open[(k0 + u) * kThreads + tid] = (uint8_t)bits[u];
-          if (slope == SLOPE_MASK) open[(k0 + u) * kThreads + tid] = (uint8_t)positive_bits(m[u]);
-        }
-    }
-  }
-  Channels ch;
-  float rstd[8];
-  load_channels(p, at, n, slope, ch, rstd);
-  copies_done();
-  for (int c = tid; c < g.C; c += kThreads) gamma[c] = p.gamma[c];
-  auto held = [&](uint32_t k) {
-    Held<T, CK> h;
-    h.dy = dys.get(k);
-    if constexpr (CK) {
-      h.codes = cs[k * kThreads + tid];
-      h.scale = scale_bytes[k * kThreads + tid];
-    } else {
-      h.x = xslots.get(k);
-    }
-    return h;
-  };
-  Sums sums;
-#pragma unroll 2
-  for (int k = 0; k < sh.mine; ++k) {
-    Held<T, CK> h = held(k);
-    if (slope == SLOPE_MASK || slope == SLOPE_BITS) {
-      h.dy = opened(h.dy, open[k * kThreads + tid]);
-      dys.put(k, h.dy);                           // gated once, for the second sweep too
-    }
-    F8 dz, d;
-    operands<T, CK>(h.dy, h, slope, ch, dz, d);
-    sums.add(dz, d);
-  }
-  sums.put(red, g, at, rstd);
-  __syncthreads();
-  channel_sums(red, g, g.C, g.lanes_c, [&](int c, float a, float b) { chan[c] = a; chan[g.C + c] = b; });
-  __syncthreads();
-  group_sums(g.G, g.Cg, g.lanes_g, [&](int c) { const float w = gamma[c]; return make_float2(w * chan[g.C + c], w * chan[c]); },
-             [&](int s, float s1, float s2) { own[s] = s1; own[g.G + s] = s2; });
-  cg::cluster_group cluster = cg::this_cluster();
-  cluster.sync();
-  for (int s = tid; s < g.G; s += kThreads) {
-    float s1 = 0.f, s2 = 0.f;
-    for (int j = 0; j < g.parts; ++j) {
-      const float* other = cluster.map_shared_rank(own, j);
-      s1 += other[s]; s2 += other[g.G + s];
-    }
-    const float r = p.stats[(size_t)(g.N + n) * g.G + s];
-    coef[s] = r * s1 * g.inv_m;
-    coef[g.G + s] = r * r * s2 * g.inv_m;
-  }
-  // each CTA of the cluster adds up a share of the channels for the parameter gradients
-  const int share = (2 * g.C + g.parts - 1) / g.parts;
-  for (int c = rank * share + tid; c < min((rank + 1) * share, 2 * g.C); c += kThreads) {
-    float t = 0.f;
-    for (int j = 0; j < g.parts; ++j) t += cluster.map_shared_rank(chan, j)[c];
-    p.totals[(size_t)n * 2 * g.C + c] = t;
-  }
-  cg::cluster_group::arrival_token token = cluster.barrier_arrive();
-  __syncthreads();
-  f32x2 k1[4], k2[4];
-  load_coefficients(g, at, coef, coef + g.G, 0, k1, k2);
-  T* const dx = p.dx + sh.row0 * g.C;
-  for (int k = 0; k < sh.mine; k += kBatch) {
-    Raw8<T> rs[kBatch];
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (res && k + u < sh.mine) rs[u] = raw8_load<T, W>(res + (from.first + (uint32_t)(k + u) * from.step), at.left);
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (k + u < sh.mine) {
-        const Held<T, CK> h = held(k + u);
-        raw8_put<T, W>(dx + (from.first + (uint32_t)(k + u) * from.step), at.left, dx_of<T, CK>(h.dy, h, slope, ch, k1, k2, res ? &rs[u] : nullptr));
-      }
-  }
-  cluster.barrier_wait(std::move(token));
-}
-
-// Streamed, first pass: A and B of each channel over a CTA's pixels.
+// First pass: A and B of each channel over a CTA's pixels.
 template <typename T, int W, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid_constant__ Backward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
@@ -1186,21 +1049,18 @@ __device__ __forceinline__ void add_rows(const float* __restrict__ in, int rows,
   }
   __syncthreads();
 }
-// out[j][i] = the sum of `rows` rows of `width` floats from in[j * rows] on, j = blockIdx.x / blocks.  Streamed, between the passes
-// where an image has many rows; resident, the parameter gradients (`split` > 0: values from there on go to out2).
-__global__ void __launch_bounds__(1024) add_rows_kernel(const float* __restrict__ in, int rows, int width, float* __restrict__ out,
-                                                        float* __restrict__ out2, int split) {
+// Between the passes where an image has many rows: totals[n][i] = the sum of the image's rows of sums, n = blockIdx.x / blocks.
+__global__ void __launch_bounds__(1024) totals_kernel(const float* __restrict__ partial, int rows, int width, float* __restrict__ totals) {
   __shared__ double fin[32][33];
-  const int blocks = (width + 31) / 32, j = blockIdx.x / blocks;
+  const int blocks = (width + 31) / 32, n = blockIdx.x / blocks;
   grid_dependency_wait();
   grid_dependency_release();
-  add_rows(in + (size_t)j * rows * width, rows, width, (blockIdx.x - j * blocks) * 32, fin, [&](int i, float v) {
-    if (split > 0 && i >= split) out2[i - split] = v; else out[(size_t)j * width + i] = v;
-  });
+  add_rows(partial + (size_t)n * rows * width, rows, width, (blockIdx.x - n * blocks) * 32, fin,
+           [&](int i, float v) { totals[(size_t)n * width + i] = v; });
 }
 
-// Streamed, second pass: dx.  Every CTA forms S1 and S2 of its tile's groups from the image's totals, or from its rows of sums.
-// The CTAs behind the last share of an image (blockIdx.y = parts) add up the parameter gradients.
+// Second pass: dx.  Every CTA forms S1 and S2 of its tile's groups from the image's totals, or from its rows of sums.
+// The CTAs behind the last image (blockIdx.x >= N) add up the parameter gradients, 32 values each.
 template <typename T, int W, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __grid_constant__ Backward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
@@ -1210,12 +1070,12 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   const int slope = SLOPE < 0 ? p.slope : SLOPE;
   const int part = blockIdx.y, n = blockIdx.x;
   const int c_first = blockIdx.z * kMaxCols * 8;
-  if (part == g.parts) {
+  if (n >= g.N) {
+    const int first = ((n - g.N) * g.parts + part) * 32;
     grid_dependency_wait();
-    if (blockIdx.z == 0)
-      for (int first = n * 32; first < 2 * g.C; first += g.N * 32)
-        add_rows(p.partial, g.N * g.parts, 2 * g.C, first, reinterpret_cast<double(*)[33]>(smem),
-                 [&](int i, float v) { (i < g.C ? p.dgamma + i : p.dbeta + (i - g.C))[0] = v; });
+    if (blockIdx.z == 0 && first < 2 * g.C)
+      add_rows(p.partial, g.N * g.parts, 2 * g.C, first, reinterpret_cast<double(*)[33]>(smem),
+               [&](int i, float v) { (i < g.C ? p.dgamma + i : p.dbeta + (i - g.C))[0] = v; });
     return;
   }
   Place at(g, blockIdx.z);
@@ -1291,9 +1151,17 @@ inline int pow2_up_to(int64_t most, int cap) {
 constexpr size_t kSmemMost = 220 * 1024;        // of 227 KB that a CTA can have
 constexpr size_t kSmemOfSm = 227 * 1024;
 
-// `vec_bytes`: shared memory per vector of 8 channels in the resident form; `fixed`: besides the vectors; `per_sm`: CTAs of the
-// streamed form on an SM.
-inline Plan plan(int N, int P, int C, int G, size_t vec_bytes, size_t fixed, int per_sm) {
+inline void split(Geom& g, int parts) {
+  g.parts = parts;
+  g.pix = g.P / parts + (g.P % parts != 0);
+  g.iters = g.pix / g.rp + (g.pix % g.rp != 0);
+  g.whole = g.pix / g.rp;
+  const int last = g.P % g.pix;
+  g.whole_last = last ? last / g.rp : g.whole;
+}
+// One wave of CTAs (`per_sm` on an SM), each with at least one batch of pixels in flight.  More waves of smaller shares cost
+// their start and end each, about 2.5 us: 23.2, 28.3 and 32.9 us with one, two and three waves (forward, 128 images of 32x32x160).
+inline Plan plan_streamed(int N, int P, int C, int G, int per_sm) {
   Plan pl{};
   Geom& g = pl.g;
   g.N = N; g.P = P; g.C = C; g.G = G; g.Cg = C / G;
@@ -1306,44 +1174,30 @@ inline Plan plan(int N, int P, int C, int G, size_t vec_bytes, size_t fixed, int
   g.cg_mul = g.Cg == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + g.Cg - 1) / g.Cg);      // exact for c * Cg < 2^32 (C <= 2^16)
   g.lanes_g = pow2_up_to(kThreads / std::min(G, kThreads), 32);
   g.lanes_c = pow2_up_to(kThreads / std::min(g.cols * 8, kThreads), 32);
-  auto shares = [&]() {
-    g.whole = g.pix / g.rp;
-    const int last = P % g.pix;
-    g.whole_last = last ? last / g.rp : g.whole;
-  };
-  auto split = [&](int parts) {
-    g.pix = P / parts + (P % parts != 0);
-    g.parts = parts;
-    g.iters = g.pix / g.rp + (g.pix % g.rp != 0);
-    return (size_t)g.iters * kThreads * vec_bytes + fixed;
-  };
-  const char* f_ = getenv("GN_FORM");
-  if (g.tiles == 1 && !(f_ && f_[0] == 's')) {
-    // as many CTAs per image as all run at once, while every thread keeps two pixels
-    for (int parts = kMaxCluster; parts >= 1; parts /= 2) {
-      pl.smem = split(parts);
-      if (parts > 1 && g.iters < 2) continue;
-      const int per = (int)std::min<size_t>(kSmemOfSm / (pl.smem + 1024), 2);
-      if (pl.smem <= kSmemMost && (int64_t)N * parts <= (int64_t)per * kSms) {
-        pl.resident = true;
-        shares();
-        return pl;
-      }
-    }
-  }
-  // one wave of CTAs, each with at least one batch of pixels in flight
-  split((int)std::max<int64_t>(1, std::min<int64_t>((int64_t)((getenv("GN_F")?atof(getenv("GN_F")):1.0)*per_sm * kSms) / N, P / (4 * g.rp))));
+  split(g, (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)per_sm * kSms / N, P / (4 * g.rp))));
   g.parts = P / g.pix + (P % g.pix != 0);         // none without pixels
-  shares();
   return pl;
 }
+// The resident form where an image fits a cluster and all of a call's CTAs run at once (two on an SM, if their shared memory
+// allows), with as many CTAs per image as that gives, and where they fill at least half of the SMs or a thread has few pixels.
+// us, resident / streamed, 16-bit storage: 8x16x16x8 4.6 / 5.4, 128x16x16x160 8.2 / 10.3, 128x8x8x640 8.7 / 10.8; on the other
+// side of the rule 2x64x64x128 with SiLU 12.2 / 10.0, and 128 images of 32x32x160 in more than one wave 31.5 / 23.4.
 inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G, bool codes) {
-  return plan(N, P, C, G, 8 * (size_t)elem_bytes, 3 * kThreads * 8 * 4 + 8 * (size_t)C + 16 * (size_t)G, codes ? kCodesPerSm : kPlainPerSm);
+  Plan pl = plan_streamed(N, P, C, G, codes ? kCodesPerSm : kPlainPerSm);
+  if (pl.g.tiles > 1) return pl;
+  Plan res = pl;
+  for (int parts = kMaxCluster; parts >= 1; parts /= 2) {
+    split(res.g, parts);
+    if (parts > 1 && res.g.iters < 2) continue;
+    res.smem = (size_t)res.g.iters * kThreads * 8 * elem_bytes + 3 * kThreads * 8 * 4 + 8 * (size_t)C + 16 * (size_t)G;
+    const int64_t per = std::min<size_t>(kSmemOfSm / (res.smem + 1024), 2), ctas = (int64_t)N * parts;
+    if (res.smem > kSmemMost || ctas > per * kSms) continue;
+    res.resident = ctas >= kSms / 2 || res.g.iters <= 4;
+    return res.resident ? res : pl;
+  }
+  return pl;
 }
-inline Plan plan_backward(int elem_bytes, int N, int P, int C, int G, bool ckpt) {
-  const size_t vec = 8 * (size_t)elem_bytes + (ckpt ? 8 : 8 * (size_t)elem_bytes) + 2;      // dy, x, a byte each for gate and scale
-  return plan(N, P, C, G, vec, 2 * kThreads * 8 * 4 + 12 * (size_t)C + 16 * (size_t)G, 2);
-}
+inline Plan plan_backward(int N, int P, int C, int G) { return plan_streamed(N, P, C, G, 2); }
 // Whether every launch's grid can be given.
 inline bool grid_ok(const Plan& pl) {
   const Geom& g = pl.g;
@@ -1419,31 +1273,23 @@ template <typename T, int W, bool CK, int SLOPE>
 inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<T> p) {
   const Geom& g = pl.g;
   const int width = 2 * g.C, blocks = (width + 31) / 32;
-  if (pl.resident) {
-    static OncePerDevice once;
-    cudaError_t e = once_per_device(&once, []() { return set_smem_limit(backward_kernel<T, W, CK, SLOPE>, kSmemMost); });
-    if (e == cudaSuccess) e = launch_cluster(backward_kernel<T, W, CK, SLOPE>, g.N, g.parts, pl.smem, st, p);
-    if (e == cudaSuccess)
-      e = launch_chained(add_rows_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, (const float*)p.totals, g.N, width, p.dgamma, p.dbeta, g.C);
-    return e;
-  }
   static OncePerDevice once;
   cudaError_t e = once_per_device(&once, []() {
     const cudaError_t f = set_smem_limit(backward_sums_kernel<T, W, CK, SLOPE>, kSmemMost);
     return f != cudaSuccess ? f : set_smem_limit(backward_apply_kernel<T, W, CK, SLOPE>, kSmemMost);
   });
+  if (e != cudaSuccess) return e;
   auto rings = [&](bool res) { return 16 * (size_t)Feed<T, W, CK>::words(p.slope == SLOPE_MASK, res); };
-  if (e == cudaSuccess)
-    e = launch_chained(backward_sums_kernel<T, W, CK, SLOPE>, dim3((unsigned)g.N, (unsigned)g.parts, (unsigned)g.tiles), dim3(kThreads),
-                       std::max(rings(false), (size_t)2 * kThreads * 8 * 4), st, p);
+  e = launch_chained(backward_sums_kernel<T, W, CK, SLOPE>, dim3((unsigned)g.N, (unsigned)g.parts, (unsigned)g.tiles), dim3(kThreads),
+                     std::max(rings(false), (size_t)2 * kThreads * 8 * 4), st, p);
   if (merges(g)) p.totals = nullptr;
   else if (e == cudaSuccess)
-    e = launch_chained(add_rows_kernel, dim3((unsigned)(g.N * blocks)), dim3(1024), 0, st, (const float*)p.partial, g.parts, width, p.totals,
-                       (float*)nullptr, 0);
+    e = launch_chained(totals_kernel, dim3((unsigned)(g.N * blocks)), dim3(1024), 0, st, (const float*)p.partial, g.parts, width, p.totals);
   // coefficients of the tile's groups; with one tile also the channels' sums
   const size_t own = 8 * (size_t)std::min(g.G, g.cols * 8) + (g.tiles == 1 ? 8 * (size_t)g.C : 0);
+  const int extra = (blocks + g.parts - 1) / g.parts;
   if (e == cudaSuccess)
-    e = launch_chained(backward_apply_kernel<T, W, CK, SLOPE>, dim3((unsigned)g.N, (unsigned)g.parts + 1, (unsigned)g.tiles), dim3(kThreads),
+    e = launch_chained(backward_apply_kernel<T, W, CK, SLOPE>, dim3((unsigned)(g.N + extra), (unsigned)g.parts, (unsigned)g.tiles), dim3(kThreads),
                        rings(p.res != nullptr) + own, st, p);
   return e;
 }
