@@ -58,21 +58,27 @@ struct Geom {
 constexpr int kMergeParts = 16;             // rows of sums that the second streamed pass adds up itself
 
 // ---- device helpers -------------------------------------------------------------------------------------
-// 1/(1 + exp(-z)).  For tensors in 16 bits from the approximate exponential and reciprocal (relative error below 2^-20 for
-// |z| < 16, growing with |z| as the rounding of z*log2(e) does), for fp32 ones from expf and a division.
-template <typename T> __device__ __forceinline__ float sigmoid(float z) {
+// 1/(1 + exp(-z)) of two values.  For tensors in 16 bits from the approximate exponential and reciprocal (relative error below
+// 2^-20 for |z| < 16, growing with |z| as the rounding of z*log2(e) does), for fp32 ones from expf and a division.  These
+// functions run at 16 values per SM and cycle, a quarter of what a streaming pass asks for, so two values share a reciprocal:
+// 1/a = b * 1/(ab).  The powers of two stop at 2^62, where ab and its reciprocal are still normal numbers: sigmoid(-43) is 2e-19.
+template <typename T> __device__ __forceinline__ f32x2 sigmoid(f32x2 z) {
   if constexpr (sizeof(T) == 2) {
-    float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
-    return r;
+    const float2 t = halves(mul2(z, pair(-1.44269504f)));
+    float a, b, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(fminf(t.x, 62.f)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(fminf(t.y, 62.f)));
+    const float2 d = halves(add2(pair(a, b), pair(1.f)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d.x * d.y));
+    return mul2(pair(r), pair(d.y, d.x));
   } else {
-    return 1.f / (1.f + expf(-z));
+    const float2 h = halves(z);
+    return pair(1.f / (1.f + expf(-h.x)), 1.f / (1.f + expf(-h.y)));
   }
 }
-template <typename T> __device__ __forceinline__ float silu_slope(float z) {
-  const float s = sigmoid<T>(z);
-  return s * fmaf(z, 1.f - s, 1.f);
+template <typename T> __device__ __forceinline__ f32x2 silu_slope(f32x2 z) {
+  const f32x2 s = sigmoid<T>(z);
+  return mul2(s, fma2(z, fma2(s, pair(-1.f), pair(1.f)), pair(1.f)));
 }
 
 __device__ __forceinline__ void copy16_async(void* smem, const void* gmem) {
@@ -483,10 +489,7 @@ template <typename T, int W, int ACT, int EXTRA> struct Emitter {
     } else {
       if (act == ACT_SILU) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 h = halves(z.p[j]);
-          z.p[j] = mul2(z.p[j], pair(sigmoid<T>(h.x), sigmoid<T>(h.y)));
-        }
+        for (int j = 0; j < 4; ++j) z.p[j] = mul2(z.p[j], sigmoid<T>(z.p[j]));
       }
       raw8_put<T, W>(y + o, left, f8_to_raw8<T>(z));
     }
@@ -856,8 +859,7 @@ __device__ __forceinline__ void operands(const Raw8<T>& dy, const Held<T, CK>& h
   if (slope == SLOPE_SILU) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float2 z = halves(fma2(d.p[j], ch.scale[j], ch.shift[j]));
-      dz.p[j] = mul2(dz.p[j], pair(silu_slope<T>(z.x), silu_slope<T>(z.y)));
+      dz.p[j] = mul2(dz.p[j], silu_slope<T>(fma2(d.p[j], ch.scale[j], ch.shift[j])));
     }
   }
 }
