@@ -555,7 +555,7 @@ class EwOps:
         self.lib = load_library()
         self.precision = precision
         self.dtype = torch.bfloat16 if precision == FDG_BF16_TC else torch.float32
-        self._gn_shapes = {}                     # (N, HW, C, groups, backward) -> (fdg_gn_shape by reference, scratch bytes)
+        self._gn_shapes, self._held_shapes = {}, {}          # what follows from a shape: see _gn, _blocks
 
     def _stream(self):
         return self.torch.cuda.current_stream().cuda_stream
@@ -618,12 +618,35 @@ class EwOps:
                        % (what, dtype, tuple(shape), t.dtype, tuple(t.shape), t.device))
 
     def _here(self):
-        """(current device, its current stream)."""
+        """(current device, its current stream): the calls that torch.cuda.current_stream() ends in, at a fortieth of its time."""
         dev = self.torch._C._cuda_getDevice()
         return dev, self.torch._C._cuda_getCurrentRawStream(dev)
 
+    @staticmethod
+    def _dense(*shape):
+        """(shape, strides) of a contiguous tensor."""
+        strides, n = [], 1
+        for v in reversed(shape):
+            strides.append(n)
+            n *= max(v, 1)
+        return shape, tuple(reversed(strides))
+
+    def _blocks(self, shape):
+        """(rows, channels, layout of the scales) of a tensor [.., C] held in 8 bits."""
+        got = self._held_shapes.get(shape)
+        if got is None:
+            if len(shape) < 1 or shape[-1] >= 2 ** 31:
+                raise FDGError(1, "expected a tensor [.., C], got %s" % (tuple(shape),))
+            ch, rows = shape[-1], 1
+            for v in shape[:-1]:
+                rows *= v
+            if len(self._held_shapes) >= 4096:
+                self._held_shapes.clear()
+            got = self._held_shapes[shape] = (rows, ch, self._dense(*shape[:-1], -(-ch // FDG_CKPT_BLOCK)))
+        return got
+
     def _gn(self, shape, groups, backward):
-        """(shape structure, scratch bytes) of a group norm of tensors [N, pixels.., C]."""
+        """(shape structure, scratch bytes, layouts of the statistics and of the gate) of a group norm of tensors [N, pixels.., C]."""
         key = (shape, groups, backward)
         got = self._gn_shapes.get(key)
         if got is None:
@@ -638,31 +661,30 @@ class EwOps:
             self._chk(self.lib.fdg_gn_scratch_bytes(self.precision, C.byref(s), backward, C.byref(need)))
             if len(self._gn_shapes) >= 4096:
                 self._gn_shapes.clear()
-            got = self._gn_shapes[key] = (C.byref(s), need.value)
+            got = self._gn_shapes[key] = (C.byref(s), need.value, self._dense(2, shape[0], groups), self._dense(*shape[:-1], (shape[-1] + 7) // 8))
         return got
 
     _ACTS = {"none": FDG_ACT_NONE, "relu": FDG_ACT_RELU, "silu": FDG_ACT_SILU}
 
     def _act(self, name):
-        if name not in self._ACTS:
+        got = self._ACTS.get(name)
+        if got is None:
             raise FDGError(1, "activation %r: none, relu or silu" % (name,))
-        return self._ACTS[name]
+        return got
 
-    @staticmethod
-    def _scale_shape(shape):
-        return shape[:-1] + (-(-shape[-1] // FDG_CKPT_BLOCK),)
-
-    def _empty_held(self, x):
-        torch = self.torch
-        return torch.empty_like(x, dtype=torch.int8), x.new_empty(self._scale_shape(x.shape), dtype=torch.uint8)
+    def _empty(self, layout, dtype, t):
+        """An uninitialised tensor beside t: the quickest of torch's calls that say so."""
+        return self.torch.empty_strided(layout[0], layout[1], dtype=dtype, device=t.device)
 
     def ckpt_encode(self, x):
         """(codes, scales): x [.., C] held in 8 bits."""
+        torch = self.torch
         dev, stream = self._here()
-        px = self._take(x, x.shape, self.dtype, "x", dev)
-        codes, scales = self._empty_held(x)
-        ch = x.shape[-1]
-        rc = self.lib.fdg_ckpt_encode(self.precision, px, x.numel() // ch if ch else 0, ch, codes.data_ptr(), scales.data_ptr(), stream)
+        shape = x.shape
+        rows, ch, layout = self._blocks(shape)
+        px = self._take(x, shape, self.dtype, "x", dev)
+        codes, scales = torch.empty_like(x, dtype=torch.int8), self._empty(layout, torch.uint8, x)
+        rc = self.lib.fdg_ckpt_encode(self.precision, px, rows, ch, codes.data_ptr(), scales.data_ptr(), stream)
         if rc:
             self._chk(rc)
         return codes, scales
@@ -673,11 +695,11 @@ class EwOps:
         dev, stream = self._here()
         codes, scales = held
         shape = codes.shape
+        rows, ch, layout = self._blocks(shape)
         pc = self._take(codes, shape, torch.int8, "codes", dev)
-        ps = self._take(scales, self._scale_shape(shape), torch.uint8, "scales", dev)
+        ps = self._take(scales, layout[0], torch.uint8, "scales", dev)
         x = torch.empty_like(codes, dtype=self.dtype)
-        ch = shape[-1]
-        rc = self.lib.fdg_ckpt_decode(self.precision, pc, ps, codes.numel() // ch if ch else 0, ch, x.data_ptr(), stream)
+        rc = self.lib.fdg_ckpt_decode(self.precision, pc, ps, rows, ch, x.data_ptr(), stream)
         if rc:
             self._chk(rc)
         return x
@@ -688,18 +710,24 @@ class EwOps:
         torch = self.torch
         dev, stream = self._here()
         shape = x.shape
-        s, need = self._gn(shape, groups, 0)
+        s, need, stats_layout, gate_layout = self._gn(shape, groups, 0)
         vec, f32 = shape[-1:], torch.float32
         px, pg, pb = self._take(x, shape, self.dtype, "x", dev), self._take(gamma, vec, f32, "gamma", dev), self._take(beta, vec, f32, "beta", dev)
         pr = None if res is None else self._take(res, shape, self.dtype, "res", dev)
         y = torch.empty_like(x)
-        stats = x.new_empty((2, shape[0], groups), dtype=f32)
-        bits = x.new_empty(shape[:-1] + ((shape[-1] + 7) // 8,), dtype=torch.uint8) if gate else None
-        held = self._empty_held(x) if checkpoint else None
-        sc = x.new_empty(need, dtype=torch.uint8) if need else None
-        rc = self.lib.fdg_gn_forward(self.precision, s, px, pg, pb, pr, self._act(act), eps, y.data_ptr(), stats.data_ptr(), _ptr(bits),
-                                     None if held is None else held[0].data_ptr(), None if held is None else held[1].data_ptr(),
-                                     _ptr(sc), need, stream)
+        stats = self._empty(stats_layout, f32, x)
+        bits = held = sc = pbits = pc = ps = psc = None
+        if gate:
+            bits = self._empty(gate_layout, torch.uint8, x)
+            pbits = bits.data_ptr()
+        if checkpoint:
+            held = torch.empty_like(x, dtype=torch.int8), self._empty(self._blocks(shape)[2], torch.uint8, x)
+            pc, ps = held[0].data_ptr(), held[1].data_ptr()
+        if need:
+            sc = self._empty(((need,), (1,)), torch.uint8, x)
+            psc = sc.data_ptr()
+        rc = self.lib.fdg_gn_forward(self.precision, s, px, pg, pb, pr, self._act(act), eps, y.data_ptr(), stats.data_ptr(), pbits, pc, ps,
+                                     psc, need, stream)
         if rc:
             self._chk(rc)
         return y, stats, bits, held
@@ -710,29 +738,27 @@ class EwOps:
         torch = self.torch
         dev, stream = self._here()
         shape = dy.shape
-        s, need = self._gn(shape, groups, 1)
+        s, need, stats_layout, gate_layout = self._gn(shape, groups, 1)
         vec, f32 = shape[-1:], torch.float32
         pdy = self._take(dy, shape, self.dtype, "dy", dev)
         px = pc = ps = None
         if isinstance(x, (tuple, list)):
             pc = self._take(x[0], shape, torch.int8, "codes", dev)
-            ps = self._take(x[1], self._scale_shape(shape), torch.uint8, "scales", dev)
+            ps = self._take(x[1], self._blocks(shape)[2][0], torch.uint8, "scales", dev)
         else:
             px = self._take(x, shape, self.dtype, "x", dev)
-        pst, pg = self._take(stats, (2, shape[0], groups), f32, "stats", dev), self._take(gamma, vec, f32, "gamma", dev)
+        pst, pg = self._take(stats, stats_layout[0], f32, "stats", dev), self._take(gamma, vec, f32, "gamma", dev)
         pb = None if beta is None else self._take(beta, vec, f32, "beta", dev)
         pm = None if mask is None else self._take(mask, shape, self.dtype, "mask", dev)
-        pgate = None if gate is None else self._take(gate, shape[:-1] + ((shape[-1] + 7) // 8,), torch.uint8, "gate", dev)
+        pgate = None if gate is None else self._take(gate, gate_layout[0], torch.uint8, "gate", dev)
         pr = None if res is None else self._take(res, shape, self.dtype, "res", dev)
         dx = torch.empty_like(dy)
-        dparam = dy.new_empty((2, shape[-1]), dtype=f32)
-        sc = dy.new_empty(need, dtype=torch.uint8)
-        dg = dparam.data_ptr()
-        rc = self.lib.fdg_gn_backward(self.precision, s, pdy, px, pc, ps, pst, pg, pb, self._act(act), pm, pgate, pr, dx.data_ptr(), dg,
-                                      dg + 4 * shape[-1], sc.data_ptr(), need, stream)
+        layout = vec, (1,)
+        dgamma, dbeta, sc = self._empty(layout, f32, dy), self._empty(layout, f32, dy), self._empty(((need,), (1,)), torch.uint8, dy)
+        rc = self.lib.fdg_gn_backward(self.precision, s, pdy, px, pc, ps, pst, pg, pb, self._act(act), pm, pgate, pr, dx.data_ptr(),
+                                      dgamma.data_ptr(), dbeta.data_ptr(), sc.data_ptr(), need, stream)
         if rc:
             self._chk(rc)
-        dgamma, dbeta = dparam.unbind()
         return dx, dgamma, dbeta
 
     def shrink(self, x, beta):
