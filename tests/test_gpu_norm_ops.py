@@ -153,20 +153,21 @@ def test_backward(prec_name, shape):
 
 
 @pytest.mark.parametrize("prec_name", PRECISIONS)
-@pytest.mark.parametrize("shape", [(2, 40, 16, 4), (2, 24, 64, 2), (2, 9, 30, 5), (1, 16384, 64, 8)], ids=str)
-def test_any_alignment(prec_name, shape):
-    """Contiguous tensors that start at an element's alignment only."""
+@pytest.mark.parametrize("by", [1, 2, 4])
+@pytest.mark.parametrize("shape", [(2, 40, 16, 4), (2, 24, 64, 2), (2, 9, 30, 5), (2, 33, 20, 5), (3, 7, 12, 4), (1, 16384, 64, 8),
+                                   (1, 20000, 36, 4)], ids=str)
+def test_any_alignment(prec_name, shape, by):
+    """Contiguous tensors that start `by` elements off a vector's alignment."""
     B, ew = _ops(prec_name)
     n, p, c, groups = shape
 
     def shifted(t):
-        buf = torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")
-        out = buf[1:].view(t.shape)
+        buf = torch.empty(t.numel() + by, dtype=t.dtype, device="cuda")
+        out = buf[by:].view(t.shape)
         out.copy_(t)
         return out
 
     x = shifted(_mk((n, p, c), 61, ew.dtype)[0])
-    assert x.data_ptr() % 16
     small = n * p * c < 200000
     x, xo, y, stats, bits, held = _check_forward(ew, shape, "relu", False, seed=60, gate=True, ckpt=small, x=x)
     _check_backward(ew, shape, "relu", 60, xo, x, stats, shifted(y), bits, True, False)
