@@ -881,7 +881,7 @@ __device__ __forceinline__ Raw8<T> dx_of(const Raw8<T>& dy, const Held<T, CK>& h
 }
 
 // The operands of a pass: rings of dy, x (or its codes), the mask and res, as far as a pass has them; the bytes
-// (scales, gate bits) come through registers, two turns ahead.
+// (scales, gate bits) come through registers, as many turns ahead.
 template <typename T, int W, bool CK> struct Feed {
   static constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   const Columns<T> from;
@@ -907,7 +907,11 @@ template <typename T, int W, bool CK> struct Feed {
     const uint32_t k = reverse && n > 0 ? (uint32_t)(n - 1) : 0u;
     next = from.first + k * from.step; next_scale = from.scale_first + k * from.scale_step; next_gate = from.gate_first + k * from.gate_step;
   }
-  // The bytes of the turn that begins with vector k, to be used two turns later.
+  __device__ __forceinline__ void start_bytes() {
+#pragma unroll
+    for (int t = 0; t < kAhead; ++t) bytes<false>(t * kBatch, t * kBatch);
+  }
+  // The bytes of the turn that begins with vector k, to be used kAhead turns later.
   template <bool FULL> __device__ __forceinline__ void bytes(int k, int slot) {
     const int to = slot / kBatch % (kAhead + 1);
 #pragma unroll
@@ -1005,8 +1009,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
   grid_dependency_wait();
   grid_dependency_release();
   Feed<T, W, CK> feed(p, at, sh, slope, nullptr, false, smem);
-  feed.template bytes<false>(0, 0);
-  feed.template bytes<false>(kBatch, kBatch);
+  feed.start_bytes();
   Channels ch;
   float rstd[8];
   Sums sums;
@@ -1014,7 +1017,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid
   Stream<kBatch>::start(sh.mine, issue);
   load_channels(p, at, n, slope, ch, rstd);
   Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot, auto full) {
-    feed.template bytes<full.value>(k + 2 * kBatch, slot + 2 * kBatch);
+    feed.template bytes<full.value>(k + kAhead * kBatch, slot + kAhead * kBatch);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (full.value || k + u < sh.mine) {
@@ -1092,8 +1095,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   grid_dependency_release();
   auto issue = [&](int slot) { feed.issue(slot); };
   if constexpr (!kEarly<T, W>) Stream<kBatch>::start(sh.mine, issue);
-  feed.template bytes<false>(0, 0);
-  feed.template bytes<false>(kBatch, kBatch);
+  feed.start_bytes();
   Channels ch;
   float rstd[8];
   load_channels(p, at, n, slope, ch, rstd);
@@ -1125,7 +1127,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
   uint32_t o = feed.from.first + (uint32_t)max(sh.mine - 1, 0) * feed.from.step;
   T* const dx = p.dx + sh.row0 * g.C;
   Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot, auto full) {
-    feed.template bytes<full.value>(k + 2 * kBatch, slot + 2 * kBatch);
+    feed.template bytes<full.value>(k + kAhead * kBatch, slot + kAhead * kBatch);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (full.value || k + u < sh.mine) {
