@@ -174,7 +174,7 @@ fdg_status fdg_bn_backward(int precision, const void* dy, const void* mask, cons
  * A block with an infinity or NaN: scale byte 255, codes 0, reads back as NaN throughout.  Largest magnitudes of
  * 127.5/128 * 2^128 and more keep e = 121 and codes of at most 127, so that finite values stay finite.
  * A decoded bf16 checkpoint is the checkpoint, with no further rounding: fdg_conv_wgrad takes it as its x.
- * The tensors of one call do not overlap.  Asynchronous on `stream`. */
+ * The tensors of one call do not overlap; at most 2^36 values and 2^28 channels (FDG_ERR_INVALID_ARG).  Asynchronous on `stream`. */
 #define FDG_CKPT_BLOCK 32
 fdg_status fdg_ckpt_encode(int precision, const void* x, size_t rows, int C, int8_t* codes, uint8_t* scales, fdg_stream stream);
 fdg_status fdg_ckpt_decode(int precision, const int8_t* codes, const uint8_t* scales, size_t rows, int C, void* x, fdg_stream stream);
@@ -182,7 +182,7 @@ fdg_status fdg_ckpt_decode(int precision, const int8_t* codes, const uint8_t* sc
 /* ---- group normalisation with an activation -------------------------------------------------------------------------
  * The normalisation that does not depend on which images share a batch.  x [N][HW][C]; group g of an image is channels
  * [g*C/groups, (g+1)*C/groups) at all of its pixels (groups = 1: layer norm over an image, groups = C: instance norm).
- * `groups` divides C; any C up to 65536, any alignment that the storage type has (multiples of 8 channels on 16-byte aligned tensors are
+ * `groups` divides C; any C up to 65536, at most 2^30 images and 2^36 values, any alignment that the storage type has (multiples of 8 channels on 16-byte aligned tensors are
  * fastest).  gamma, beta, dgamma, dbeta [C], stats [2][N][groups] (mean, then 1/sqrt(var + eps), biased variance) are fp32.
  * `scratch`: fdg_gn_scratch_bytes bytes of device memory for that pass (0 for a forward pass that needs none: scratch may then
  * be NULL), 256-byte aligned, any contents; not to be shared by calls that may run at the same time.  The result of a call does not depend on scheduling.  No output

@@ -289,35 +289,33 @@ __global__ void __launch_bounds__(kCkptThreads) ckpt_decode_any_kernel(const int
   }
 }
 
-// ---- host side -----------------------------------------------------------------------------------------
-constexpr size_t kCkptMaxGrid = (size_t)1 << 30;
-
+// ---- host side (at most 2^36 values and 2^28 channels: grids below 2^31, offsets inside a warp's blocks in 32 bits) ----------
+inline size_t ceil_div(size_t n, size_t d) { return (n + d - 1) / d; }
 template <typename T>
 inline cudaError_t launch_ckpt_encode(cudaStream_t st, const T* x, size_t rows, int C, int8_t* codes, uint8_t* scales) {
   const int lanes = ckpt_block_lanes(C), per_row = (C + kCkptBlock - 1) / kCkptBlock;
   const size_t blocks = rows * (size_t)per_row;
-  if (access_width<T>(C, {x}, codes) == kWhole) {
-    const size_t vecs = rows * (size_t)(C / 8), per = kCkptThreads * kCkptUnroll, grid = lanes ? (vecs + per - 1) / per : (blocks + kCkptThreads - 1) / kCkptThreads;
-    if (grid <= kCkptMaxGrid && lanes)
-      return launch_chained(ckpt_encode_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, x, vecs, lanes, codes, scales);
-    if (grid <= kCkptMaxGrid)
-      return launch_chained(ckpt_encode_blocks_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, x, blocks, C / 8, per_row, codes, scales);
-  }
-  const size_t per = kCkptThreads / 32 * kCkptBlocks, grid = (blocks + per - 1) / per;
-  if (grid > INT32_MAX) return cudaErrorInvalidValue;
-  return launch_chained(ckpt_encode_any_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, x, blocks, C, per_row, codes, scales);
+  const dim3 threads(kCkptThreads);
+  if (access_width<T>(C, {x}, codes) != kWhole)
+    return launch_chained(ckpt_encode_any_kernel<T>, dim3((unsigned)ceil_div(blocks, kCkptThreads / 32 * kCkptBlocks)), threads, 0, st, x, blocks, C,
+                          per_row, codes, scales);
+  if (!lanes)
+    return launch_chained(ckpt_encode_blocks_kernel<T>, dim3((unsigned)ceil_div(blocks, kCkptThreads)), threads, 0, st, x, blocks, C / 8, per_row,
+                          codes, scales);
+  const size_t vecs = rows * (size_t)(C / 8);
+  return launch_chained(ckpt_encode_kernel<T>, dim3((unsigned)ceil_div(vecs, kCkptThreads * kCkptUnroll)), threads, 0, st, x, vecs, lanes, codes, scales);
 }
 template <typename T>
 inline cudaError_t launch_ckpt_decode(cudaStream_t st, const int8_t* codes, const uint8_t* scales, size_t rows, int C, T* x) {
   const int per_row = (C + kCkptBlock - 1) / kCkptBlock;
+  const dim3 threads(kCkptThreads);
   if (access_width<T>(C, {x}, codes) == kWhole) {
-    const size_t vecs = rows * (size_t)(C / 8), per = kCkptThreads * kCkptUnroll, grid = (vecs + per - 1) / per;
-    if (grid <= kCkptMaxGrid)
-      return launch_chained(ckpt_decode_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, codes, scales, vecs, ckpt_block_lanes(C), C / 8, per_row,
-                            kCkptThreads / (C / 8), kCkptThreads % (C / 8), x);
+    const size_t vecs = rows * (size_t)(C / 8);
+    return launch_chained(ckpt_decode_kernel<T>, dim3((unsigned)ceil_div(vecs, kCkptThreads * kCkptUnroll)), threads, 0, st, codes, scales, vecs,
+                          ckpt_block_lanes(C), C / 8, per_row, kCkptThreads / (C / 8), kCkptThreads % (C / 8), x);
   }
-  const size_t elems = rows * (size_t)C, grid = std::min<size_t>((elems + kCkptThreads - 1) / kCkptThreads, (size_t)kSms * 64);
-  return launch_chained(ckpt_decode_any_kernel<T>, dim3((unsigned)grid), dim3(kCkptThreads), 0, st, codes, scales, elems, C, per_row, x);
+  const size_t elems = rows * (size_t)C, grid = std::min<size_t>(ceil_div(elems, kCkptThreads), (size_t)kSms * 64);
+  return launch_chained(ckpt_decode_any_kernel<T>, dim3((unsigned)grid), threads, 0, st, codes, scales, elems, C, per_row, x);
 }
 
 }  // namespace fdg

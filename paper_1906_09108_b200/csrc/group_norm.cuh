@@ -56,6 +56,7 @@ struct Geom {
   float inv_m;              // 1 / (P * Cg)
 };
 constexpr int kMergeParts = 16;             // rows of sums that the second streamed pass adds up itself
+constexpr int kForwardPerSm = 3, kBackwardPerSm = 2;      // CTAs on an SM: 80 and 128 registers a thread
 
 // ---- device helpers -------------------------------------------------------------------------------------
 // 1/(1 + exp(-z)) of two values.  For tensors in 16 bits from the approximate exponential and reciprocal (relative error below
@@ -435,7 +436,6 @@ __device__ __forceinline__ uint32_t positive_bits(const Raw8<float>& y) {
 // y (and the gate's bits, and x in 8 bits) of a thread's pixels.  ACT < 0: p.act.  EXTRA 1: res and gate may be asked for; 2: and
 // codes.  Offsets inside a CTA's pixels fit 32 bits.
 enum { PLAIN = 0, WITH_RES_GATE = 1, WITH_CODES = 2 };
-constexpr int kPlainPerSm = 3, kCodesPerSm = 3;       // CTAs on an SM that the registers allow (80 spill where codes are formed)
 template <typename T, int W, int ACT, int EXTRA> struct Emitter {
   T* y;                       // of the CTA's first pixel, as the others: the same for all threads
   const T* res;
@@ -543,7 +543,7 @@ __device__ __forceinline__ void load_affine(const Forward<T>& p, const Place& at
 
 // The resident form: blockIdx = image, share of its pixels, tile of columns: a cluster per image.
 template <typename T, int W, int ACT, int EXTRA>
-__global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : kPlainPerSm) forward_kernel(const __grid_constant__ Forward<T> p) {
+__global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_kernel(const __grid_constant__ Forward<T> p) {
   constexpr int kBatch = 2;
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
@@ -603,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : 
 
 // Streamed, first pass: moments of each group (with tiles > 1: of each channel) over a CTA's pixels.
 template <typename T, int W>
-__global__ void __launch_bounds__(kThreads, 3) moments_kernel(const __grid_constant__ Forward<T> p) {
+__global__ void __launch_bounds__(kThreads, kForwardPerSm) moments_kernel(const __grid_constant__ Forward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
@@ -699,7 +699,7 @@ __global__ void __launch_bounds__(1024) combine_kernel(const __grid_constant__ F
 // Streamed, second pass: y from x and the statistics, which every CTA of an image forms from the rows of sums itself (the same
 // bits everywhere; its first CTA writes them out) unless combine_kernel has.
 template <typename T, int W, int ACT, int EXTRA>
-__global__ void __launch_bounds__(kThreads, EXTRA == WITH_CODES ? kCodesPerSm : kPlainPerSm) apply_kernel(const __grid_constant__ Forward<T> p) {
+__global__ void __launch_bounds__(kThreads, kForwardPerSm) apply_kernel(const __grid_constant__ Forward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
@@ -775,6 +775,7 @@ template <typename T> struct Backward {
   float* totals;              // [N][2][C]: A, B of each image, or null if the second pass adds up the rows itself
   float* dgamma;
   float* dbeta;
+  int extra;                  // of the second pass: ceil(2C / 32 / parts)
   int slope;
 };
 
@@ -858,9 +859,7 @@ __device__ __forceinline__ void operands(const Raw8<T>& dy, const Held<T, CK>& h
   }
   if (slope == SLOPE_SILU) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      dz.p[j] = mul2(dz.p[j], silu_slope<T>(fma2(d.p[j], ch.scale[j], ch.shift[j])));
-    }
+    for (int j = 0; j < 4; ++j) dz.p[j] = mul2(dz.p[j], silu_slope<T>(fma2(d.p[j], ch.scale[j], ch.shift[j])));
   }
 }
 
@@ -996,7 +995,7 @@ struct Sums {
 
 // First pass: A and B of each channel over a CTA's pixels.
 template <typename T, int W, bool CK, int SLOPE>
-__global__ void __launch_bounds__(kThreads, 2) backward_sums_kernel(const __grid_constant__ Backward<T> p) {
+__global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_sums_kernel(const __grid_constant__ Backward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
@@ -1065,19 +1064,20 @@ __global__ void __launch_bounds__(1024) totals_kernel(const float* __restrict__ 
 }
 
 // Second pass: dx.  Every CTA forms S1 and S2 of its tile's groups from the image's totals, or from its rows of sums.
-// The CTAs behind the last image (blockIdx.x >= N) add up the parameter gradients, 32 values each.
+// The first `extra` CTAs of a share add up the parameter gradients, 32 values each.
 template <typename T, int W, bool CK, int SLOPE>
-__global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __grid_constant__ Backward<T> p) {
+__global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_apply_kernel(const __grid_constant__ Backward<T> p) {
   constexpr int kBatch = batch_of<T>(), kRing = ring_of<T>();
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
   float* coef = reinterpret_cast<float*>(smem + Feed<T, W, CK>::words((SLOPE < 0 ? p.slope : SLOPE) == SLOPE_MASK, p.res != nullptr));   // [2][sets]
   const int slope = SLOPE < 0 ? p.slope : SLOPE;
-  const int part = blockIdx.y, n = blockIdx.x;
+  const int part = blockIdx.y, n = (int)blockIdx.x - p.extra;
   const int c_first = blockIdx.z * kMaxCols * 8;
-  if (n >= g.N) {
-    const int first = ((n - g.N) * g.parts + part) * 32;
+  if (n < 0) {
+    const int first = ((int)blockIdx.x * g.parts + part) * 32;
     grid_dependency_wait();
+    grid_dependency_release();
     if (blockIdx.z == 0 && first < 2 * g.C)
       add_rows(p.partial, g.N * g.parts, 2 * g.C, first, reinterpret_cast<double(*)[33]>(smem),
                [&](int i, float v) { (i < g.C ? p.dgamma + i : p.dbeta + (i - g.C))[0] = v; });
@@ -1134,8 +1134,7 @@ __global__ void __launch_bounds__(kThreads, 2) backward_apply_kernel(const __gri
         const Held<T, CK> h = feed.get(slot, u);
         Raw8<T> r;
         if (feed.res) r = feed.ress.get(slot + u);
-        raw8_put<T, W>(dx + o, at.left,
-                         dx_of<T, CK>(passed<T, CK>(h, slope), h, slope, ch, k1, k2, feed.res ? &r : nullptr));
+        raw8_put<T, W>(dx + o, at.left, dx_of<T, CK>(passed<T, CK>(h, slope), h, slope, ch, k1, k2, feed.res ? &r : nullptr));
         o += feed.step;
       }
   });
@@ -1186,8 +1185,8 @@ inline Plan plan_streamed(int N, int P, int C, int G, int per_sm) {
 // allows), with as many CTAs per image as that gives, and where they fill at least half of the SMs or a thread has few pixels.
 // us, resident / streamed, 16-bit storage: 8x16x16x8 4.6 / 5.4, 128x16x16x160 8.2 / 10.3, 128x8x8x640 8.7 / 10.8; on the other
 // side of the rule 2x64x64x128 with SiLU 12.2 / 10.0, and 128 images of 32x32x160 in more than one wave 31.5 / 23.4.
-inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G, bool codes) {
-  Plan pl = plan_streamed(N, P, C, G, codes ? kCodesPerSm : kPlainPerSm);
+inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G) {
+  Plan pl = plan_streamed(N, P, C, G, kForwardPerSm);
   if (pl.g.tiles > 1) return pl;
   Plan res = pl;
   for (int parts = kMaxCluster; parts >= 1; parts /= 2) {
@@ -1201,16 +1200,15 @@ inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G, bool codes)
   }
   return pl;
 }
-inline Plan plan_backward(int N, int P, int C, int G) { return plan_streamed(N, P, C, G, 2); }
-// Whether every launch's grid can be given.
-inline bool grid_ok(const Plan& pl) {
-  const Geom& g = pl.g;
-  return pl.resident || ((int64_t)g.N * g.parts <= INT32_MAX && (int64_t)g.N * g.G <= INT32_MAX &&
-                         (int64_t)g.N * ((2 * (int64_t)g.C + 31) / 32) <= INT32_MAX);
-}
+inline Plan plan_backward(int N, int P, int C, int G) { return plan_streamed(N, P, C, G, kBackwardPerSm); }
 inline size_t partial_floats(const Plan& pl) { return pl.resident ? 0 : (size_t)pl.g.N * pl.g.parts * 2 * pl.g.C; }
 // Whether a second streamed pass adds up an image's rows of sums itself.
 inline bool merges(const Geom& g) { return g.tiles == 1 && g.parts <= kMergeParts; }
+// Whether every launch's grid can be given (with many images a plan has one share of each).
+inline bool grid_ok(const Plan& pl) {
+  const Geom& g = pl.g;
+  return pl.resident || merges(g) || ((int64_t)g.N * g.G <= INT32_MAX && (int64_t)g.N * ((2 * (int64_t)g.C + 31) / 32) <= INT32_MAX);
+}
 
 // ---- host side: launches ---------------------------------------------------------------------------------------
 template <typename Kernel, typename Params>
@@ -1291,9 +1289,9 @@ inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<
     e = launch_chained(totals_kernel, dim3((unsigned)(g.N * blocks)), dim3(1024), 0, st, (const float*)p.partial, g.parts, width, p.totals);
   // coefficients of the tile's groups; with one tile also the channels' sums
   const size_t own = 8 * (size_t)std::min(g.G, g.cols * 8) + (g.tiles == 1 ? 8 * (size_t)g.C : 0);
-  const int extra = (blocks + g.parts - 1) / g.parts;
+  p.extra = (blocks + g.parts - 1) / g.parts;
   if (e == cudaSuccess)
-    e = launch_chained(backward_apply_kernel<T, W, CK, SLOPE>, dim3((unsigned)(g.N + extra), (unsigned)g.parts, (unsigned)g.tiles), dim3(kThreads),
+    e = launch_chained(backward_apply_kernel<T, W, CK, SLOPE>, dim3((unsigned)(g.N + p.extra), (unsigned)g.parts, (unsigned)g.tiles), dim3(kThreads),
                        rings(p.res != nullptr) + own, st, p);
   return e;
 }

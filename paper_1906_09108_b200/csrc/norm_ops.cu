@@ -11,18 +11,18 @@ static bool precision_ok(int precision) { return precision == FDG_FP32_CUDACORE 
 static unsigned elem_bytes(int precision) { return precision == FDG_BF16_TC ? 2 : 4; }
 static fdg_status status_of(cudaError_t e) { return e == cudaSuccess ? FDG_OK : FDG_ERR_CUDA; }
 
-// rows * C values whose bytes can be counted, and whose share of a CTA can be in 32 bits.
-static bool rows_ok(size_t rows, int C) { return C >= 1 && rows >= 1 && rows <= ((size_t)1 << 38) / (size_t)C; }
+// Values whose bytes, blocks of 32 and shares can be counted in the widths that the kernels use.
+static bool rows_ok(size_t rows, int C) { return C >= 1 && C <= 1 << 28 && rows >= 1 && rows <= ((size_t)1 << 36) / (size_t)C; }
 static bool gn_shape_ok(int precision, const fdg_gn_shape* s) {
-  return s && precision_ok(precision) && s->N >= 1 && s->HW >= 1 && s->C >= 1 && s->groups >= 1 && s->C % s->groups == 0 &&
+  return s && precision_ok(precision) && s->N >= 1 && s->N <= 1 << 30 && s->HW >= 1 && s->C >= 1 && s->groups >= 1 && s->C % s->groups == 0 &&
          s->C <= 1 << 16 && rows_ok((size_t)s->N * (size_t)s->HW, s->C);
 }
 static size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Scratch: the forward pass's rows of sums; the backward pass's per-image totals [N][2][C] and then its rows of sums.
+// Scratch: the forward pass's rows of sums; the backward pass's per-image totals [N][2][C], where it forms them, and its rows of sums.
 static size_t forward_need(const gn::Plan& pl) { return align256(gn::partial_floats(pl) * sizeof(float)); }
-static size_t totals_bytes(const fdg_gn_shape* s) { return align256((size_t)s->N * 2 * s->C * sizeof(float)); }
-static size_t backward_need(const fdg_gn_shape* s, const gn::Plan& pl) { return totals_bytes(s) + align256(gn::partial_floats(pl) * sizeof(float)); }
+static size_t totals_bytes(const gn::Plan& pl) { return gn::merges(pl.g) ? 0 : align256((size_t)pl.g.N * 2 * pl.g.C * sizeof(float)); }
+static size_t backward_need(const gn::Plan& pl) { return totals_bytes(pl) + align256(gn::partial_floats(pl) * sizeof(float)); }
 
 template <typename T>
 static cudaError_t gn_forward_as(const gn::Plan& pl, const void* x, const float* gamma, const float* beta, const void* res, int act, float eps,
@@ -34,7 +34,7 @@ static cudaError_t gn_forward_as(const gn::Plan& pl, const void* x, const float*
   return gn::launch_forward<T>(st, pl, p);
 }
 template <typename T>
-static cudaError_t gn_backward_as(const fdg_gn_shape* s, const gn::Plan& pl, const void* dy, const void* x, const int8_t* codes, const uint8_t* scales,
+static cudaError_t gn_backward_as(const gn::Plan& pl, const void* dy, const void* x, const int8_t* codes, const uint8_t* scales,
                                   const float* stats, const float* gamma, const float* beta, int act, const void* mask, const uint8_t* gate,
                                   const void* res, void* dx, float* dgamma, float* dbeta, void* scratch, cudaStream_t st) {
   gn::Backward<T> p{};
@@ -42,7 +42,7 @@ static cudaError_t gn_backward_as(const fdg_gn_shape* s, const gn::Plan& pl, con
   p.mask = (const T*)mask; p.gate = gate; p.res = (const T*)res; p.dx = (T*)dx;
   p.slope = act == FDG_ACT_SILU ? gn::SLOPE_SILU : mask ? gn::SLOPE_MASK : gate ? gn::SLOPE_BITS : gn::SLOPE_ONE;
   p.totals = static_cast<float*>(scratch);
-  p.partial = reinterpret_cast<float*>(static_cast<char*>(scratch) + totals_bytes(s));
+  p.partial = reinterpret_cast<float*>(static_cast<char*>(scratch) + totals_bytes(pl));
   p.dgamma = dgamma; p.dbeta = dbeta;
   return gn::launch_backward<T>(st, pl, p);
 }
@@ -70,14 +70,14 @@ fdg_status fdg_gn_scratch_bytes(int precision, const fdg_gn_shape* s, int backwa
   if (!bytes || !gn_shape_ok(precision, s)) return FDG_ERR_INVALID_ARG;
   const int b = (int)elem_bytes(precision);
   if (!backward) {
-    const gn::Plan plain = gn::plan_forward(b, s->N, s->HW, s->C, s->groups, false), codes = gn::plan_forward(b, s->N, s->HW, s->C, s->groups, true);
-    if (!gn::grid_ok(plain) || !gn::grid_ok(codes)) return FDG_ERR_INVALID_ARG;
-    *bytes = std::max(forward_need(plain), forward_need(codes));
+    const gn::Plan pl = gn::plan_forward(b, s->N, s->HW, s->C, s->groups);
+    if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
+    *bytes = forward_need(pl);
     return FDG_OK;
   }
   const gn::Plan pl = gn::plan_backward(s->N, s->HW, s->C, s->groups);
   if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
-  *bytes = backward_need(s, pl);
+  *bytes = backward_need(pl);
   return FDG_OK;
 }
 
@@ -89,7 +89,7 @@ fdg_status fdg_gn_forward(int precision, const fdg_gn_shape* s, const void* x, c
   if ((act == FDG_ACT_SILU && res) || (gate && act != FDG_ACT_RELU) || (codes != nullptr) != (scales != nullptr)) return FDG_ERR_INVALID_ARG;
   const unsigned b = elem_bytes(precision);
   if (!aligned_to(x, b) || !aligned_to(y, b) || !aligned_to(res, b) || !aligned_to(scratch, 256)) return FDG_ERR_INVALID_ARG;
-  const gn::Plan pl = gn::plan_forward((int)b, s->N, s->HW, s->C, s->groups, codes != nullptr);
+  const gn::Plan pl = gn::plan_forward((int)b, s->N, s->HW, s->C, s->groups);
   if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
   const size_t need = forward_need(pl);
   if (need > 0 && (!scratch || scratch_bytes < need)) return FDG_ERR_WORKSPACE_TOO_SMALL;
@@ -110,11 +110,11 @@ fdg_status fdg_gn_backward(int precision, const fdg_gn_shape* s, const void* dy,
     return FDG_ERR_INVALID_ARG;
   const gn::Plan pl = gn::plan_backward(s->N, s->HW, s->C, s->groups);
   if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
-  if (!scratch || scratch_bytes < backward_need(s, pl)) return FDG_ERR_WORKSPACE_TOO_SMALL;
+  if (!scratch || scratch_bytes < backward_need(pl)) return FDG_ERR_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return status_of(precision == FDG_BF16_TC
-                       ? gn_backward_as<bf16>(s, pl, dy, x, codes, scales, stats, gamma, beta, act, mask, gate, res, dx, dgamma, dbeta, scratch, st)
-                       : gn_backward_as<float>(s, pl, dy, x, codes, scales, stats, gamma, beta, act, mask, gate, res, dx, dgamma, dbeta, scratch, st));
+                       ? gn_backward_as<bf16>(pl, dy, x, codes, scales, stats, gamma, beta, act, mask, gate, res, dx, dgamma, dbeta, scratch, st)
+                       : gn_backward_as<float>(pl, dy, x, codes, scales, stats, gamma, beta, act, mask, gate, res, dx, dgamma, dbeta, scratch, st));
 }
 
 }  // extern "C"

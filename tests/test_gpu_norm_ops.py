@@ -27,6 +27,7 @@ SHAPES = [
     (2, 1024, 160, 32), (2, 64, 640, 1), (3, 49, 320, 32),          # groups of 5 channels; one group; odd maps
     (2, 784, 30, 6), (3, 65, 33, 11), (7, 9, 24, 3), (1, 100, 7, 7),   # channels that fill no column
     (2, 17, 2048, 16), (1, 3, 2056, 8), (2, 5, 4104, 27), (1, 2, 4112, 1),      # as wide as a CTA goes, and wider
+    (1, 3, 65536, 32), (1, 2, 65536, 65536), (500, 5, 16, 4), (700, 2, 30, 3),     # the widest; more images than CTAs run at once
 ]
 # images that no cluster holds
 LARGE = [(1, 16384, 64, 8), (2, 9001, 160, 32), (1, 20011, 30, 1)]
