@@ -181,8 +181,6 @@ template <int B> struct Stream {
 
 // Whether copies of these vectors may begin before a kernel's grid_dependency_wait(), see moments_kernel: those that go past L1.
 template <typename T, int W> constexpr bool kEarly = W == kWhole && sizeof(T) == 2;
-// Bytes of a piece of 8 codes.
-template <typename T, int W> constexpr int kCodeWidth = W == kWhole ? 8 : W / (int)sizeof(T);
 
 // This thread's place in a CTA's tile.
 struct Place {

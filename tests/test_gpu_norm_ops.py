@@ -229,7 +229,7 @@ def test_what_is_not_finite_stays_in_its_group(prec_name, shape):
 
 @pytest.mark.parametrize("prec_name", PRECISIONS)
 @pytest.mark.parametrize("rows, c", [(1, 1), (5, 8), (300, 16), (70, 24), (33, 30), (64, 32), (9, 33), (50, 40), (20, 160), (6, 650), (4099, 64),
-                                     (1, 1000)])
+                                     (1, 1000), (40, 12), (40, 20), (33, 100), (50, 72), (9, 34)])
 def test_checkpoints_are_the_format(prec_name, rows, c):
     _, ew = _ops(prec_name)
     g = np.random.default_rng(rows * 1000 + c)
