@@ -59,10 +59,15 @@ constexpr int kMergeParts = 16;             // rows of sums that the second stre
 constexpr int kForwardPerSm = 3, kBackwardPerSm = 2;      // CTAs on an SM: 80 and 128 registers a thread
 
 // ---- device helpers -------------------------------------------------------------------------------------
-// 1/(1 + exp(-z)) of two values.  For tensors in 16 bits from the approximate exponential and reciprocal (relative error below
-// 2^-20 for |z| < 16, growing with |z| as the rounding of z*log2(e) does), for fp32 ones from expf and a division.  These
-// functions run at 16 values per SM and cycle, a quarter of what a streaming pass asks for, so two values share a reciprocal:
-// 1/a = b * 1/(ab).  The powers of two stop at 2^62, where ab and its reciprocal are still normal numbers: sigmoid(-43) is 2e-19.
+// 1/(1 + exp(-z)) of two values.  Exponentials and reciprocals run at 16 values per SM and cycle, a quarter of what a streaming
+// pass asks for.
+// For tensors in 16 bits from the approximate ones (relative error below 2^-20 for |z| < 16, growing with |z| as the rounding of
+// z*log2(e) does), two values sharing a reciprocal: 1/a = b * 1/(ab).  The powers of two stop at 2^62, where ab and its reciprocal
+// are still normal numbers: sigmoid(-43) is 2e-19.
+// For fp32 ones from expf and the approximate reciprocal r of d = 1 + exp(-z), which a step of Newton's iteration, r + r(1 - dr),
+// brings from 2^-23 to the rounding of its last sum.  Below the smallest normal number the value is 0; d stops short of infinity,
+// which the step would turn into NaN.  A division here branches: forward 22.8 us with it and 14.6 with this, 128 images of
+// 16x16x160; backward 151 and 109 at 2048 pixels of 160 channels.
 template <typename T> __device__ __forceinline__ f32x2 sigmoid(f32x2 z) {
   if constexpr (sizeof(T) == 2) {
     const float2 t = halves(mul2(z, pair(-1.44269504f)));
@@ -74,7 +79,12 @@ template <typename T> __device__ __forceinline__ f32x2 sigmoid(f32x2 z) {
     return mul2(pair(r), pair(d.y, d.x));
   } else {
     const float2 h = halves(z);
-    return pair(1.f / (1.f + expf(-h.x)), 1.f / (1.f + expf(-h.y)));
+    const float a = fminf(1.f + expf(-h.x), 3e38f), b = fminf(1.f + expf(-h.y), 3e38f);
+    float ra, rb;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(ra) : "f"(a));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rb) : "f"(b));
+    const f32x2 r = pair(ra, rb);
+    return fma2(r, fma2(pair(-a, -b), r, pair(1.f)), r);
   }
 }
 template <typename T> __device__ __forceinline__ f32x2 silu_slope(f32x2 z) {

@@ -472,3 +472,36 @@ def test_a_block_with_its_activations_held_in_8_bits(c, groups):
     for got, want in zip((dx1, dgamma, dbeta), exact):
         assert float((got.float() - want.float()).norm() / want.float().norm()) <= 2 * off + _half_step(ew.dtype)
     assert not conv.timed_out()
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+def test_silu_over_its_range(prec_name):
+    """gamma = 0 and one pixel make z = beta exactly, dbeta = SiLU's slope there.  u = 2^-24.  A sigmoid s is off by d of itself: fp32
+    storage 4u (expf, 2 ulp) + u (1 + exp) + u (the reciprocal); 16-bit storage (1 + 1)|z|u (z*log2(e): the constant and the product)
+    + 4u (the exponential) + u + 4u (the product of two denominators, its reciprocal at 1 ulp, the product that gives one back).
+    z*s adds u; s*(1 + z(1 - s)) adds |z|(d*s + 2u(1 - s) + u) + u inside the bracket and d + u outside.  fp32: a sigmoid below the
+    smallest normal number, 2^-126, may be 0, which costs up to 2^-126 (1 + |z|)."""
+    _, ew = _ops(prec_name)
+    dt = ew.dtype
+    c = 4096
+    z = np.linspace(-120, 120, c) if prec_name == "fp32" else np.linspace(-40, 40, c)
+    z = z.astype(np.float32)
+    zz = z.astype(np.float64)
+    x = torch.zeros(1, 1, c, device="cuda", dtype=dt)
+    zero = torch.zeros(c, device="cuda")
+    u = 2.0 ** -24
+    s = 1 / (1 + np.exp(-zz))
+    d = 6 * u if prec_name == "fp32" else (2 * np.abs(zz) + 9) * u
+    lost = 2.0 ** -126 * (1 + np.abs(zz))
+    y, stats, _, _ = ew.gn_forward(x, 4, zero, _f32(z), act="silu")
+    _near(y.reshape(c), zz * s, np.abs(zz * s) * (_half_step(dt) * (1 + 2 * d) + d + u) + lost, "y")
+    _, _, db = ew.gn_backward(torch.ones_like(x), x, stats, 4, zero, _f32(z), act="silu")
+    slope = s * (1 + zz * (1 - s))
+    inner = np.abs(zz) * (d * s + 2 * u * (1 - s) + u) + u
+    _near(db, slope, s * inner * (1 + 2 * d) + np.abs(slope) * (d + u) + lost, "dbeta")
+    # past both ends, and nothing there: the ends of the formula as a division gives them
+    ends = _f32([0.0, -1e4, 1e4, -3e38, 3e38, float("inf"), float("nan"), 1.0])
+    y = ew.gn_forward(x[..., :8].contiguous(), 4, zero[:8], ends, act="silu")[0].reshape(8).float().cpu()
+    if prec_name == "fp32":
+        assert y[1] == 0 and y[3] == 0
+    assert y[0] == 0 and y[2] == ends[2].to(dt).float() and y[5] == float("inf") and torch.isnan(y[6]) and torch.isfinite(y[7])
