@@ -54,6 +54,10 @@ struct Geom {
   uint32_t col_mul, cg_mul; // tid / cols = tid * col_mul >> 16;  c / Cg = the high word of c * cg_mul (0: Cg = 1)
   int tiles;                // tiles of columns (1 unless streamed with more than 2048 channels)
   float inv_m;              // 1 / (P * Cg)
+  int team;                 // team form: threads that take an image
+  int entries, per_row;     // what a group's sums add in a row of threads: its columns or, where columns are cut, its channels
+  int lanes_log, rows_on, cols_on;      // of a group's lanes: how many (log2), and how far apart in rows and entries a lane's terms are
+  int buffers;              // images that a team has room for
 };
 constexpr int kMergeParts = 16;             // rows of sums that the second streamed pass adds up itself
 constexpr int kForwardPerSm = 3, kBackwardPerSm = 2;      // CTAs on an SM: 80 and 128 registers a thread
@@ -197,8 +201,8 @@ struct Place {
   int col, r;
   bool active;
   int c0, left;               // first channel, channels of the column that exist
-  __device__ __forceinline__ Place(const Geom& g, int tile) {
-    r = (int)(threadIdx.x * g.col_mul >> 16); col = (int)threadIdx.x - r * g.cols;
+  __device__ __forceinline__ Place(const Geom& g, int tile, uint32_t tid = threadIdx.x) {
+    r = (int)(tid * g.col_mul >> 16); col = (int)tid - r * g.cols;
     active = r < g.rp;
     c0 = (tile * kMaxCols + col) * 8;
     left = min(8, g.C - c0);
@@ -607,6 +611,154 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_kernel(const 
     out.template turn<false>(k, sh.mine, false, affine, xs, rs);
   }
   cluster.barrier_wait(std::move(token));                                 // nor do they read its own
+}
+
+// The team form, for small images: `team` threads (32 to 256, whole warps) take an image, a CTA the images that its teams have room
+// for, each team one after the other with the next one's copy under way; a team waits for nobody else.  An image is in shared
+// memory, so its mean comes first and the squares of what is left of it after, from sums over groups (a value per thread where
+// columns lie in one group each).  What a CTA per image spends on starting, on exchanging sums and on its end is the time of these
+// calls: us, with the other forms / with this one, 16-bit storage: 4096x2x2x64 54 / 4.9, 4096x4x4x256 66 / 14, 1024x8x8x160 23 / 10,
+// 20000x1x512 284 / 26, 128x8x8x160 6.4 / 4.6, one image of 8x8x64 4.9 / 3.2.  Bound by issue slots at one pixel per image (a quarter of the
+// copy rate), by memory from a few kilobytes per image on (60 to 72 %).  A pixel at a time: two cost spilled registers (14.3 against 16.4).
+struct Team {
+  int first, tid, size;       // its first thread, this thread's number in it
+  int sub, set, r0, j0;       // which of a group's lanes, of which of the first groups; where that lane's terms start
+  __device__ __forceinline__ explicit Team(const Geom& g)
+      : first(threadIdx.x & ~(g.team - 1)), tid(threadIdx.x & (g.team - 1)), size(g.team), sub(tid & (g.lanes_g - 1)), set(tid >> g.lanes_log),
+        r0(sub / g.entries), j0(sub - r0 * g.entries) {}
+  __device__ __forceinline__ void sync() const {
+    if (size == 32) __syncwarp();
+    else asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + first / 32), "r"(size) : "memory");
+  }
+};
+// red = what a thread adds to its groups' sums: a value where its column is in one group, else one per channel.
+__device__ __forceinline__ void team_put(float* red, const Geom& g, const Place& at, const F8& v) {
+  if (!at.active) return;
+  float* d = red + (at.r * g.per_row) + at.col * (g.entries == g.Cg ? 8 : 1);
+  if (g.entries == g.Cg) {
+    reinterpret_cast<ulonglong2*>(d)[0] = make_ulonglong2(v.p[0], v.p[1]);
+    reinterpret_cast<ulonglong2*>(d)[1] = make_ulonglong2(v.p[2], v.p[3]);
+  } else {
+    const float2 t = halves(add2(add2(v.p[0], v.p[1]), add2(v.p[2], v.p[3])));
+    *d = t.x + t.y;
+  }
+}
+// done(s, the sum over group s).
+template <typename Done> __device__ __forceinline__ void team_group_sums(const Geom& g, const Team& t, const float* red, Done done) {
+  const int n = g.entries;
+  for (int s0 = 0; s0 < g.G; s0 += t.size >> g.lanes_log) {
+    const int s = s0 + t.set;
+    float a = 0.f;
+    if (s < g.G) {
+      const float* v = red + s * n;
+      for (int r = t.r0, j = t.j0; r < g.rp;) {
+        a += v[r * g.per_row + j];
+        r += g.rows_on; j += g.cols_on;
+        if (j >= n) { j -= n; ++r; }
+      }
+    }
+    a = lane_sum(a, g.lanes_g);
+    if (s < g.G && t.sub == 0) done(s, a);
+  }
+}
+// A group's value for each channel of a thread's column.
+template <typename Value> __device__ __forceinline__ void team_values(const Geom& g, const Place& at, Value value, float (&m)[8]) {
+  if (g.entries == g.Cg) {
+    each_channel(g, at, [&](int i, int, int s) { m[i] = value(s); });
+  } else {
+    const float v = value(group_of(g, at.c0));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m[i] = v;
+  }
+}
+template <typename T, int W, int ACT, int EXTRA>
+__global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_teams_kernel(const __grid_constant__ Forward<T> p) {
+  extern __shared__ uint4 smem[];
+  const Geom& g = p.g;
+  const Team t(g);
+  const Place at(g, 0, (uint32_t)t.tid);
+  const Slots<T> slots(smem);                                                                   // two images, iters of each
+  float* red = reinterpret_cast<float*>(smem + (size_t)g.buffers * g.iters * Slots<T>::Q * kThreads) + t.first * 8;      // [8 * team]
+  float2* mom = reinterpret_cast<float2*>(reinterpret_cast<float*>(smem + (size_t)g.buffers * g.iters * Slots<T>::Q * kThreads) + 8 * kThreads) +
+                (t.first / t.size) * g.G;                                                       // [G]: mean, rstd
+  const int teams = kThreads / t.size, stride = gridDim.x * teams;
+  const uint32_t first = (uint32_t)at.r * g.C + at.c0, step = (uint32_t)g.rp * g.C;
+  const int mine = Share(g, at, 0, 0).mine;
+  auto fetch = [&](int n, int buf) {
+    const T* src = p.x + (size_t)n * g.P * g.C + first;
+    for (int k = 0; k < mine; ++k) slots.template fetch<W>(buf * g.iters + k, src + (uint32_t)k * step, at.left);
+    if constexpr (EXTRA >= WITH_RES_GATE)
+      if (p.res)
+        for (int k = 0; k < mine; ++k) prefetch_l2(p.res + (size_t)n * g.P * g.C + (first + (uint32_t)k * step));
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int n = blockIdx.x * teams + t.first / t.size, buf = 0;
+  grid_dependency_wait();
+  if (n < g.N) fetch(n, 0);
+  float gamma[8], beta[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { gamma[i] = p.gamma[at.channel(i)]; beta[i] = p.beta[at.channel(i)]; }
+  for (; n < g.N; n += stride, buf ^= 1) {
+    if (n < g.N - stride) fetch(n + stride, buf ^ 1);
+    else asm volatile("cp.async.commit_group;" ::: "memory");
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    const int at0 = buf * g.iters;
+    F8 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v.p[j] = 0;
+    for (int k = 0; k < mine; ++k) {
+      const F8 x = raw8_to_f8(slots.get(at0 + k));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v.p[j] = add2(v.p[j], x.p[j]);
+    }
+    team_put(red, g, at, v);
+    t.sync();
+    team_group_sums(g, t, red, [&](int s, float a) { mom[s].x = a * g.inv_m; });
+    t.sync();
+    F8 less;
+    {
+      float m[8];
+      team_values(g, at, [&](int s) { return mom[s].x; }, m);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { less.p[j] = pair(-m[2 * j], -m[2 * j + 1]); v.p[j] = 0; }
+    }
+    for (int k = 0; k < mine; ++k) {
+      const F8 x = raw8_to_f8(slots.get(at0 + k));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x2 d = add2(x.p[j], less.p[j]);
+        v.p[j] = fma2(d, d, v.p[j]);
+      }
+    }
+    team_put(red, g, at, v);
+    t.sync();
+    team_group_sums(g, t, red, [&](int s, float a) {
+      const float rstd = 1.f / sqrtf(fmaf(a, g.inv_m, p.eps));
+      mom[s].y = rstd;
+      p.stats[(size_t)n * g.G + s] = mom[s].x;
+      p.stats[(size_t)(g.N + n) * g.G + s] = rstd;
+    });
+    t.sync();
+    Affine<T> affine;
+    float rstd[8];
+    team_values(g, at, [&](int s) { return mom[s].y; }, rstd);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 m = halves(less.p[j]);
+      affine.set(j, make_float2(-m.x, -m.y), make_float2(gamma[2 * j] * rstd[2 * j], gamma[2 * j + 1] * rstd[2 * j + 1]), make_float2(beta[2 * j], beta[2 * j + 1]));
+    }
+    const Share sh(g, at, n, 0);
+    const Emitter<T, W, ACT, EXTRA> out(p, at, sh);
+    Raw8<T> next_res{};
+    if constexpr (EXTRA >= WITH_RES_GATE)
+      if (out.res && mine > 0) next_res = raw8_load<T, W>(out.res + out.first, at.left);
+    for (int k = 0; k < (EXTRA == WITH_CODES ? sh.turns : mine); ++k) {
+      const Raw8<T> xs[1] = {slots.get(at0 + min(k, g.iters - 1))}, rs[1] = {next_res};
+      if constexpr (EXTRA >= WITH_RES_GATE)
+        if (out.res && k + 1 < mine) next_res = raw8_load<T, W>(out.res + (out.first + (uint32_t)(k + 1) * step), at.left);
+      out.template turn<false>(k, mine, false, affine, xs, rs);
+    }
+  }
 }
 
 // Streamed, first pass: moments of each group (with tiles > 1: of each channel) over a CTA's pixels.
@@ -1151,8 +1303,9 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_apply_kerne
 // ---- host side: plans ----------------------------------------------------------------------------------------
 struct Plan {
   Geom g;
-  bool resident;
-  size_t smem;                // dynamic shared memory of the resident kernel
+  bool resident;              // one launch and no scratch: a cluster per image, or (g.team) the team form
+  size_t smem;                // dynamic shared memory of the resident kernels
+  int ctas;                   // of the team form
 };
 inline int pow2_up_to(int64_t most, int cap) {
   int v = 1;
@@ -1193,7 +1346,53 @@ inline Plan plan_streamed(int N, int P, int C, int G, int per_sm) {
 // allows), with as many CTAs per image as that gives, and where they fill at least half of the SMs or a thread has few pixels.
 // us, resident / streamed, 16-bit storage: 8x16x16x8 4.6 / 5.4, 128x16x16x160 8.2 / 10.3, 128x8x8x640 8.7 / 10.8; on the other
 // side of the rule 2x64x64x128 with SiLU 12.2 / 10.0, and 128 images of 32x32x160 in more than one wave 31.5 / 23.4.
+// The team form: the size of a team that gives the least of (rounds of images per team) * (pixels per thread + 4, the fixed part of
+// a round, in pixels), the larger team where two are alike.  Teams smaller than a CTA only where they leave no SM without one
+// (37x28x28x30 on 19 SMs: 12 us for 8.4); with a CTA per image at most 12 pixels a thread, beyond which a cluster or the streamed
+// form is as fast without codes and faster with them (128x16x16x160, 22 pixels: 7.5 / 8.2 and 13 / 10.5).
+inline Plan plan_teams(int vec_bytes, int N, int P, int C, int G) {
+  Plan best{};
+  const int cols = C / 8 + (C % 8 != 0);
+  int64_t least = INT64_MAX;
+  for (int team = kThreads; team >= 32 && team >= cols; team /= 2) {
+    const int rp = team / cols, iters = P / rp + (P % rp != 0), teams = kThreads / team;
+    const int64_t all = N / teams + (N % teams != 0);
+    if (team < kThreads ? all < kSms : iters > 12) continue;
+    if (iters > 48) break;          // no room
+    Plan pl{};
+    pl.resident = true;
+    Geom& g = pl.g;
+    g.N = N; g.P = P; g.C = C; g.G = G; g.Cg = C / G;
+    g.cols = cols; g.rp = rp; g.team = team; g.tiles = 1;
+    g.inv_m = (float)(1.0 / ((double)P * g.Cg));
+    g.col_mul = (65536 + cols - 1) / cols;
+    g.cg_mul = g.Cg == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + g.Cg - 1) / g.Cg);
+    g.lanes_g = pow2_up_to(team / std::min(G, team), 32);
+    while (1 << g.lanes_log < g.lanes_g) ++g.lanes_log;
+    g.entries = g.Cg % 8 ? g.Cg : g.Cg / 8;
+    g.per_row = g.Cg % 8 ? cols * 8 : cols;
+    g.rows_on = g.lanes_g / g.entries;
+    g.cols_on = g.lanes_g % g.entries;
+    split(g, 1);
+    const size_t own = 32 * kThreads + 8 * (size_t)teams * G;
+    int64_t at_once = 0;
+    for (g.buffers = 1; at_once < all && g.buffers <= 2; ++g.buffers) {      // a second one where a team has a second image
+      pl.smem = (size_t)vec_bytes * iters * kThreads * g.buffers + own;
+      at_once = (int64_t)kSms * std::min<size_t>(kForwardPerSm, kSmemOfSm / (pl.smem + 1024));
+    }
+    --g.buffers;
+    if (pl.smem > kSmemMost) continue;
+    const int64_t cost = (all + at_once - 1) / at_once * (iters + 4);
+    if (cost >= least) continue;
+    pl.ctas = (int)std::min(all, at_once);
+    least = cost;
+    best = pl;
+  }
+  return best;
+}
 inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G) {
+  const Plan small = plan_teams(8 * elem_bytes, N, P, C, G);
+  if (small.g.team) return small;
   Plan pl = plan_streamed(N, P, C, G, kForwardPerSm);
   if (pl.g.tiles > 1) return pl;
   Plan res = pl;
@@ -1234,6 +1433,11 @@ inline cudaError_t launch_cluster(Kernel kernel, int images, int cluster, size_t
 
 template <typename T, int W, int ACT, int EXTRA> inline cudaError_t launch_forward_as(cudaStream_t st, const Plan& pl, Forward<T> p) {
   const Geom& g = pl.g;
+  if (g.team) {
+    static OncePerDevice once;
+    const cudaError_t e = once_per_device(&once, []() { return set_smem_limit(forward_teams_kernel<T, W, ACT, EXTRA>, kSmemMost); });
+    return e != cudaSuccess ? e : launch_chained(forward_teams_kernel<T, W, ACT, EXTRA>, dim3((unsigned)pl.ctas), dim3(kThreads), pl.smem, st, p);
+  }
   if (pl.resident) {
     static OncePerDevice once;
     const cudaError_t e = once_per_device(&once, []() { return set_smem_limit(forward_kernel<T, W, ACT, EXTRA>, kSmemMost); });

@@ -505,3 +505,46 @@ def test_silu_over_its_range(prec_name):
     if prec_name == "fp32":
         assert y[1] == 0 and y[3] == 0
     assert y[0] == 0 and y[2] == ends[2].to(dt).float() and y[5] == float("inf") and torch.isnan(y[6]) and torch.isfinite(y[7])
+
+
+# many small images: a few rows of threads each, several to a CTA, more than run at once; groups inside and across columns
+SMALL = [
+    (4096, 4, 64, 4), (2000, 9, 128, 32), (2000, 1, 512, 32), (900, 3, 30, 6), (1300, 7, 33, 11), (601, 21, 160, 32), (3001, 2, 8, 1),
+    (500, 200, 3, 1), (700, 5, 264, 3), (450, 2, 2048, 16), (450, 3, 1000, 1), (500, 1, 2048, 2048), (2999, 1, 1, 1), (150, 90, 40, 40),
+    (450, 5, 640, 8), (20011, 1, 48, 2), (300, 100, 64, 8), (1100, 25, 96, 4),
+]
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("shape", SMALL, ids=str)
+def test_many_small_images(prec_name, shape):
+    _, ew = _ops(prec_name)
+    _check_forward(ew, shape, "relu", True, seed=60, gate=True, ckpt=True)
+    for seed, act in ((70, "none"), (80, "relu"), (90, "silu")):
+        x, xo, y, stats, bits, held = _check_forward(ew, shape, act, False, seed=seed, gate=act == "relu", ckpt=act == "silu")
+        _check_backward(ew, shape, act, seed, xo, x, stats, y, bits, act == "none", False)
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+def test_small_images_far_from_zero_and_not_finite(prec_name):
+    """The variance of values far from zero, and one image with an infinity and one with a NaN: only these are lost."""
+    _, ew = _ops(prec_name)
+    n, p, c, groups = 700, 9, 64, 4
+    x, xo = _mk((n, p, c), 3, ew.dtype, 1.0, 300.0)
+    x[5, 3, 7], x[600, 0, 63] = float("inf"), float("nan")
+    xo = x.double().cpu().numpy()
+    gamma, beta = _params(c, 4)
+    y, stats, _, held = ew.gn_forward(x, groups, _f32(gamma), _f32(beta), act="silu", checkpoint=True)
+    lost = np.zeros((n, groups), bool)
+    lost[5, 0] = lost[600, 3] = True
+    st = _np(stats)
+    assert np.isnan(st[0][600, 3]) and not np.isfinite(st[0][5, 0]) and np.isfinite(st[:, ~lost]).all()
+    back = _np(ew.ckpt_decode(held))
+    clean = [i for i in range(n) if i not in (5, 600)]
+    want = L.groupnorm_stats(xo[clean], groups, EPS)
+    mag = np.abs(xo[clean]).reshape(len(clean), p, groups, -1).mean((1, 3))
+    _near(st[0][clean], want[0], K * mag, "mean")
+    _near(st[1][clean], want[1], want[1] * (K + (K * mag * want[1]) ** 2), "rstd")
+    assert np.isfinite(_np(y)[clean]).all() and np.isfinite(back[clean]).all()
+    yl = np.isnan(_np(y).reshape(n, p, groups, -1)).all((1, 3))
+    assert yl[600, 3] and yl[5, 0] and yl.sum() == 2
