@@ -21,12 +21,14 @@
 // Resident, forward only (plan_forward): a cluster of up to 8 CTAs takes an image, each a share of its pixels, which it copies to
 // shared memory at once (every thread its own vectors, so nothing but a thread's own wait stands between copy and use).  The
 // moments are formed there, exchanged through distributed shared memory, and applied from there: one launch, one read, one write.
-// (A resident backward pass was no faster anywhere: its parameter gradients need a second launch all the same.)
+// (A backward pass by clusters was no faster anywhere: its parameter gradients need a second launch all the same.)
+// In teams (plan_teams): small images, several to a CTA, one after the other.
 //
 // Variance: a thread sums its values and their squares less its first value, brings them about a common value of the CTA (the
 // mean of the channel's first row of threads), then about the CTA's group mean, and CTAs are combined by Chan's formula.  The
 // square of the distance from a mean over a share f of the values to the mean over all is at most var*(1 - f)/f, so what cancels
-// in each step is bounded by the data itself (by the number of a thread's values, then by rp), whatever offset x has.
+// in each step is bounded by the data itself (by the number of a thread's values, then by rp), whatever offset x has.  The team form
+// has the image at hand and takes the mean first.
 // All sums are fp32 within a CTA (a chain of a thread's values, then of rows of threads, then a tree), in a fixed order.
 #pragma once
 #include <cooperative_groups.h>
@@ -1223,6 +1225,171 @@ __global__ void __launch_bounds__(1024) totals_kernel(const float* __restrict__ 
            [&](int i, float v) { totals[(size_t)n * width + i] = v; });
 }
 
+// The team form of the backward pass: both passes over an image from shared memory.  A team adds its images' A and B up in registers (at
+// most kTeamImages of them, so that sums stay short), a CTA leaves one row of its teams' in scratch for parameters_kernel.  What ReLU
+// passes of dy replaces it in shared memory, so that the mask or its bits are read once.  us, streamed / this form, 16-bit storage, no
+// activation: 4096x2x2x64 62 / 9, 4096x4x4x256 74 / 28, 2000x7x7x128 39 / 34, 20000x1x512 365 / 37; from codes and bits 75 / 10, 90 / 40,
+// 48 / 42, 437 / 45.  Bound by issue slots, at one pixel per image by what an image costs beside its values.
+constexpr int kTeamImages = 128;
+template <typename T, int W, bool CK, int SLOPE>
+__global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_teams_kernel(const __grid_constant__ Backward<T> p) {
+  extern __shared__ uint4 smem[];
+  const Geom& g = p.g;
+  const int slope = SLOPE < 0 ? p.slope : SLOPE;
+  const Team t(g);
+  const Place at(g, 0, (uint32_t)t.tid);
+  const int vectors = g.buffers * g.iters * Slots<T>::Q * kThreads;          // 16-byte words of an operand
+  const Slots<T> dys(smem), xs(smem + vectors);
+  uint2* const codes = reinterpret_cast<uint2*>(smem + vectors) + threadIdx.x;
+  float* const all = reinterpret_cast<float*>(smem + 2 * vectors);           // [2][kThreads * 8]
+  float* const red = all + t.first * 8;
+  float* const own = all + 2 * kThreads * 8 + (t.first / t.size) * 6 * g.G;  // [2][2][G]: mean, rstd of two images
+  float* const coef = own + 4 * g.G;                                         // [2][G]
+  const int teams = kThreads / t.size, stride = gridDim.x * teams;
+  const uint32_t first = (uint32_t)at.r * g.C + at.c0, step = (uint32_t)g.rp * g.C;
+  const int mine = Share(g, at, 0, 0).mine;
+  auto fetch = [&](int n, int buf) {
+    const size_t off = (size_t)n * g.P * g.C + first;
+    for (int k = 0; k < mine; ++k) {
+      const size_t o = off + (uint32_t)k * step;
+      const int slot = buf * g.iters + k;
+      dys.template fetch<W>(slot, p.dy + o, at.left);
+      if constexpr (CK) {
+        if constexpr (W == kWhole) copy8_async(codes + slot * kThreads, p.codes + o);
+        else codes[slot * kThreads] = load_codes<kCodeWidth<T, W>>(p.codes + o, at.left);
+      } else {
+        xs.template fetch<W>(slot, p.x + o, at.left);
+      }
+      if (slope == SLOPE_MASK) prefetch_l2(p.mask + o);
+      if (p.res) prefetch_l2(p.res + o);
+    }
+    for (int s = t.tid; s < g.G; s += t.size) {
+      copy_piece_async<4>(own + buf * 2 * g.G + s, p.stats + (size_t)n * g.G + s, true);
+      copy_piece_async<4>(own + (buf * 2 + 1) * g.G + s, p.stats + (size_t)(g.N + n) * g.G + s, true);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int n = blockIdx.x * teams + t.first / t.size, buf = 0;
+  grid_dependency_wait();
+  grid_dependency_release();
+  if (n < g.N) fetch(n, 0);
+  float gamma[8], beta[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    gamma[i] = p.gamma[at.channel(i)];
+    beta[i] = slope == SLOPE_SILU ? p.beta[at.channel(i)] : 0.f;
+  }
+  float A[8], B[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) A[i] = B[i] = 0.f;
+  for (; n < g.N; n += stride, buf ^= 1) {
+    if (n < g.N - stride) fetch(n + stride, buf ^ 1);
+    else asm volatile("cp.async.commit_group;" ::: "memory");
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    t.sync();                         // the statistics are the team's
+    const int at0 = buf * g.iters;
+    const float *means = own + buf * 2 * g.G, *rstds = means + g.G;
+    Channels ch;
+    float rstd[8];
+    {
+      float mean[8];
+      team_values(g, at, [&](int s) { return means[s]; }, mean);
+      team_values(g, at, [&](int s) { return rstds[s]; }, rstd);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        ch.less[j] = pair(-mean[2 * j], -mean[2 * j + 1]);
+        ch.scale[j] = pair(gamma[2 * j] * rstd[2 * j], gamma[2 * j + 1] * rstd[2 * j + 1]);
+        ch.shift[j] = pair(beta[2 * j], beta[2 * j + 1]);
+      }
+    }
+    const Share sh(g, at, n, 0);
+    const Columns<T> from(p, at, sh);
+    auto held = [&](int k) {
+      Held<T, CK> h;
+      h.dy = dys.get(at0 + k);
+      if constexpr (CK) {
+        h.codes = codes[(at0 + k) * kThreads];
+        h.scale = from.scales[from.scale_first + (uint32_t)k * from.scale_step];
+      } else {
+        h.x = xs.get(at0 + k);
+      }
+      return h;
+    };
+    Sums sums;
+    for (int k = 0; k < mine; ++k) {
+      Held<T, CK> h = held(k);
+      if (slope == SLOPE_MASK) h.mask = raw8_load<T, W>(from.mask + (from.first + (uint32_t)k * from.step), at.left);
+      if (slope == SLOPE_BITS) h.open = from.gate[from.gate_first + (uint32_t)k * from.gate_step];
+      const Raw8<T> dy = passed<T, CK>(h, slope);
+      if (slope == SLOPE_MASK || slope == SLOPE_BITS) dys.put(at0 + k, dy);
+      F8 dz, d;
+      operands<T, CK>(dy, h, slope, ch, dz, d);
+      sums.add(dz, d);
+    }
+    F8 w1, w2;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 a = halves(sums.a.p[j]), b = halves(sums.b.p[j]);
+      const float a0 = a.x * rstd[2 * j], a1 = a.y * rstd[2 * j + 1];
+      A[2 * j] += a0; A[2 * j + 1] += a1;
+      B[2 * j] += b.x; B[2 * j + 1] += b.y;
+      w1.p[j] = pair(gamma[2 * j] * b.x, gamma[2 * j + 1] * b.y);
+      w2.p[j] = pair(gamma[2 * j] * a0, gamma[2 * j + 1] * a1);
+    }
+    team_put(red, g, at, w1);
+    team_put(red + kThreads * 8, g, at, w2);
+    t.sync();
+    team_group_sums(g, t, red, [&](int s, float v) { coef[s] = -(rstds[s] * v * g.inv_m); });
+    team_group_sums(g, t, red + kThreads * 8, [&](int s, float v) { coef[g.G + s] = -(rstds[s] * rstds[s] * v * g.inv_m); });
+    t.sync();
+    f32x2 k1[4], k2[4];
+    {
+      float c1[8], c2[8];
+      team_values(g, at, [&](int s) { return coef[s]; }, c1);
+      team_values(g, at, [&](int s) { return coef[g.G + s]; }, c2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { k1[j] = pair(c1[2 * j], c1[2 * j + 1]); k2[j] = pair(c2[2 * j], c2[2 * j + 1]); }
+    }
+    T* const dx = p.dx + sh.row0 * g.C;
+    const T* const res = p.res ? p.res + sh.row0 * g.C : nullptr;
+    Raw8<T> next{};
+    if (res && mine > 0) next = raw8_load<T, W>(res + first, at.left);
+    for (int k = 0; k < mine; ++k) {
+      const Raw8<T> r = next;
+      if (res && k + 1 < mine) next = raw8_load<T, W>(res + (first + (uint32_t)(k + 1) * step), at.left);
+      const Held<T, CK> h = held(k);
+      raw8_put<T, W>(dx + (first + (uint32_t)k * step), at.left, dx_of<T, CK>(h.dy, h, slope, ch, k1, k2, res ? &r : nullptr));
+    }
+  }
+  __syncthreads();
+  put_sums(red, g, at, A);
+  put_sums(red + kThreads * 8, g, at, B);
+  __syncthreads();
+  float* const out = p.partial + (size_t)blockIdx.x * 2 * g.C;
+  const int lanes = g.lanes_c, sub = threadIdx.x & (lanes - 1), rows = teams * g.rp;
+  for (int c0 = 0; c0 < g.C; c0 += kThreads / lanes) {
+    const int c = c0 + threadIdx.x / lanes;
+    float a = 0.f, b = 0.f;
+    if (c < g.C)
+      for (int i = sub; i < rows; i += lanes) {
+        const int team = i / g.rp;
+        const float* v = all + (team * t.size + (i - team * g.rp) * g.cols) * 8 + c;
+        a += v[0]; b += v[kThreads * 8];
+      }
+    a = lane_sum(a, lanes);
+    b = lane_sum(b, lanes);
+    if (c < g.C && sub == 0) { out[c] = a; out[g.C + c] = b; }
+  }
+}
+// dgamma and dbeta, 32 of them, from `rows` rows of sums.
+__global__ void __launch_bounds__(1024) parameters_kernel(const float* __restrict__ partial, int rows, int C, float* __restrict__ dgamma,
+                                                          float* __restrict__ dbeta) {
+  __shared__ double fin[32][33];
+  grid_dependency_wait();
+  grid_dependency_release();
+  add_rows(partial, rows, 2 * C, blockIdx.x * 32, fin, [&](int i, float v) { (i < C ? dgamma + i : dbeta + (i - C))[0] = v; });
+}
+
 // Second pass: dx.  Every CTA forms S1 and S2 of its tile's groups from the image's totals, or from its rows of sums.
 // The first `extra` CTAs of a share add up the parameter gradients, 32 values each.
 template <typename T, int W, bool CK, int SLOPE>
@@ -1306,6 +1473,7 @@ struct Plan {
   bool resident;              // one launch and no scratch: a cluster per image, or (g.team) the team form
   size_t smem;                // dynamic shared memory of the resident kernels
   int ctas;                   // of the team form
+  int64_t rows;               // of sums in scratch
 };
 inline int pow2_up_to(int64_t most, int cap) {
   int v = 1;
@@ -1340,24 +1508,26 @@ inline Plan plan_streamed(int N, int P, int C, int G, int per_sm) {
   g.lanes_c = pow2_up_to(kThreads / std::min(g.cols * 8, kThreads), 32);
   split(g, (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)per_sm * kSms / N, P / (4 * g.rp))));
   g.parts = P / g.pix + (P % g.pix != 0);         // none without pixels
+  pl.rows = (int64_t)N * g.parts;
   return pl;
 }
-// The resident form where an image fits a cluster and all of a call's CTAs run at once (two on an SM, if their shared memory
-// allows), with as many CTAs per image as that gives, and where they fill at least half of the SMs or a thread has few pixels.
-// us, resident / streamed, 16-bit storage: 8x16x16x8 4.6 / 5.4, 128x16x16x160 8.2 / 10.3, 128x8x8x640 8.7 / 10.8; on the other
-// side of the rule 2x64x64x128 with SiLU 12.2 / 10.0, and 128 images of 32x32x160 in more than one wave 31.5 / 23.4.
 // The team form: the size of a team that gives the least of (rounds of images per team) * (pixels per thread + 4, the fixed part of
-// a round, in pixels), the larger team where two are alike.  Teams smaller than a CTA only where they leave no SM without one
-// (37x28x28x30 on 19 SMs: 12 us for 8.4); with a CTA per image at most 12 pixels a thread, beyond which a cluster or the streamed
-// form is as fast without codes and faster with them (128x16x16x160, 22 pixels: 7.5 / 8.2 and 13 / 10.5).
-inline Plan plan_teams(int vec_bytes, int N, int P, int C, int G) {
+// a round, in pixels), the larger team where two are alike; none where an image does not fit.  vec_bytes: of a thread's pixel in shared
+// memory; shared, per_group: bytes of a CTA, of a team's group beside them.
+// Forward (`most` = 12): teams smaller than a CTA only where they leave no SM without one (37x28x28x30 on 19 SMs: 12 us for 8.4); with
+// a CTA per image at most 12 pixels a thread, beyond which a cluster or the streamed form is as fast without codes and faster with
+// them (128x16x16x160, 22 pixels: 7.5 / 8.2 and 13 / 10.5).
+// Backward (`most` = 4, `fill`): with fewer CTAs than SMs the streamed form is faster (8x16x16x8 4.9 / 6.9 us), and where only one CTA
+// fits an SM too (1024x8x8x160 from codes and bits 31.8 / 35, fp32 41.8 / 59); with a CTA per image, 8 pixels a thread 14.9 / 20.0 (400x32x32x16).
+inline Plan plan_teams(int vec_bytes, bool fill, int per_sm, size_t shared, int per_group, int most, int N, int P, int C, int G) {
   Plan best{};
   const int cols = C / 8 + (C % 8 != 0);
   int64_t least = INT64_MAX;
   for (int team = kThreads; team >= 32 && team >= cols; team /= 2) {
     const int rp = team / cols, iters = P / rp + (P % rp != 0), teams = kThreads / team;
     const int64_t all = N / teams + (N % teams != 0);
-    if (team < kThreads ? all < kSms : iters > 12) continue;
+    if ((fill || team < kThreads) && all < kSms) continue;
+    if (team == kThreads && iters > most) continue;
     if (iters > 48) break;          // no room
     Plan pl{};
     pl.resident = true;
@@ -1368,20 +1538,21 @@ inline Plan plan_teams(int vec_bytes, int N, int P, int C, int G) {
     g.col_mul = (65536 + cols - 1) / cols;
     g.cg_mul = g.Cg == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + g.Cg - 1) / g.Cg);
     g.lanes_g = pow2_up_to(team / std::min(G, team), 32);
+    g.lanes_c = pow2_up_to(kThreads / std::min(C, kThreads), 32);
     while (1 << g.lanes_log < g.lanes_g) ++g.lanes_log;
     g.entries = g.Cg % 8 ? g.Cg : g.Cg / 8;
     g.per_row = g.Cg % 8 ? cols * 8 : cols;
     g.rows_on = g.lanes_g / g.entries;
     g.cols_on = g.lanes_g % g.entries;
     split(g, 1);
-    const size_t own = 32 * kThreads + 8 * (size_t)teams * G;
+    const size_t own = shared + (size_t)per_group * teams * G;
     int64_t at_once = 0;
     for (g.buffers = 1; at_once < all && g.buffers <= 2; ++g.buffers) {      // a second one where a team has a second image
       pl.smem = (size_t)vec_bytes * iters * kThreads * g.buffers + own;
-      at_once = (int64_t)kSms * std::min<size_t>(kForwardPerSm, kSmemOfSm / (pl.smem + 1024));
+      at_once = (int64_t)kSms * std::min<size_t>(per_sm, kSmemOfSm / (pl.smem + 1024));
     }
     --g.buffers;
-    if (pl.smem > kSmemMost) continue;
+    if (pl.smem > kSmemMost || (fill && at_once < (int64_t)kSms * per_sm)) continue;
     const int64_t cost = (all + at_once - 1) / at_once * (iters + 4);
     if (cost >= least) continue;
     pl.ctas = (int)std::min(all, at_once);
@@ -1390,12 +1561,17 @@ inline Plan plan_teams(int vec_bytes, int N, int P, int C, int G) {
   }
   return best;
 }
+// The team form for small images, else a cluster where an image fits one and all of a call's CTAs run at once (two on an SM, if their shared memory allows), with
+// as many CTAs per image as that gives, and where they fill at least half of the SMs or a thread has few pixels.
+// us, cluster / streamed, 16-bit storage: 128x16x16x160 8.2 / 10.3, 128x8x8x640 8.7 / 10.8; on the other side of the rule
+// 2x64x64x128 with SiLU 12.2 / 10.0, and 128 images of 32x32x160 in more than one wave 31.5 / 23.4.
 inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G) {
-  const Plan small = plan_teams(8 * elem_bytes, N, P, C, G);
+  const Plan small = plan_teams(8 * elem_bytes, false, kForwardPerSm, 32 * kThreads, 8, 12, N, P, C, G);
   if (small.g.team) return small;
   Plan pl = plan_streamed(N, P, C, G, kForwardPerSm);
   if (pl.g.tiles > 1) return pl;
   Plan res = pl;
+  res.rows = 0;
   for (int parts = kMaxCluster; parts >= 1; parts /= 2) {
     split(res.g, parts);
     if (parts > 1 && res.g.iters < 2) continue;
@@ -1407,8 +1583,17 @@ inline Plan plan_forward(int elem_bytes, int N, int P, int C, int G) {
   }
   return pl;
 }
-inline Plan plan_backward(int N, int P, int C, int G) { return plan_streamed(N, P, C, G, kBackwardPerSm); }
-inline size_t partial_floats(const Plan& pl) { return pl.resident ? 0 : (size_t)pl.g.N * pl.g.parts * 2 * pl.g.C; }
+inline Plan plan_backward(int elem_bytes, int N, int P, int C, int G) {
+  Plan small = plan_teams(2 * 8 * elem_bytes, true, kBackwardPerSm, 64 * kThreads, 24, 4, N, P, C, G);
+  if (small.g.team) {
+    const int64_t images = (int64_t)(kThreads / small.g.team) * kTeamImages;
+    small.ctas = std::max(small.ctas, (int)((N + images - 1) / images));
+    small.rows = small.ctas;
+    return small;
+  }
+  return plan_streamed(N, P, C, G, kBackwardPerSm);
+}
+inline size_t partial_floats(const Plan& pl) { return (size_t)pl.rows * 2 * pl.g.C; }
 // Whether a second streamed pass adds up an image's rows of sums itself.
 inline bool merges(const Geom& g) { return g.tiles == 1 && g.parts <= kMergeParts; }
 // Whether every launch's grid can be given (with many images a plan has one share of each).
@@ -1487,6 +1672,14 @@ template <typename T, int W, bool CK, int SLOPE>
 inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<T> p) {
   const Geom& g = pl.g;
   const int width = 2 * g.C, blocks = (width + 31) / 32;
+  if (g.team) {
+    static OncePerDevice once;
+    cudaError_t e = once_per_device(&once, []() { return set_smem_limit(backward_teams_kernel<T, W, CK, SLOPE>, kSmemMost); });
+    if (e == cudaSuccess) e = launch_chained(backward_teams_kernel<T, W, CK, SLOPE>, dim3((unsigned)pl.ctas), dim3(kThreads), pl.smem, st, p);
+    if (e == cudaSuccess)
+      e = launch_chained(parameters_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, (const float*)p.partial, (int)pl.rows, g.C, p.dgamma, p.dbeta);
+    return e;
+  }
   static OncePerDevice once;
   cudaError_t e = once_per_device(&once, []() {
     const cudaError_t f = set_smem_limit(backward_sums_kernel<T, W, CK, SLOPE>, kSmemMost);

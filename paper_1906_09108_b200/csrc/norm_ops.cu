@@ -75,7 +75,7 @@ fdg_status fdg_gn_scratch_bytes(int precision, const fdg_gn_shape* s, int backwa
     *bytes = forward_need(pl);
     return FDG_OK;
   }
-  const gn::Plan pl = gn::plan_backward(s->N, s->HW, s->C, s->groups);
+  const gn::Plan pl = gn::plan_backward(b, s->N, s->HW, s->C, s->groups);
   if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
   *bytes = backward_need(pl);
   return FDG_OK;
@@ -108,7 +108,7 @@ fdg_status fdg_gn_backward(int precision, const fdg_gn_shape* s, const void* dy,
   const unsigned b = elem_bytes(precision);
   if (!aligned_to(dy, b) || !aligned_to(x, b) || !aligned_to(mask, b) || !aligned_to(res, b) || !aligned_to(dx, b) || !aligned_to(scratch, 256))
     return FDG_ERR_INVALID_ARG;
-  const gn::Plan pl = gn::plan_backward(s->N, s->HW, s->C, s->groups);
+  const gn::Plan pl = gn::plan_backward((int)b, s->N, s->HW, s->C, s->groups);
   if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
   if (!scratch || scratch_bytes < backward_need(pl)) return FDG_ERR_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);

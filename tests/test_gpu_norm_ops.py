@@ -511,7 +511,7 @@ def test_silu_over_its_range(prec_name):
 SMALL = [
     (4096, 4, 64, 4), (2000, 9, 128, 32), (2000, 1, 512, 32), (900, 3, 30, 6), (1300, 7, 33, 11), (601, 21, 160, 32), (3001, 2, 8, 1),
     (500, 200, 3, 1), (700, 5, 264, 3), (450, 2, 2048, 16), (450, 3, 1000, 1), (500, 1, 2048, 2048), (2999, 1, 1, 1), (150, 90, 40, 40),
-    (450, 5, 640, 8), (20011, 1, 48, 2), (300, 100, 64, 8), (1100, 25, 96, 4),
+    (450, 5, 640, 8), (20011, 1, 48, 2), (300, 100, 64, 8), (1100, 25, 96, 4), (800, 6, 20, 5),
 ]
 
 
@@ -519,9 +519,13 @@ SMALL = [
 @pytest.mark.parametrize("shape", SMALL, ids=str)
 def test_many_small_images(prec_name, shape):
     _, ew = _ops(prec_name)
-    _check_forward(ew, shape, "relu", True, seed=60, gate=True, ckpt=True)
+    c = shape[2]
+    for seed, act, gate in ((60, "relu", True), (65, "silu", False)):
+        x, xo, y, stats, bits, held = _check_forward(ew, shape, act, gate, seed=seed, gate=gate, ckpt=True)
+        kept = L.ckpt_decode(held[0].cpu().numpy().reshape(-1, c), held[1].cpu().numpy().reshape(shape[0] * shape[1], -1)).reshape(xo.shape)
+        _check_backward(ew, shape, act, seed, kept, held, stats, y, bits, gate, gate)
     for seed, act in ((70, "none"), (80, "relu"), (90, "silu")):
-        x, xo, y, stats, bits, held = _check_forward(ew, shape, act, False, seed=seed, gate=act == "relu", ckpt=act == "silu")
+        x, xo, y, stats, bits, held = _check_forward(ew, shape, act, False, seed=seed, gate=act == "relu")
         _check_backward(ew, shape, act, seed, xo, x, stats, y, bits, act == "none", False)
 
 
