@@ -60,6 +60,7 @@ struct Geom {
   int entries, per_row;     // what a group's sums add in a row of threads: its columns or, where columns are cut, its channels
   int lanes_log, rows_on, cols_on;      // of a group's lanes: how many (log2), and how far apart in rows and entries a lane's terms are
   int buffers;              // images that a team has room for
+  int slices, slice, Gs;    // a team's part of an image: of how many, its channels and groups (whole ones)
 };
 constexpr int kMergeParts = 16;             // rows of sums that the second streamed pass adds up itself
 constexpr int kForwardPerSm = 3, kBackwardPerSm = 2;      // CTAs on an SM: 80 and 128 registers a thread
@@ -648,10 +649,10 @@ __device__ __forceinline__ void team_put(float* red, const Geom& g, const Place&
 // done(s, the sum over group s).
 template <typename Done> __device__ __forceinline__ void team_group_sums(const Geom& g, const Team& t, const float* red, Done done) {
   const int n = g.entries;
-  for (int s0 = 0; s0 < g.G; s0 += t.size >> g.lanes_log) {
+  for (int s0 = 0; s0 < g.Gs; s0 += t.size >> g.lanes_log) {
     const int s = s0 + t.set;
     float a = 0.f;
-    if (s < g.G) {
+    if (s < g.Gs) {
       const float* v = red + s * n;
       for (int r = t.r0, j = t.j0; r < g.rp;) {
         a += v[r * g.per_row + j];
@@ -660,7 +661,7 @@ template <typename Done> __device__ __forceinline__ void team_group_sums(const G
       }
     }
     a = lane_sum(a, g.lanes_g);
-    if (s < g.G && t.sub == 0) done(s, a);
+    if (s < g.Gs && t.sub == 0) done(s, a);
   }
 }
 // A group's value for each channel of a thread's column.
@@ -678,13 +679,16 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_teams_kernel(
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
   const Team t(g);
-  const Place at(g, 0, (uint32_t)t.tid);
+  const Place at(g, 0, (uint32_t)t.tid);                                                        // in the slice, and
+  Place whole = at;                                                                             // in the image
+  whole.c0 += blockIdx.y * g.slice;
+  const int g_first = blockIdx.y * g.Gs;
   const Slots<T> slots(smem);                                                                   // two images, iters of each
   float* red = reinterpret_cast<float*>(smem + (size_t)g.buffers * g.iters * Slots<T>::Q * kThreads) + t.first * 8;      // [8 * team]
   float2* mom = reinterpret_cast<float2*>(reinterpret_cast<float*>(smem + (size_t)g.buffers * g.iters * Slots<T>::Q * kThreads) + 8 * kThreads) +
-                (t.first / t.size) * g.G;                                                       // [G]: mean, rstd
+                (t.first / t.size) * g.Gs;                                                      // [Gs]: mean, rstd
   const int teams = kThreads / t.size, stride = gridDim.x * teams;
-  const uint32_t first = (uint32_t)at.r * g.C + at.c0, step = (uint32_t)g.rp * g.C;
+  const uint32_t first = (uint32_t)at.r * g.C + whole.c0, step = (uint32_t)g.rp * g.C;
   const int mine = Share(g, at, 0, 0).mine;
   auto fetch = [&](int n, int buf) {
     const T* src = p.x + (size_t)n * g.P * g.C + first;
@@ -699,7 +703,7 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_teams_kernel(
   if (n < g.N) fetch(n, 0);
   float gamma[8], beta[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { gamma[i] = p.gamma[at.channel(i)]; beta[i] = p.beta[at.channel(i)]; }
+  for (int i = 0; i < 8; ++i) { gamma[i] = p.gamma[whole.channel(i)]; beta[i] = p.beta[whole.channel(i)]; }
   for (; n < g.N; n += stride, buf ^= 1) {
     if (n < g.N - stride) fetch(n + stride, buf ^ 1);
     else asm volatile("cp.async.commit_group;" ::: "memory");
@@ -737,8 +741,8 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_teams_kernel(
     team_group_sums(g, t, red, [&](int s, float a) {
       const float rstd = 1.f / sqrtf(fmaf(a, g.inv_m, p.eps));
       mom[s].y = rstd;
-      p.stats[(size_t)n * g.G + s] = mom[s].x;
-      p.stats[(size_t)(g.N + n) * g.G + s] = rstd;
+      p.stats[(size_t)n * g.G + g_first + s] = mom[s].x;
+      p.stats[(size_t)(g.N + n) * g.G + g_first + s] = rstd;
     });
     t.sync();
     Affine<T> affine;
@@ -750,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_teams_kernel(
       affine.set(j, make_float2(-m.x, -m.y), make_float2(gamma[2 * j] * rstd[2 * j], gamma[2 * j + 1] * rstd[2 * j + 1]), make_float2(beta[2 * j], beta[2 * j + 1]));
     }
     const Share sh(g, at, n, 0);
-    const Emitter<T, W, ACT, EXTRA> out(p, at, sh);
+    const Emitter<T, W, ACT, EXTRA> out(p, whole, sh);
     Raw8<T> next_res{};
     if constexpr (EXTRA >= WITH_RES_GATE)
       if (out.res && mine > 0) next_res = raw8_load<T, W>(out.res + out.first, at.left);
@@ -1237,16 +1241,19 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_teams_kerne
   const Geom& g = p.g;
   const int slope = SLOPE < 0 ? p.slope : SLOPE;
   const Team t(g);
-  const Place at(g, 0, (uint32_t)t.tid);
+  const Place at(g, 0, (uint32_t)t.tid);                                     // in the slice, and
+  Place whole = at;                                                          // in the image
+  whole.c0 += blockIdx.y * g.slice;
+  const int g_first = blockIdx.y * g.Gs;
   const int vectors = g.buffers * g.iters * Slots<T>::Q * kThreads;          // 16-byte words of an operand
   const Slots<T> dys(smem), xs(smem + vectors);
   uint2* const codes = reinterpret_cast<uint2*>(smem + vectors) + threadIdx.x;
   float* const all = reinterpret_cast<float*>(smem + 2 * vectors);           // [2][kThreads * 8]
   float* const red = all + t.first * 8;
-  float* const own = all + 2 * kThreads * 8 + (t.first / t.size) * 6 * g.G;  // [2][2][G]: mean, rstd of two images
-  float* const coef = own + 4 * g.G;                                         // [2][G]
+  float* const own = all + 2 * kThreads * 8 + (t.first / t.size) * 6 * g.Gs; // [2][2][Gs]: mean, rstd of two images
+  float* const coef = own + 4 * g.Gs;                                        // [2][Gs]
   const int teams = kThreads / t.size, stride = gridDim.x * teams;
-  const uint32_t first = (uint32_t)at.r * g.C + at.c0, step = (uint32_t)g.rp * g.C;
+  const uint32_t first = (uint32_t)at.r * g.C + whole.c0, step = (uint32_t)g.rp * g.C;
   const int mine = Share(g, at, 0, 0).mine;
   auto fetch = [&](int n, int buf) {
     const size_t off = (size_t)n * g.P * g.C + first;
@@ -1263,9 +1270,9 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_teams_kerne
       if (slope == SLOPE_MASK) prefetch_l2(p.mask + o);
       if (p.res) prefetch_l2(p.res + o);
     }
-    for (int s = t.tid; s < g.G; s += t.size) {
-      copy_piece_async<4>(own + buf * 2 * g.G + s, p.stats + (size_t)n * g.G + s, true);
-      copy_piece_async<4>(own + (buf * 2 + 1) * g.G + s, p.stats + (size_t)(g.N + n) * g.G + s, true);
+    for (int s = t.tid; s < g.Gs; s += t.size) {
+      copy_piece_async<4>(own + buf * 2 * g.Gs + s, p.stats + (size_t)n * g.G + g_first + s, true);
+      copy_piece_async<4>(own + (buf * 2 + 1) * g.Gs + s, p.stats + (size_t)(g.N + n) * g.G + g_first + s, true);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -1276,8 +1283,8 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_teams_kerne
   float gamma[8], beta[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    gamma[i] = p.gamma[at.channel(i)];
-    beta[i] = slope == SLOPE_SILU ? p.beta[at.channel(i)] : 0.f;
+    gamma[i] = p.gamma[whole.channel(i)];
+    beta[i] = slope == SLOPE_SILU ? p.beta[whole.channel(i)] : 0.f;
   }
   float A[8], B[8];
 #pragma unroll
@@ -1288,7 +1295,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_teams_kerne
     asm volatile("cp.async.wait_group 1;" ::: "memory");
     t.sync();                         // the statistics are the team's
     const int at0 = buf * g.iters;
-    const float *means = own + buf * 2 * g.G, *rstds = means + g.G;
+    const float *means = own + buf * 2 * g.Gs, *rstds = means + g.Gs;
     Channels ch;
     float rstd[8];
     {
@@ -1303,7 +1310,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_teams_kerne
       }
     }
     const Share sh(g, at, n, 0);
-    const Columns<T> from(p, at, sh);
+    const Columns<T> from(p, whole, sh);
     auto held = [&](int k) {
       Held<T, CK> h;
       h.dy = dys.get(at0 + k);
@@ -1340,13 +1347,13 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_teams_kerne
     team_put(red + kThreads * 8, g, at, w2);
     t.sync();
     team_group_sums(g, t, red, [&](int s, float v) { coef[s] = -(rstds[s] * v * g.inv_m); });
-    team_group_sums(g, t, red + kThreads * 8, [&](int s, float v) { coef[g.G + s] = -(rstds[s] * rstds[s] * v * g.inv_m); });
+    team_group_sums(g, t, red + kThreads * 8, [&](int s, float v) { coef[g.Gs + s] = -(rstds[s] * rstds[s] * v * g.inv_m); });
     t.sync();
     f32x2 k1[4], k2[4];
     {
       float c1[8], c2[8];
       team_values(g, at, [&](int s) { return coef[s]; }, c1);
-      team_values(g, at, [&](int s) { return coef[g.G + s]; }, c2);
+      team_values(g, at, [&](int s) { return coef[g.Gs + s]; }, c2);
 #pragma unroll
       for (int j = 0; j < 4; ++j) { k1[j] = pair(c1[2 * j], c1[2 * j + 1]); k2[j] = pair(c2[2 * j], c2[2 * j + 1]); }
     }
@@ -1365,12 +1372,12 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_teams_kerne
   put_sums(red, g, at, A);
   put_sums(red + kThreads * 8, g, at, B);
   __syncthreads();
-  float* const out = p.partial + (size_t)blockIdx.x * 2 * g.C;
+  float* const out = p.partial + (size_t)blockIdx.x * 2 * g.C + blockIdx.y * g.slice;
   const int lanes = g.lanes_c, sub = threadIdx.x & (lanes - 1), rows = teams * g.rp;
-  for (int c0 = 0; c0 < g.C; c0 += kThreads / lanes) {
+  for (int c0 = 0; c0 < g.slice; c0 += kThreads / lanes) {
     const int c = c0 + threadIdx.x / lanes;
     float a = 0.f, b = 0.f;
-    if (c < g.C)
+    if (c < g.slice)
       for (int i = sub; i < rows; i += lanes) {
         const int team = i / g.rp;
         const float* v = all + (team * t.size + (i - team * g.rp) * g.cols) * 8 + c;
@@ -1378,7 +1385,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_teams_kerne
       }
     a = lane_sum(a, lanes);
     b = lane_sum(b, lanes);
-    if (c < g.C && sub == 0) { out[c] = a; out[g.C + c] = b; }
+    if (c < g.slice && sub == 0) { out[c] = a; out[g.C + c] = b; }
   }
 }
 // dgamma and dbeta, 32 of them, from `rows` rows of sums.
@@ -1511,9 +1518,13 @@ inline Plan plan_streamed(int N, int P, int C, int G, int per_sm) {
   pl.rows = (int64_t)N * g.parts;
   return pl;
 }
-// The team form: the size of a team that gives the least of (rounds of images per team) * (pixels per thread + 4, the fixed part of
-// a round, in pixels), the larger team where two are alike; none where an image does not fit.  vec_bytes: of a thread's pixel in shared
-// memory; shared, per_group: bytes of a CTA, of a team's group beside them.
+// The team form: the slices of an image (whole groups and blocks of 32 channels) and the size of a team that give the least of
+// (rounds of images per team) * (pixels per thread + 4, the fixed part of a round, in pixels), the fewest slices and the largest team
+// where some are alike; none where an image does not fit.  vec_bytes: of a thread's pixel in shared memory; shared, per_group: bytes of
+// a CTA, of a team's group beside them.
+// Slices are for rows wider than a CTA (us, streamed / sliced: 4096x1x4096 263 / 48, 512x4x4x4096 63 / 28) and, forward, for images that
+// all run at once then (16x16x16x256 6.8 / 3.4, 64x7x7x512 7.1 / 4.5, 128x8x8x640 8.7 / 7.2; in rounds 512x8x8x640 30 / 28 and with codes
+// 38 / 44; backward 512x16x16x64 16.5 / 20.3).
 // Forward (`most` = 12): teams smaller than a CTA only where they leave no SM without one (37x28x28x30 on 19 SMs: 12 us for 8.4); with
 // a CTA per image at most 12 pixels a thread, beyond which a cluster or the streamed form is as fast without codes and faster with
 // them (128x16x16x160, 22 pixels: 7.5 / 8.2 and 13 / 10.5).
@@ -1521,44 +1532,51 @@ inline Plan plan_streamed(int N, int P, int C, int G, int per_sm) {
 // fits an SM too (1024x8x8x160 from codes and bits 31.8 / 35, fp32 41.8 / 59); with a CTA per image, 8 pixels a thread 14.9 / 20.0 (400x32x32x16).
 inline Plan plan_teams(int vec_bytes, bool fill, int per_sm, size_t shared, int per_group, int most, int N, int P, int C, int G) {
   Plan best{};
-  const int cols = C / 8 + (C % 8 != 0);
   int64_t least = INT64_MAX;
-  for (int team = kThreads; team >= 32 && team >= cols; team /= 2) {
-    const int rp = team / cols, iters = P / rp + (P % rp != 0), teams = kThreads / team;
-    const int64_t all = N / teams + (N % teams != 0);
-    if ((fill || team < kThreads) && all < kSms) continue;
-    if (team == kThreads && iters > most) continue;
-    if (iters > 48) break;          // no room
-    Plan pl{};
-    pl.resident = true;
-    Geom& g = pl.g;
-    g.N = N; g.P = P; g.C = C; g.G = G; g.Cg = C / G;
-    g.cols = cols; g.rp = rp; g.team = team; g.tiles = 1;
-    g.inv_m = (float)(1.0 / ((double)P * g.Cg));
-    g.col_mul = (65536 + cols - 1) / cols;
-    g.cg_mul = g.Cg == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + g.Cg - 1) / g.Cg);
-    g.lanes_g = pow2_up_to(team / std::min(G, team), 32);
-    g.lanes_c = pow2_up_to(kThreads / std::min(C, kThreads), 32);
-    while (1 << g.lanes_log < g.lanes_g) ++g.lanes_log;
-    g.entries = g.Cg % 8 ? g.Cg : g.Cg / 8;
-    g.per_row = g.Cg % 8 ? cols * 8 : cols;
-    g.rows_on = g.lanes_g / g.entries;
-    g.cols_on = g.lanes_g % g.entries;
-    split(g, 1);
-    const size_t own = shared + (size_t)per_group * teams * G;
-    int64_t at_once = 0;
-    for (g.buffers = 1; at_once < all && g.buffers <= 2; ++g.buffers) {      // a second one where a team has a second image
-      pl.smem = (size_t)vec_bytes * iters * kThreads * g.buffers + own;
-      at_once = (int64_t)kSms * std::min<size_t>(per_sm, kSmemOfSm / (pl.smem + 1024));
+  for (int slices = 1; slices == 1 || (G % slices == 0 && C % (32 * slices) == 0); slices *= 2) {
+    const int slice = C / slices, cols = slice / 8 + (slice % 8 != 0), Gs = G / slices;
+    for (int team = kThreads; team >= 32 && team >= cols; team /= 2) {
+      const int rp = team / cols, iters = P / rp + (P % rp != 0), teams = kThreads / team;
+      const int64_t all = N / teams + (N % teams != 0);
+      if ((fill || team < kThreads) && all * slices < kSms) continue;
+      if (team == kThreads && iters > most) continue;
+      if (iters > 48) break;        // no room
+      const size_t own = shared + (size_t)per_group * teams * Gs, image = (size_t)vec_bytes * iters * kThreads;
+      int64_t at_once = 0;          // CTAs of a slice
+      int buffers = 0;
+      for (; at_once < all && buffers < 2; ++buffers) {           // a second one where a team has a second image
+        const size_t ctas = std::min<size_t>(per_sm, kSmemOfSm / (image * (buffers + 1) + own + 1024));
+        at_once = ctas < (fill ? per_sm : 1) ? 0 : std::max<int64_t>(1, (int64_t)kSms * ctas / slices);
+      }
+      const size_t smem = image * buffers + own;
+      if (smem > kSmemMost || at_once == 0) continue;
+      if (slices > 1 && C <= 8 * kMaxCols && (fill || at_once < all)) continue;
+      const int64_t cost = (all + at_once - 1) / at_once * (iters + 4);
+      if (cost >= least) continue;
+      least = cost;
+      best = Plan{};
+      best.resident = true;
+      best.smem = smem;
+      best.ctas = (int)std::min(all, at_once);
+      Geom& g = best.g;
+      g.N = N; g.P = P; g.C = C; g.G = G; g.Cg = C / G;
+      g.cols = cols; g.rp = rp; g.team = team; g.tiles = 1; g.buffers = buffers;
+      g.slices = slices; g.slice = slice; g.Gs = Gs;
     }
-    --g.buffers;
-    if (pl.smem > kSmemMost || (fill && at_once < (int64_t)kSms * per_sm)) continue;
-    const int64_t cost = (all + at_once - 1) / at_once * (iters + 4);
-    if (cost >= least) continue;
-    pl.ctas = (int)std::min(all, at_once);
-    least = cost;
-    best = pl;
   }
+  Geom& g = best.g;
+  if (g.team == 0) return best;
+  g.inv_m = (float)(1.0 / ((double)P * g.Cg));
+  g.col_mul = (65536 + g.cols - 1) / g.cols;
+  g.cg_mul = g.Cg == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + g.Cg - 1) / g.Cg);
+  g.lanes_g = pow2_up_to(g.team / std::min(g.Gs, g.team), 32);
+  g.lanes_c = pow2_up_to(kThreads / std::min(g.slice, kThreads), 32);
+  while (1 << g.lanes_log < g.lanes_g) ++g.lanes_log;
+  g.entries = g.Cg % 8 ? g.Cg : g.Cg / 8;
+  g.per_row = g.Cg % 8 ? g.cols * 8 : g.cols;
+  g.rows_on = g.lanes_g / g.entries;
+  g.cols_on = g.lanes_g % g.entries;
+  split(g, 1);
   return best;
 }
 // The team form for small images, else a cluster where an image fits one and all of a call's CTAs run at once (two on an SM, if their shared memory allows), with
@@ -1594,8 +1612,10 @@ inline Plan plan_backward(int elem_bytes, int N, int P, int C, int G) {
   return plan_streamed(N, P, C, G, kBackwardPerSm);
 }
 inline size_t partial_floats(const Plan& pl) { return (size_t)pl.rows * 2 * pl.g.C; }
-// Whether a second streamed pass adds up an image's rows of sums itself.
+// Whether a second streamed pass adds up an image's rows of sums itself.  (Backward also with tiles: a launch that forms the totals of
+// many images of one row each took 5 of 5.8 ms for 4096 of 4096 channels.)
 inline bool merges(const Geom& g) { return g.tiles == 1 && g.parts <= kMergeParts; }
+inline bool merges_backward(const Geom& g) { return g.parts <= kMergeParts; }
 // Whether every launch's grid can be given (with many images a plan has one share of each).
 inline bool grid_ok(const Plan& pl) {
   const Geom& g = pl.g;
@@ -1621,7 +1641,7 @@ template <typename T, int W, int ACT, int EXTRA> inline cudaError_t launch_forwa
   if (g.team) {
     static OncePerDevice once;
     const cudaError_t e = once_per_device(&once, []() { return set_smem_limit(forward_teams_kernel<T, W, ACT, EXTRA>, kSmemMost); });
-    return e != cudaSuccess ? e : launch_chained(forward_teams_kernel<T, W, ACT, EXTRA>, dim3((unsigned)pl.ctas), dim3(kThreads), pl.smem, st, p);
+    return e != cudaSuccess ? e : launch_chained(forward_teams_kernel<T, W, ACT, EXTRA>, dim3((unsigned)pl.ctas, (unsigned)g.slices), dim3(kThreads), pl.smem, st, p);
   }
   if (pl.resident) {
     static OncePerDevice once;
@@ -1675,7 +1695,7 @@ inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<
   if (g.team) {
     static OncePerDevice once;
     cudaError_t e = once_per_device(&once, []() { return set_smem_limit(backward_teams_kernel<T, W, CK, SLOPE>, kSmemMost); });
-    if (e == cudaSuccess) e = launch_chained(backward_teams_kernel<T, W, CK, SLOPE>, dim3((unsigned)pl.ctas), dim3(kThreads), pl.smem, st, p);
+    if (e == cudaSuccess) e = launch_chained(backward_teams_kernel<T, W, CK, SLOPE>, dim3((unsigned)pl.ctas, (unsigned)g.slices), dim3(kThreads), pl.smem, st, p);
     if (e == cudaSuccess)
       e = launch_chained(parameters_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, (const float*)p.partial, (int)pl.rows, g.C, p.dgamma, p.dbeta);
     return e;
@@ -1689,7 +1709,7 @@ inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<
   auto rings = [&](bool res) { return 16 * (size_t)Feed<T, W, CK>::words(p.slope == SLOPE_MASK, res); };
   e = launch_chained(backward_sums_kernel<T, W, CK, SLOPE>, dim3((unsigned)g.N, (unsigned)g.parts, (unsigned)g.tiles), dim3(kThreads),
                      std::max(rings(false), (size_t)2 * kThreads * 8 * 4), st, p);
-  if (merges(g)) p.totals = nullptr;
+  if (merges_backward(g)) p.totals = nullptr;
   else if (e == cudaSuccess)
     e = launch_chained(totals_kernel, dim3((unsigned)(g.N * blocks)), dim3(1024), 0, st, (const float*)p.partial, g.parts, width, p.totals);
   // coefficients of the tile's groups; with one tile also the channels' sums

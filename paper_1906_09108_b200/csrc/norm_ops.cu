@@ -21,7 +21,7 @@ static size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Scratch: the forward pass's rows of sums; the backward pass's per-image totals [N][2][C], where it forms them, and its rows of sums.
 static size_t forward_need(const gn::Plan& pl) { return align256(gn::partial_floats(pl) * sizeof(float)); }
-static size_t totals_bytes(const gn::Plan& pl) { return gn::merges(pl.g) ? 0 : align256((size_t)pl.g.N * 2 * pl.g.C * sizeof(float)); }
+static size_t totals_bytes(const gn::Plan& pl) { return gn::merges_backward(pl.g) ? 0 : align256((size_t)pl.g.N * 2 * pl.g.C * sizeof(float)); }
 static size_t backward_need(const gn::Plan& pl) { return totals_bytes(pl) + align256(gn::partial_floats(pl) * sizeof(float)); }
 
 template <typename T>

@@ -512,6 +512,8 @@ SMALL = [
     (4096, 4, 64, 4), (2000, 9, 128, 32), (2000, 1, 512, 32), (900, 3, 30, 6), (1300, 7, 33, 11), (601, 21, 160, 32), (3001, 2, 8, 1),
     (500, 200, 3, 1), (700, 5, 264, 3), (450, 2, 2048, 16), (450, 3, 1000, 1), (500, 1, 2048, 2048), (2999, 1, 1, 1), (150, 90, 40, 40),
     (450, 5, 640, 8), (20011, 1, 48, 2), (300, 100, 64, 8), (1100, 25, 96, 4), (800, 6, 20, 5),
+    # rows in slices, and where groups allow none
+    (300, 1, 4096, 32), (40, 3, 5120, 16), (16, 130, 256, 8), (33, 49, 512, 32), (200, 2, 4096, 1), (20, 2, 6144, 64), (700, 1, 2176, 2),
 ]
 
 
