@@ -554,3 +554,39 @@ def test_small_images_far_from_zero_and_not_finite(prec_name):
     assert np.isfinite(_np(y)[clean]).all() and np.isfinite(back[clean]).all()
     yl = np.isnan(_np(y).reshape(n, p, groups, -1)).all((1, 3))
     assert yl[600, 3] and yl[5, 0] and yl.sum() == 2
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("shape", [(2000, 4, 64, 4), (700, 1, 4096, 32)], ids=str)
+def test_small_images_captured_and_beside_one_another(prec_name, shape):
+    """The same bits from a graph that is replayed on new values, and from calls on two streams at once."""
+    _, ew = _ops(prec_name)
+    n, p, c, groups = shape
+    gamma, beta = (_f32(t) for t in _params(c, 5))
+    sets = [(_mk((n, p, c), 6 + i, ew.dtype)[0], _mk((n, p, c), 16 + i, ew.dtype, 0.01)[0]) for i in range(3)]
+
+    def step(x, dy):
+        y, stats, bits, held = ew.gn_forward(x, groups, gamma, beta, act="relu", gate=True, checkpoint=True)
+        return (y, stats, bits, *held, *ew.gn_backward(dy, held, stats, groups, gamma, act="relu", gate=bits))
+
+    want = [step(*s) for s in sets]
+    torch.cuda.synchronize()
+    x, dy = sets[0][0].clone(), sets[0][1].clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(x, dy)
+    for (a, b), w in zip(sets, want):
+        x.copy_(a)
+        dy.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, u) for t, u in zip(got, w))
+    streams = [torch.cuda.Stream() for _ in sets]
+    beside = []
+    for _ in range(4):
+        for st, s in zip(streams, sets):
+            with torch.cuda.stream(st):
+                beside.append(step(*s))
+    torch.cuda.synchronize()
+    for i, b in enumerate(beside):
+        assert all(torch.equal(t, u) for t, u in zip(b, want[i % 3]))
