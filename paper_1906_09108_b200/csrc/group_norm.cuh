@@ -24,10 +24,10 @@
 // (A backward pass by clusters was no faster anywhere: its parameter gradients need a second launch all the same.)
 // In teams (plan_teams): small images, several to a CTA, one after the other.
 //
-// Variance: a thread sums its values and their squares less its first value, brings them about a common value of the CTA (the
-// mean of the channel's first row of threads), then about the CTA's group mean, and CTAs are combined by Chan's formula.  The
+// Variance: a thread sums its values and their squares less a pivot that follows their mean (Moments), brings them about a common
+// value of the CTA (the mean of the channel's first row of threads), then about the CTA's group mean, and CTAs are combined by Chan's formula.  The
 // square of the distance from a mean over a share f of the values to the mean over all is at most var*(1 - f)/f, so what cancels
-// in each step is bounded by the data itself (by the number of a thread's values, then by rp), whatever offset x has.  The team form
+// in each step is bounded by the data itself (a few times in a thread, then by rp), whatever offset x has.  The team form
 // has the image at hand and takes the mean first.
 // All sums are fp32 within a CTA (a chain of a thread's values, then of rows of threads, then a tree), in a fixed order.
 #pragma once
@@ -160,11 +160,19 @@ template <int B> struct Stream {
       if (k % B == B - 1) asm volatile("cp.async.commit_group;" ::: "memory");
     }
   }
-  template <typename Issue, typename Turn> static __device__ __forceinline__ void run(int n, int mine, Issue issue, Turn turn) {
+  // `after`(k), once k vectors have been used, k a multiple of R: after whole rounds of the ring, which ask nothing of a single vector.
+  // Fewer than R + B * kAhead vectors follow the last of them.
+  template <typename Issue, typename Turn, typename After>
+  static __device__ __forceinline__ void run(int n, int mine, Issue issue, Turn turn, After after) {
     int k0 = 0;
-    // whole rounds of the ring ask nothing of a single vector
-    for (; k0 + R + B * kAhead <= mine; k0 += R) round<true>(k0, n, mine, issue, turn);
+    for (; k0 + R + B * kAhead <= mine; k0 += R) {
+      round<true>(k0, n, mine, issue, turn);
+      after(k0 + R);
+    }
     for (; k0 < n; k0 += R) round<false>(k0, n, mine, issue, turn);
+  }
+  template <typename Issue, typename Turn> static __device__ __forceinline__ void run(int n, int mine, Issue issue, Turn turn) {
+    run(n, mine, issue, turn, [](int) {});
   }
   // The same in a loop of single turns, for turns whose code unrolled over the ring does not fit the instruction caches.
   template <typename Issue, typename Turn> static __device__ __forceinline__ void run_rolled(int n, int mine, Issue issue, Turn turn) {
@@ -311,23 +319,41 @@ template <typename T> struct Forward {
   bool combined;              // streamed: `stats` holds the statistics when the second pass starts
 };
 
-// A thread's moments of its 8 channels: sums of its values and of their squares less the first of them.
+// A thread's moments of its 8 channels: sums of its values and of their squares less a pivot, at first the first of them.
+// close(n), n values so far, moves the pivot to their mean and puts their squared deviations from it with those of earlier values, at
+// every doubling and then every kChain values (closes()).  With M = sum (x - mean)^2 over all n values of the thread, the mean of the
+// first k differs from that of all by at most sqrt(M/k): the squares of the next min(k, kChain) values about it add up to no
+// more than a few M whatever the first value is, and no chain of additions is longer than kChain, or than the number of chains.
+// (From the first value alone: n M, which at 2048 values of spread 1 around 100, the first one 0, cost rstd its second digit.)
+constexpr int kChain = 64;
 struct Moments {
-  F8 first, sum, square;
+  F8 pivot, sum, square, closed;                 // the pivot with its sign turned
   __device__ __forceinline__ Moments() {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) first.p[j] = sum.p[j] = square.p[j] = 0;
+    for (int j = 0; j < 4; ++j) pivot.p[j] = sum.p[j] = square.p[j] = closed.p[j] = 0;
   }
   __device__ __forceinline__ void start(const F8& x) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) first.p[j] = mul2(x.p[j], pair(-1.f));
+    for (int j = 0; j < 4; ++j) pivot.p[j] = mul2(x.p[j], pair(-1.f));
   }
   __device__ __forceinline__ void add(const F8& x) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const f32x2 d = add2(x.p[j], first.p[j]);
+      const f32x2 d = add2(x.p[j], pivot.p[j]);
       sum.p[j] = add2(sum.p[j], d);
       square.p[j] = fma2(d, d, square.p[j]);
+    }
+  }
+  static __device__ __forceinline__ int after(int n) { return n + min(n, kChain); }      // when to close next
+  // The pivot moves by t as rounded, and what the sum is not exactly 0 by then stays in it: roundings of the pivot do not add up.
+  __device__ __forceinline__ void close(int n) {
+    const f32x2 over = pair(-1.f / (float)n), less_n = pair(-(float)n);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x2 to = fma2(sum.p[j], over, pivot.p[j]);
+      const f32x2 t = fma2(to, pair(-1.f), pivot.p[j]), rest = fma2(t, less_n, sum.p[j]);
+      closed.p[j] = add2(closed.p[j], fma2(mul2(t, pair(-1.f)), add2(sum.p[j], rest), square.p[j]));
+      sum.p[j] = rest; square.p[j] = 0; pivot.p[j] = to;
     }
   }
 };
@@ -340,11 +366,11 @@ __device__ __forceinline__ void cta_moments(const Geom& g, const Place& at, cons
   float mu[8], dev[8];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float2 f = halves(m.first.p[j]), s1 = halves(m.sum.p[j]), s2 = halves(m.square.p[j]);
+    const float2 f = halves(m.pivot.p[j]), s1 = halves(m.sum.p[j]), s2 = halves(m.square.p[j]), s3 = halves(m.closed.p[j]);
     mu[2 * j] = fmaf(s1.x, over, -f.x);
     mu[2 * j + 1] = fmaf(s1.y, over, -f.y);
-    dev[2 * j] = fmaf(-s1.x * over, s1.x, s2.x);
-    dev[2 * j + 1] = fmaf(-s1.y * over, s1.y, s2.y);
+    dev[2 * j] = fmaf(-s1.x * over, s1.x, s2.x) + s3.x;
+    dev[2 * j + 1] = fmaf(-s1.y * over, s1.y, s2.y) + s3.y;
   }
   if (at.r == 0) put_sums(common, g, at, mu);
   __syncthreads();
@@ -587,8 +613,12 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_kernel(const 
   copies_done();
   Moments m;
   if (sh.mine > 0) m.start(raw8_to_f8(slots.get(0)));
+  for (int k = 0, stop = 8; k < sh.mine; stop = Moments::after(stop)) {
+    const int to = min(stop, sh.mine);
 #pragma unroll 4
-  for (int k = 0; k < sh.mine; ++k) m.add(raw8_to_f8(slots.get(k)));
+    for (; k < to; ++k) m.add(raw8_to_f8(slots.get(k)));
+    if (k < sh.mine) m.close(k);
+  }
   cta_moments(g, at, m, sh.mine, sh.count, g.C, red, common, chan);
   group_moments(g, sh.count, chan, [&](int s, float mu, float q) { own[s] = mu; own[g.G + s] = q; });
   cg::cluster_group cluster = cg::this_cluster();
@@ -798,10 +828,13 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) moments_kernel(const 
   };
   Stream<kBatch>::start(sh.mine, issue);
   m.start(raw8_to_f8(first));
+  int close_at = kRing;
   Stream<kBatch>::run(sh.mine, sh.mine, issue, [&](int k, int slot, auto full) {
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (full.value || k + u < sh.mine) m.add(raw8_to_f8(ring.get(slot + u)));
+  }, [&](int n) {
+    if (n == close_at) { m.close(n); close_at = Moments::after(n); }
   });
   const int c_first = blockIdx.z * kMaxCols * 8, sets = min(g.cols * 8, g.C - c_first);
   cta_moments(g, at, m, sh.mine, sh.count, sets, red, common, chan);

@@ -590,3 +590,52 @@ def test_small_images_captured_and_beside_one_another(prec_name, shape):
     torch.cuda.synchronize()
     for i, b in enumerate(beside):
         assert all(torch.equal(t, u) for t, u in zip(b, want[i % 3]))
+
+
+# ---- long threads, blank groups, far tails, options together ------------------------------------------------------------
+
+def _stats64(x, groups):
+    """mean, rstd [N, groups] of a tensor on the GPU, in float64, image by image."""
+    n, p, c = x.shape
+    out = torch.empty((2, n, groups), dtype=torch.float64, device="cuda")
+    for i in range(n):
+        v = x[i].double().view(p, groups, c // groups)
+        mean = v.mean((0, 2))
+        out[0, i] = mean
+        out[1, i] = 1 / ((v - mean[:, None]).square_().mean((0, 2)) + EPS).sqrt()
+    return out
+
+
+def _check_stats64(x, groups, stats):
+    n, p, c = x.shape
+    want = _stats64(x, groups)
+    mag = torch.stack([x[i].abs().view(p, groups, -1).mean((0, 2), dtype=torch.float64) for i in range(n)])
+    off = (stats.double() - want).abs()
+    assert (off[0] <= K * mag).all(), ("mean", float((off[0] / mag).max()))
+    assert (off[1] <= want[1] * (K + (K * mag * want[1]) ** 2)).all(), ("rstd", float((off[1] / want[1]).max()))
+    return want
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("offset", [10.0, 1000.0])
+@pytest.mark.parametrize("shape", [(224, 512, 1032, 8), (256, 4096, 1024, 32), (160, 4096, 264, 1), (1, 444 * 256 * 512, 1, 1)], ids=str)
+def test_variance_where_a_thread_has_many_values(prec_name, offset, shape):
+    """Hundreds of values a thread, the first of them 0 as at the border of a padded map, the rest far from 0.  What a thread's
+    sums cancel must not grow with their number: the tolerance is that of the small cases."""
+    _, ew = _ops(prec_name)
+    n, p, c, groups = shape
+    x = torch.empty((n, p, c), dtype=ew.dtype, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(11)
+    for i in range(n):
+        x[i] = torch.randn((p, c), generator=g, device="cuda") + offset
+    rows = 256 // -(-c // 8)                         # of threads: the first pixels of an image, or of a CTA's share of it
+    x.view(-1, 512 * 256 if c == 1 else p, c)[:, :rows] = 0
+    gamma, beta = (_f32(a) for a in _params(c, 161))
+    y, stats, _, _ = ew.gn_forward(x, groups, gamma, beta, eps=EPS)
+    want = _check_stats64(x, groups, stats)
+    wide = lambda t: t.repeat_interleave(c // groups)  # noqa: E731
+    for i in {0, n - 1}:
+        m, r, v = wide(want[0, i]), wide(want[1, i]), x[i].double()
+        z = (v - m) * r * gamma + beta
+        size = (v.abs() + m.abs()) * r * gamma.abs() + beta.abs()
+        assert ((y[i].double() - z).abs() <= _half_step(ew.dtype) * z.abs() + 1.1 * K * size).all()
