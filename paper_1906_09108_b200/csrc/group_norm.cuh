@@ -25,10 +25,9 @@
 // In teams (plan_teams): small images, several to a CTA, one after the other.
 //
 // Variance: a thread sums its values and their squares less a pivot that follows their mean (Moments), brings them about a common
-// value of the CTA (the mean of the channel's first row of threads), then about the CTA's group mean, and CTAs are combined by Chan's formula.  The
-// square of the distance from a mean over a share f of the values to the mean over all is at most var*(1 - f)/f, so what cancels
-// in each step is bounded by the data itself (a few times in a thread, then by rp), whatever offset x has.  The team form
-// has the image at hand and takes the mean first.
+// value of the CTA (a mean over at least a 64th of the channel's values), then about the CTA's group mean, and CTAs are combined by Chan's
+// formula.  The square of the distance from a mean over a share f of the values to the mean over all is at most var*(1 - f)/f, so what
+// cancels in each step is bounded by the data itself, whatever offset x has.  The team form has the image at hand and takes the mean first.
 // All sums are fp32 within a CTA (a chain of a thread's values, then of rows of threads, then a tree), in a fixed order.
 #pragma once
 #include <cooperative_groups.h>
@@ -360,6 +359,10 @@ struct Moments {
 
 // The CTA's moments from its threads' (each over n values): chan[c] = mean and squared deviations from it of the tile's first
 // `sets` channels.  `red`: 4096 floats, `common`: 2048 floats.  Ends with a barrier.
+// A channel's rows of threads are summed about a common value.  That value's distance from the mean, where it is a mean over a share f
+// of the values, is at most sqrt(var (1 - f)/f), so the sums lose a factor of up to 1/f: a row of the rp.  Beyond 64 rows (three columns
+// or fewer) eight of them, far apart, give it: with the first of 256 alone, a map whose first column is blank cost rstd 4e-5 of itself.
+constexpr int kRowsAbout = 8;
 __device__ __forceinline__ void cta_moments(const Geom& g, const Place& at, const Moments& m, int n, int count, int sets, float* red, float* common,
                                             float2* chan) {
   const float fn = (float)n, over = n > 0 ? 1.f / fn : 0.f;
@@ -373,6 +376,16 @@ __device__ __forceinline__ void cta_moments(const Geom& g, const Place& at, cons
     dev[2 * j + 1] = fmaf(-s1.y * over, s1.y, s2.y) + s3.y;
   }
   if (at.r == 0) put_sums(common, g, at, mu);
+  const int filled = min(g.rp, count);                   // rows of threads with values
+  if (filled > 64) {
+    const int apart = filled / kRowsAbout, row = at.r / apart, w = g.cols * 8;
+    if (at.r == row * apart && row < kRowsAbout) put_sums(red + (row - at.r) * w, g, at, mu);          // rows 0 to 7 of red
+    __syncthreads();
+    if (threadIdx.x < w) {
+      const float* v = red + threadIdx.x;                  // in pairs, so that equal ones give themselves exactly
+      common[threadIdx.x] = 0.125f * (((v[0] + v[w]) + (v[2 * w] + v[3 * w])) + ((v[4 * w] + v[5 * w]) + (v[6 * w] + v[7 * w])));
+    }
+  }
   __syncthreads();
   const float4* k = reinterpret_cast<const float4*>(common + at.col * 8);
   const float4 k0 = k[0], k1 = k[1];

@@ -639,3 +639,18 @@ def test_variance_where_a_thread_has_many_values(prec_name, offset, shape):
         z = (v - m) * r * gamma + beta
         size = (v.abs() + m.abs()) * r * gamma.abs() + beta.abs()
         assert ((y[i].double() - z).abs() <= _half_step(ew.dtype) * z.abs() + 1.1 * K * size).all()
+
+
+@pytest.mark.parametrize("offset", [1367.9, 535.4, 1501.1])
+def test_variance_where_a_row_of_threads_differs(offset):
+    """Maps of 256 pixels a row whose first column is blank: one of a CTA's 256 rows of threads has nothing but that column."""
+    _, ew = _ops("fp32")
+    for n, c, groups in ((1, 8, 1), (2, 16, 2)):
+        x = torch.full((n, 65536, c), offset, device="cuda")
+        x.view(n, 256, 256, c)[:, :, 0] = 0
+        one, zero = torch.ones(c, device="cuda"), torch.zeros(c, device="cuda")
+        _check_stats64(x, groups, ew.gn_forward(x, groups, one, zero, eps=EPS)[1])
+    # a last share of 50 pixels for 85 rows of threads
+    x = torch.full((1, 150772, 24), offset, device="cuda")
+    x[:, ::85] = 0
+    _check_stats64(x, 3, ew.gn_forward(x, 3, torch.ones(24, device="cuda"), torch.zeros(24, device="cuda"), eps=EPS)[1])
