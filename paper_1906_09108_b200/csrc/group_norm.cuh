@@ -414,9 +414,10 @@ __device__ __forceinline__ void group_moments(const Geom& g, int count, const fl
   for (int s0 = 0; s0 < g.G; s0 += per_pass) {
     const int s = s0 + threadIdx.x / lanes;
     float a = 0.f, q = 0.f;
+    const float first = chan[min(s, g.G - 1) * g.Cg].x;          // differences from it: equal means give themselves exactly
     if (s < g.G)
-      for (int j = sub; j < g.Cg; j += lanes) a += chan[s * g.Cg + j].x;
-    const float mu = lane_sum(a, lanes) * inv;
+      for (int j = sub; j < g.Cg; j += lanes) a += chan[s * g.Cg + j].x - first;
+    const float mu = fmaf(lane_sum(a, lanes), inv, first);
     if (s < g.G)
       for (int j = sub; j < g.Cg; j += lanes) {
         const float2 c = chan[s * g.Cg + j];
@@ -437,9 +438,10 @@ __device__ __forceinline__ void image_moments(const Geom& g, int rows, float eps
   for (int s0 = 0; s0 < g.G; s0 += per_pass) {
     const int s = s0 + threadIdx.x / lanes;
     float a = 0.f, q = 0.f;
+    const float first = row(0)[min(s, g.G - 1)];
     if (s < g.G)
-      for (int j = sub; j < rows; j += lanes) a = fmaf(row(j)[s], pixels(j) * inv_p, a);
-    const float mu = lane_sum(a, lanes);
+      for (int j = sub; j < rows; j += lanes) a = fmaf(row(j)[s] - first, pixels(j) * inv_p, a);
+    const float mu = lane_sum(a, lanes) + first;
     if (s < g.G)
       for (int j = sub; j < rows; j += lanes) {
         const float d = row(j)[s] - mu;
@@ -450,23 +452,18 @@ __device__ __forceinline__ void image_moments(const Geom& g, int rows, float eps
   }
 }
 
-// What a thread multiplies its 8 channels by: scale = gamma*rstd and shift = beta, and the mean with its sign turned.  16-bit
-// tensors take the mean into the shift: that rounds |mean|*scale to 24 bits where x itself has 8.
-template <typename T> struct Affine {
-  static constexpr bool kFolded = sizeof(T) == 2;
-  f32x2 scale[4], shift[4], less[kFolded ? 1 : 4];
+// What a thread multiplies its 8 channels by: scale = gamma*rstd and shift = beta, and the mean with its sign turned.  The mean is
+// subtracted before anything is rounded: in a group without spread, where rstd is 1/sqrt(eps), x - mean is 0 and y is act(beta) exactly.
+// (Taken into the shift, it is rounded at the size of |mean|*scale: blank groups of 100 came out up to 2e-3 beside beta, ReLU's
+// gate of a whole group with them.)
+struct Affine {
+  f32x2 scale[4], shift[4], less[4];
   __device__ __forceinline__ void set(int j, float2 mean, float2 sc, float2 sh) {
     scale[j] = pair(sc.x, sc.y);
-    if constexpr (kFolded) {
-      shift[j] = pair(fmaf(-mean.x, sc.x, sh.x), fmaf(-mean.y, sc.y, sh.y));
-    } else {
-      shift[j] = pair(sh.x, sh.y);
-      less[j] = pair(-mean.x, -mean.y);
-    }
+    shift[j] = pair(sh.x, sh.y);
+    less[j] = pair(-mean.x, -mean.y);
   }
-  __device__ __forceinline__ f32x2 of(int j, f32x2 x) const {
-    if constexpr (kFolded) return fma2(x, scale[j], shift[j]); else return fma2(add2(x, less[j]), scale[j], shift[j]);
-  }
+  __device__ __forceinline__ f32x2 of(int j, f32x2 x) const { return fma2(add2(x, less[j]), scale[j], shift[j]); }
 };
 
 // Bits of [y > 0] of 8 stored values.
@@ -526,7 +523,7 @@ template <typename T, int W, int ACT, int EXTRA> struct Emitter {
     }
   }
   // Pixel k of the thread, at element offset o.
-  __device__ __forceinline__ void value(uint32_t k, uint32_t o, const Affine<T>& affine, const F8& x, const Raw8<T>& raw_res) const {
+  __device__ __forceinline__ void value(uint32_t k, uint32_t o, const Affine& affine, const F8& x, const Raw8<T>& raw_res) const {
     F8 z;
 #pragma unroll
     for (int j = 0; j < 4; ++j) z.p[j] = affine.of(j, x.p[j]);
@@ -552,7 +549,7 @@ template <typename T, int W, int ACT, int EXTRA> struct Emitter {
   // A turn of B pixels, raw, k counting from the thread's first pixel or (back) its last; for the whole warp where codes are
   // formed, since the lanes that share a block of 32 channels (they have the same pixels) exchange its maximum.
   template <bool FULL, int B>
-  __device__ __forceinline__ void turn(int k, int mine, bool back, const Affine<T>& affine, const Raw8<T> (&raw)[B], const Raw8<T>* raw_res) const {
+  __device__ __forceinline__ void turn(int k, int mine, bool back, const Affine& affine, const Raw8<T> (&raw)[B], const Raw8<T>* raw_res) const {
     uint32_t top[B];
     if constexpr (EXTRA == WITH_CODES)
       if (W == kWhole || codes) block_tops<B>(raw, top);
@@ -587,7 +584,7 @@ template <typename T, int W, int ACT, int EXTRA> struct Emitter {
 };
 // The constants of a thread's channels from their groups' statistics.
 template <typename T, typename Stat>
-__device__ __forceinline__ void load_affine(const Forward<T>& p, const Place& at, const float (&gamma)[8], const float (&beta)[8], Stat stat, Affine<T>& affine) {
+__device__ __forceinline__ void load_affine(const Forward<T>& p, const Place& at, const float (&gamma)[8], const float (&beta)[8], Stat stat, Affine& affine) {
   float2 m[8];
   each_channel(p.g, at, [&](int i, int, int s) { m[i] = stat(s); });
 #pragma unroll
@@ -599,7 +596,7 @@ __device__ __forceinline__ void load_affine(const Forward<T>& p, const Place& at
 // The resident form: blockIdx = image, share of its pixels, tile of columns: a cluster per image.
 template <typename T, int W, int ACT, int EXTRA>
 __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_kernel(const __grid_constant__ Forward<T> p) {
-  constexpr int kBatch = 2;
+  constexpr int kBatch = W == kWhole ? 2 : 1;           // pieces of a vector take registers of their own: 16x16384x36 35.4 us with 2, 33.1 with 1
   extern __shared__ uint4 smem[];
   const Geom& g = p.g;
   float* red = reinterpret_cast<float*>(smem + (size_t)g.iters * Slots<T>::Q * kThreads);      // [4096]
@@ -626,12 +623,13 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_kernel(const 
   copies_done();
   Moments m;
   if (sh.mine > 0) m.start(raw8_to_f8(slots.get(0)));
-  for (int k = 0, stop = 8; k < sh.mine; stop = Moments::after(stop)) {
-    const int to = min(stop, sh.mine);
+  int k = 0, close_at = 8;
+  for (; k + 8 <= sh.mine; k += 8) {
 #pragma unroll 4
-    for (; k < to; ++k) m.add(raw8_to_f8(slots.get(k)));
-    if (k < sh.mine) m.close(k);
+    for (int u = 0; u < 8; ++u) m.add(raw8_to_f8(slots.get(k + u)));
+    if (k + 8 == close_at) { m.close(k + 8); close_at = Moments::after(k + 8); }
   }
+  for (; k < sh.mine; ++k) m.add(raw8_to_f8(slots.get(k)));
   cta_moments(g, at, m, sh.mine, sh.count, g.C, red, common, chan);
   group_moments(g, sh.count, chan, [&](int s, float mu, float q) { own[s] = mu; own[g.G + s] = q; });
   cg::cluster_group cluster = cg::this_cluster();
@@ -645,15 +643,22 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_kernel(const 
   });
   cg::cluster_group::arrival_token token = cluster.barrier_arrive();      // this CTA reads its neighbours' sums no more
   __syncthreads();
-  Affine<T> affine;
+  Affine affine;
   load_affine(p, at, gamma, beta, [&](int s) { return mom[s]; }, affine);
+  Raw8<T> next_res{};
+  if constexpr (EXTRA >= WITH_RES_GATE && kBatch == 1)
+    if (out.res && sh.mine > 0) next_res = raw8_load<T, W>(out.res + out.first, at.left);
   for (int k = 0; k < (EXTRA == WITH_CODES ? sh.turns : sh.mine); k += kBatch) {
     Raw8<T> xs[kBatch], rs[EXTRA >= WITH_RES_GATE ? kBatch : 1];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       if (EXTRA == WITH_CODES || k + u < sh.mine) xs[u] = slots.get(min(k + u, g.iters - 1));
-      if constexpr (EXTRA >= WITH_RES_GATE)
+      if constexpr (EXTRA >= WITH_RES_GATE && kBatch > 1)
         if (out.res && k + u < sh.mine) rs[u] = raw8_load<T, W>(out.res + (out.first + (uint32_t)(k + u) * step), at.left);
+    }
+    if constexpr (EXTRA >= WITH_RES_GATE && kBatch == 1) {
+      rs[0] = next_res;
+      if (out.res && k + 1 < sh.mine) next_res = raw8_load<T, W>(out.res + (out.first + (uint32_t)(k + 1) * step), at.left);
     }
     out.template turn<false>(k, sh.mine, false, affine, xs, rs);
   }
@@ -678,10 +683,14 @@ struct Team {
     else asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + first / 32), "r"(size) : "memory");
   }
 };
-// red = what a thread adds to its groups' sums: a value where its column is in one group, else one per channel.
+// Where a thread's entries of a group's sums are: one where its column is in one group, else one per channel.
+__device__ __forceinline__ float* team_at(float* red, const Geom& g, const Place& at) {
+  return red + (at.r * g.per_row) + at.col * (g.entries == g.Cg ? 8 : 1);
+}
+// red = what a thread adds to its groups' sums.
 __device__ __forceinline__ void team_put(float* red, const Geom& g, const Place& at, const F8& v) {
   if (!at.active) return;
-  float* d = red + (at.r * g.per_row) + at.col * (g.entries == g.Cg ? 8 : 1);
+  float* d = team_at(red, g, at);
   if (g.entries == g.Cg) {
     reinterpret_cast<ulonglong2*>(d)[0] = make_ulonglong2(v.p[0], v.p[1]);
     reinterpret_cast<ulonglong2*>(d)[1] = make_ulonglong2(v.p[2], v.p[3]);
@@ -706,6 +715,27 @@ template <typename Done> __device__ __forceinline__ void team_group_sums(const G
     }
     a = lane_sum(a, g.lanes_g);
     if (s < g.Gs && t.sub == 0) done(s, a);
+  }
+}
+// The same of threads' means, weighted by the pixels of their rows: done(s, the mean over group s), as differences from the first of
+// them, so that a group without spread has exactly its value.  over: 1 / (entries * pixels).
+template <typename Done> __device__ __forceinline__ void team_group_means(const Geom& g, const Team& t, const float* red, float over, Done done) {
+  const int n = g.entries, more = g.P - g.whole * g.rp;
+  const float cnt = (float)g.whole;
+  for (int s0 = 0; s0 < g.Gs; s0 += t.size >> g.lanes_log) {
+    const int s = s0 + t.set;
+    float a = 0.f, first = 0.f;
+    if (s < g.Gs) {
+      const float* v = red + s * n;
+      first = v[0];
+      for (int r = t.r0, j = t.j0; r < g.rp;) {
+        a = fmaf(v[r * g.per_row + j] - first, r < more ? cnt + 1.f : cnt, a);
+        r += g.rows_on; j += g.cols_on;
+        if (j >= n) { j -= n; ++r; }
+      }
+    }
+    a = lane_sum(a, g.lanes_g);
+    if (s < g.Gs && t.sub == 0) done(s, fmaf(a, over, first));
   }
 }
 // A group's value for each channel of a thread's column.
@@ -734,6 +764,8 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_teams_kernel(
   const int teams = kThreads / t.size, stride = gridDim.x * teams;
   const uint32_t first = (uint32_t)at.r * g.C + whole.c0, step = (uint32_t)g.rp * g.C;
   const int mine = Share(g, at, 0, 0).mine;
+  const bool cut = g.entries == g.Cg;                                                           // columns lie in more than one group
+  const float over = mine > 0 ? 1.f / (float)(cut ? mine : 8 * mine) : 0.f, m = (float)(g.P * g.Cg);
   auto fetch = [&](int n, int buf) {
     const T* src = p.x + (size_t)n * g.P * g.C + first;
     for (int k = 0; k < mine; ++k) slots.template fetch<W>(buf * g.iters + k, src + (uint32_t)k * step, at.left);
@@ -754,23 +786,58 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_teams_kernel(
     asm volatile("cp.async.wait_group 1;" ::: "memory");
     const int at0 = buf * g.iters;
     F8 v;
+    if constexpr (sizeof(T) == 2) {
+      // Sums of values.  Those of equal 16-bit values are exact (a group has at most 48 * 1024 here, plan_teams), so with a quotient
+      // rounded once the mean of a group without spread is its value.
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v.p[j] = 0;
-    for (int k = 0; k < mine; ++k) {
-      const F8 x = raw8_to_f8(slots.get(at0 + k));
+      for (int j = 0; j < 4; ++j) v.p[j] = 0;
+      for (int k = 0; k < mine; ++k) {
+        const F8 x = raw8_to_f8(slots.get(at0 + k));
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v.p[j] = add2(v.p[j], x.p[j]);
+        for (int j = 0; j < 4; ++j) v.p[j] = add2(v.p[j], x.p[j]);
+      }
+      team_put(red, g, at, v);
+      t.sync();
+      team_group_sums(g, t, red, [&](int s, float a) { mom[s].x = __fdiv_rn(a, m); });
+    } else {
+      // Means of a thread's values, from sums of their differences from its first pixel; then of the group's, alike.
+      float* const d = team_at(red, g, at);
+      F8 x{}, first;
+      if (mine > 0) x = raw8_to_f8(slots.get(at0));
+      if (cut) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { first.p[j] = mul2(x.p[j], pair(-1.f)); v.p[j] = 0; }
+      } else {
+        const f32x2 f = pair(-halves(x.p[0]).x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { first.p[j] = f; v.p[j] = add2(x.p[j], f); }
+      }
+      for (int k = 1; k < mine; ++k) {
+        x = raw8_to_f8(slots.get(at0 + k));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v.p[j] = add2(v.p[j], add2(x.p[j], first.p[j]));
+      }
+      if (cut) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v.p[j] = fma2(v.p[j], pair(over), mul2(first.p[j], pair(-1.f)));
+        if (at.active) {
+          reinterpret_cast<ulonglong2*>(d)[0] = make_ulonglong2(v.p[0], v.p[1]);
+          reinterpret_cast<ulonglong2*>(d)[1] = make_ulonglong2(v.p[2], v.p[3]);
+        }
+      } else if (at.active) {
+        const float2 a = halves(add2(add2(v.p[0], v.p[1]), add2(v.p[2], v.p[3])));
+        *d = fmaf(a.x + a.y, over, -halves(first.p[0]).x);
+      }
+      t.sync();
+      team_group_means(g, t, red, cut ? g.inv_m : 8.f * g.inv_m, [&](int s, float mu) { mom[s].x = mu; });
     }
-    team_put(red, g, at, v);
-    t.sync();
-    team_group_sums(g, t, red, [&](int s, float a) { mom[s].x = a * g.inv_m; });
     t.sync();
     F8 less;
     {
-      float m[8];
-      team_values(g, at, [&](int s) { return mom[s].x; }, m);
+      float mu[8];
+      team_values(g, at, [&](int s) { return mom[s].x; }, mu);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { less.p[j] = pair(-m[2 * j], -m[2 * j + 1]); v.p[j] = 0; }
+      for (int j = 0; j < 4; ++j) { less.p[j] = pair(-mu[2 * j], -mu[2 * j + 1]); v.p[j] = 0; }
     }
     for (int k = 0; k < mine; ++k) {
       const F8 x = raw8_to_f8(slots.get(at0 + k));
@@ -789,7 +856,7 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_teams_kernel(
       p.stats[(size_t)(g.N + n) * g.G + g_first + s] = rstd;
     });
     t.sync();
-    Affine<T> affine;
+    Affine affine;
     float rstd[8];
     team_values(g, at, [&](int s) { return mom[s].y; }, rstd);
 #pragma unroll
@@ -950,7 +1017,7 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) apply_kernel(const __
     });
     __syncthreads();
   }
-  Affine<T> affine;
+  Affine affine;
   if (p.combined)
     load_affine(p, at, gamma, beta, [&](int s) { return make_float2(p.stats[(size_t)n * g.G + s], p.stats[(size_t)(g.N + n) * g.G + s]); }, affine);
   else

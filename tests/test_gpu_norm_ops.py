@@ -654,3 +654,30 @@ def test_variance_where_a_row_of_threads_differs(offset):
     x = torch.full((1, 150772, 24), offset, device="cuda")
     x[:, ::85] = 0
     _check_stats64(x, 3, ew.gn_forward(x, 3, torch.ones(24, device="cuda"), torch.zeros(24, device="cuda"), eps=EPS)[1])
+
+
+# (N, pixels, C, groups) of every form: teams (one pixel, columns in one group and cut, slices), clusters, streamed with the rows of sums
+# merged and combined, tiles of columns
+FORMS = [(700, 1, 64, 4), (4096, 4, 30, 6), (500, 49, 40, 8), (500, 3, 4096, 32), (2, 1024, 160, 32), (128, 256, 48, 3), (130, 1024, 96, 32),
+         (1, 16384, 64, 8), (2, 9001, 160, 32), (1, 20011, 30, 1), (1, 3, 2056, 8), (2, 40, 4104, 27), (30, 40, 4104, 513)]
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("shape", FORMS, ids=str)
+def test_groups_without_spread(prec_name, shape):
+    """Every value of a group the same: x - mean is 0 and y = act(beta), rounded once, whatever the value and gamma are."""
+    _, ew = _ops(prec_name)
+    n, p, c, groups = shape
+    r = np.random.default_rng(171)
+    level = _f32(r.choice([100.0, 3.3, -0.7, 4096.0, 1e4, -777.77, 0.0, 1e-3], (n, 1, groups))).to(ew.dtype)
+    x = level.repeat_interleave(c // groups, -1).expand(n, p, c).contiguous()
+    gamma = _f32(r.choice([1.0, 0.9, 1.13, -2.0], c))
+    beta = _f32(r.choice([0.0, 0.25, -0.125, 1e-3], c))
+    for act in ("none", "relu"):
+        y, stats, bits, _ = ew.gn_forward(x, groups, gamma, beta, act=act, eps=EPS, gate=act == "relu")
+        assert torch.equal(stats[0], level[:, 0].float()), "mean"
+        assert ((stats[1].double() * EPS ** 0.5 - 1).abs() <= K).all(), "rstd"
+        want = (beta if act == "none" else beta.clamp(min=0)).to(ew.dtype).expand(n, p, c)
+        assert torch.equal(y, want), float((y.double() - want.double()).abs().max())
+    bits = np.unpackbits(bits.cpu().numpy(), axis=-1, bitorder="little")[..., :c]
+    assert (bits == (beta > 0).cpu().numpy()).all()
