@@ -681,3 +681,38 @@ def test_groups_without_spread(prec_name, shape):
         assert torch.equal(y, want), float((y.double() - want.double()).abs().max())
     bits = np.unpackbits(bits.cpu().numpy(), axis=-1, bitorder="little")[..., :c]
     assert (bits == (beta > 0).cpu().numpy()).all()
+
+
+def test_silu_of_16_bit_tensors_far_from_zero():
+    """As test_silu_over_its_range, to the ends: sigmoids down to the smallest normal number (a smaller one may be 0, which costs
+    2^-126 (1 + |z|)), nothing beyond, infinities as a division has them.  A sigmoid of z < 0 is a product more, u, than there."""
+    _, ew = _ops("bf16")
+    c = 4096
+    z = np.linspace(-120, 120, c).astype(np.float32)
+    zz = z.astype(np.float64)
+    x = torch.zeros(1, 1, c, device="cuda", dtype=ew.dtype)
+    zero = torch.zeros(c, device="cuda")
+    u = 2.0 ** -24
+    s = 1 / (1 + np.exp(-zz))
+    d = (2 * np.abs(zz) + 10) * u
+    lost = 2.0 ** -126 * (1 + np.abs(zz))
+    y, stats, _, _ = ew.gn_forward(x, 4, zero, _f32(z), act="silu")
+    _near(y.reshape(c), zz * s, np.abs(zz * s) * (_half_step(ew.dtype) * (1 + 2 * d) + d + u) + lost, "y")
+    _, _, db = ew.gn_backward(torch.ones_like(x), x, stats, 4, zero, _f32(z), act="silu")
+    slope = s * (1 + zz * (1 - s))
+    inner = np.abs(zz) * (d * s + 2 * u * (1 - s) + u) + u
+    _near(db, slope, s * inner * (1 + 2 * d) + np.abs(slope) * (d + u) + lost, "dbeta")
+    inf, nan = float("inf"), float("nan")
+    ends = _f32([-1e4, -3e38, -inf, 1.0, nan, -1.0, inf, 3e38, -1e13, nan, -inf, -inf, 2.0, -60.0, -60.0, 60.0])
+    x = torch.zeros(1, 1, 16, device="cuda", dtype=ew.dtype)
+    y, stats, _, _ = ew.gn_forward(x, 4, zero[:16], ends, act="silu")
+    got, want = y.reshape(16).double().cpu(), (ends.double() / (1 + (-ends.double()).exp())).cpu()
+    assert torch.equal(got.isnan(), want.isnan()) and got[6] == inf
+    fine = want.isfinite()
+    assert ((got - want).abs()[fine] <= want.abs()[fine] * (2.0 ** -8 + 2.0 ** -15) + 1e-33).all(), (got, want)
+    _, _, db = ew.gn_backward(torch.ones_like(x), x, stats, 4, zero[:16], ends, act="silu")
+    s = torch.sigmoid(ends.double()).cpu()
+    want = s * (1 + ends.double().cpu() * (1 - s))
+    assert torch.equal(db.double().cpu().isnan(), want.isnan())
+    fine = want.isfinite()
+    assert ((db.double().cpu() - want).abs()[fine] <= want.abs()[fine] * 2.0 ** -15 + 1e-33).all(), (db, want)
