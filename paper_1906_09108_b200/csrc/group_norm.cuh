@@ -28,7 +28,8 @@
 // value of the CTA (a mean over at least a 64th of the channel's values), then about the CTA's group mean, and CTAs are combined by Chan's
 // formula.  The square of the distance from a mean over a share f of the values to the mean over all is at most var*(1 - f)/f, so what
 // cancels in each step is bounded by the data itself, whatever offset x has.  The team form has the image at hand and takes the mean first.
-// All sums are fp32 within a CTA (a chain of a thread's values, then of rows of threads, then a tree), in a fixed order.
+// All sums are fp32 within a CTA (a thread's values in chains of 64 that are added up in turn, then rows of threads, then a tree), in a
+// fixed order; what many CTAs leave is added in fp64.
 #pragma once
 #include <cooperative_groups.h>
 
@@ -282,7 +283,8 @@ __device__ __forceinline__ float lane_sum(float v, int lanes) {
   for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-// done(s, sum of first(c), sum of second(c) over the group's channels) for groups s < sets of `size` channels from c = 0 on.
+// done(s, sum of first(c), sum of second(c) over the group's channels) for groups s < sets of `size` channels from c = 0 on; chains of
+// at most 64 and then of at most 32 for 65536 channels.
 template <typename Value, typename Done>
 __device__ __forceinline__ void group_sums(int sets, int size, int lanes, Value value, Done done) {
   const int sub = threadIdx.x & (lanes - 1), per_pass = kThreads / lanes;
@@ -290,10 +292,15 @@ __device__ __forceinline__ void group_sums(int sets, int size, int lanes, Value 
     const int s = s0 + threadIdx.x / lanes;
     float2 a = make_float2(0.f, 0.f);
     if (s < sets)
+      for (int j0 = 0; j0 < size; j0 += 64 * lanes) {
+        float2 b = make_float2(0.f, 0.f);
+        const int end = min(size, j0 + 64 * lanes);
 #pragma unroll 8
-      for (int j = sub; j < size; j += lanes) {
-        const float2 v = value(s * size + j);
-        a.x += v.x; a.y += v.y;
+        for (int j = j0 + sub; j < end; j += lanes) {
+          const float2 v = value(s * size + j);
+          b.x += v.x; b.y += v.y;
+        }
+        a.x += b.x; a.y += b.y;
       }
     a.x = lane_sum(a.x, lanes);
     a.y = lane_sum(a.y, lanes);
@@ -1275,6 +1282,48 @@ struct Sums {
   }
 };
 
+// What chains of kChain vectors have come to, so that no chain is longer (one of 4096 equal gradients was off by 6e-5 of its sum): in
+// registers, or, in the forms that have none left, in 16 floats of the thread's own in shared memory, which a call asks for where its
+// threads have that many vectors.  (All forms there: fp32 with a mask 112 -> 137 us, 128 images of 32x32x160, for want of L1.)
+template <bool REGISTERS> struct Closed;
+template <> struct Closed<true> {
+  Sums all;
+  __device__ __forceinline__ Closed(uint4*) {}
+  __device__ __forceinline__ void take(Sums& s, bool) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      all.a.p[j] = add2(all.a.p[j], s.a.p[j]); all.b.p[j] = add2(all.b.p[j], s.b.p[j]);
+      s.a.p[j] = s.b.p[j] = 0;
+    }
+  }
+  __device__ __forceinline__ void give(Sums& s) { take(s, false); s = all; }
+};
+template <> struct Closed<false> {
+  ulonglong2* own;
+  __device__ __forceinline__ Closed(uint4* smem) : own(reinterpret_cast<ulonglong2*>(smem) + threadIdx.x) {}
+  __device__ __forceinline__ void take(Sums& s, bool first) {
+    if (!first) give(s);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      own[j * kThreads] = make_ulonglong2(s.a.p[2 * j], s.a.p[2 * j + 1]);
+      own[(2 + j) * kThreads] = make_ulonglong2(s.b.p[2 * j], s.b.p[2 * j + 1]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s.a.p[j] = s.b.p[j] = 0;
+  }
+  __device__ __forceinline__ void give(Sums& s) const {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const ulonglong2 a = own[j * kThreads], b = own[(2 + j) * kThreads];
+      s.a.p[2 * j] = add2(s.a.p[2 * j], a.x); s.a.p[2 * j + 1] = add2(s.a.p[2 * j + 1], a.y);
+      s.b.p[2 * j] = add2(s.b.p[2 * j], b.x); s.b.p[2 * j + 1] = add2(s.b.p[2 * j + 1], b.y);
+    }
+  }
+};
+template <typename T> constexpr int kClosedFrom = kChain + batch_of<T>() * kAhead;       // vectors from which a chain is closed, see Stream::run
+constexpr size_t kClosedBytes = (size_t)kThreads * 16 * sizeof(float);
+template <int SLOPE> constexpr bool kClosedInRegisters = SLOPE == SLOPE_ONE || SLOPE == SLOPE_MASK;
+
 // First pass: A and B of each channel over a CTA's pixels.
 template <typename T, int W, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_sums_kernel(const __grid_constant__ Backward<T> p) {
@@ -1294,6 +1343,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_sums_kernel
   Channels ch;
   float rstd[8];
   Sums sums;
+  Closed<kClosedInRegisters<SLOPE>> closed(smem + Feed<T, W, CK>::words(slope == SLOPE_MASK, false));
   auto issue = [&](int slot) { feed.issue(slot); };
   Stream<kBatch>::start(sh.mine, issue);
   load_channels(p, at, n, slope, ch, rstd);
@@ -1307,7 +1357,10 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_sums_kernel
         operands<T, CK>(passed<T, CK>(h, slope), h, slope, ch, dz, d);
         sums.add(dz, d);
       }
+  }, [&](int k) {
+    if ((k & (kChain - 1)) == 0) closed.take(sums, k == kChain);
   });
+  if (sh.mine >= kClosedFrom<T>) closed.give(sums);
   __syncthreads();                    // the sums go where the rings were
   float* red = reinterpret_cast<float*>(smem);
   sums.put(red, g, at, rstd);
@@ -1829,7 +1882,7 @@ inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<
   if (e != cudaSuccess) return e;
   auto rings = [&](bool res) { return 16 * (size_t)Feed<T, W, CK>::words(p.slope == SLOPE_MASK, res); };
   e = launch_chained(backward_sums_kernel<T, W, CK, SLOPE>, dim3((unsigned)g.N, (unsigned)g.parts, (unsigned)g.tiles), dim3(kThreads),
-                     std::max(rings(false), (size_t)2 * kThreads * 8 * 4), st, p);
+                     rings(false) + (kClosedInRegisters<SLOPE> || g.iters < kClosedFrom<T> ? 0 : kClosedBytes), st, p);
   if (merges_backward(g)) p.totals = nullptr;
   else if (e == cudaSuccess)
     e = launch_chained(totals_kernel, dim3((unsigned)(g.N * blocks)), dim3(1024), 0, st, (const float*)p.partial, g.parts, width, p.totals);

@@ -716,3 +716,72 @@ def test_silu_of_16_bit_tensors_far_from_zero():
     assert torch.equal(db.double().cpu().isnan(), want.isnan())
     fine = want.isfinite()
     assert ((db.double().cpu() - want).abs()[fine] <= want.abs()[fine] * 2.0 ** -15 + 1e-33).all(), (db, want)
+
+
+@pytest.mark.parametrize("prec_name, shape, value", [("fp32", (1, 296 * 256 * 4096, 1, 1), 0.5108032), ("fp32", (150, 4096, 1032, 8), 0.5108032),
+                                                      ("bf16", (150, 4096, 1032, 8), 0.51171875)], ids=str)
+def test_gradients_where_a_thread_has_many_values(prec_name, shape, value):
+    """Thousands of gradients a thread, all of them the same, as the mean of a map hands them down: no sum may drift with their
+    number."""
+    _, ew = _ops(prec_name)
+    n, p, c, groups = shape
+    x = torch.empty((n, p, c), dtype=ew.dtype, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(13)
+    for i in range(n):
+        x[i] = torch.randn((p, c), generator=g, device="cuda") * 1.3 + 0.4
+    dy = torch.full_like(x, value)
+    one = torch.ones(c, device="cuda")
+    _, stats, _, _ = ew.gn_forward(x, groups, one, torch.zeros_like(one), eps=EPS)
+    dx, dgamma, dbeta = ew.gn_backward(dy, x, stats, groups, one)
+    v, wide = float(dy.view(-1)[0]), lambda t: t.double().repeat_interleave(c // groups)
+    total = v * n * p
+    assert ((dbeta.double() - total).abs() <= 2 * K * total).all(), float((dbeta.double() / total - 1).abs().max())
+    A, mag = torch.zeros(c, dtype=torch.float64, device="cuda"), torch.zeros(c, dtype=torch.float64, device="cuda")
+    for i in range(n):
+        m, r = wide(stats[0, i]), wide(stats[1, i])
+        A += v * ((x[i].double() - m) * r).sum(0)
+        mag += v * (r * (x[i].double().abs() + m.abs())).sum(0)
+    assert ((dgamma.double() - A).abs() <= 2 * K * mag).all()
+    m, r, x0 = wide(stats[0, 0]), wide(stats[1, 0]), x[0].double()
+    by = lambda t: wide(t.view(p, groups, c // groups).mean((0, 2)))  # noqa: E731
+    xhat = (x0 - m) * r
+    size = (x0.abs() + m.abs()) * r
+    want = r * (v - v - xhat * by(v * xhat))
+    assert ((dx[0].double() - want).abs() <= _half_step(ew.dtype) * want.abs() + 2 * K * r * (2 * v + size * by(v * size))).all()
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("act, gate, held, by", [("none", False, True, 0), ("relu", False, False, 0), ("relu", True, False, 0), ("relu", True, True, 0), ("silu", False, False, 0),
+                                                 ("silu", False, True, 0), ("relu", True, True, 4), ("silu", False, False, 2), ("relu", False, False, 1)])
+def test_gradients_of_long_threads_in_every_form(prec_name, act, gate, held, by):
+    """More vectors a thread than a chain of sums has, against float64 on the GPU."""
+    _, ew = _ops(prec_name)
+    n, p, c, groups = 2, 148 * 90 + 5, 1032, 8
+    buf = torch.empty(n * p * c + by, dtype=ew.dtype, device="cuda")
+    x = buf[by:].view(n, p, c)
+    x.copy_(torch.randn((n, p, c), generator=torch.Generator(device="cuda").manual_seed(23), device="cuda") * 1.3 + 0.4)
+    dy = torch.randn((n, p, c), generator=torch.Generator(device="cuda").manual_seed(24), device="cuda").mul_(0.2).add_(0.5108032).to(ew.dtype)
+    gamma, beta = (_f32(a) for a in _params(c, 231))
+    y, stats, bits, kept = ew.gn_forward(x, groups, gamma, beta, act=act, gate=gate, checkpoint=held)
+    dx, dgamma, dbeta = ew.gn_backward(dy, kept if held else x, stats, groups, gamma, beta, act=act, gate=bits, mask=y if act == "relu" and not gate else None)
+    xo = (ew.ckpt_decode(kept) if held else x).double()
+    for i in range(n):
+        m, r = (stats[k, i].double().repeat_interleave(c // groups) for k in range(2))
+        xhat, size = (xo[i] - m) * r, (xo[i].abs() + m.abs()) * r
+        dz = dy[i].double()
+        adz = dz.abs()
+        if act == "relu":
+            dz = dz * (y[i] > 0)
+            adz = dz.abs()
+        elif act == "silu":
+            z = gamma * xhat + beta
+            s = torch.sigmoid(z)
+            dz, adz = dz * s * (1 + z * (1 - s)), (dz * s * (1 + z * (1 - s))).abs() + 0.5 * adz * (size * gamma.abs() + beta.abs())
+        total = (dz * xhat).sum(0), dz.sum(0), (adz * size).sum(0), adz.sum(0)
+        A, B, ma, mb = total if i == 0 else (s + t for s, t in zip((A, B, ma, mb), total))
+        mean = lambda t: t.view(p, groups, -1).mean((0, 2)).repeat_interleave(c // groups)  # noqa: E731
+        h = dz * gamma
+        want = r * (h - mean(h) - xhat * mean(h * xhat))
+        h = adz * gamma.abs()
+        assert ((dx[i].double() - want).abs() <= _half_step(ew.dtype) * want.abs() + 2 * K * r * (h + mean(h) + size * mean(h * size))).all()
+    assert ((dgamma.double() - A).abs() <= 2 * K * ma).all() and ((dbeta.double() - B).abs() <= 2 * K * mb).all()
