@@ -206,7 +206,8 @@ template <int B> struct Stream {
   }
 };
 
-// Whether copies of these vectors may begin before a kernel's grid_dependency_wait(), see moments_kernel: those that go past L1.
+// Whether copies of these vectors may begin before a kernel's grid_dependency_wait(), see moments_kernel: those that go past L1.  (L1 is
+// not coherent: a line that it holds from before the wait may be older than what the wait makes visible.)
 template <typename T, int W> constexpr bool kEarly = W == kWhole && sizeof(T) == 2;
 
 // This thread's place in a CTA's tile.
@@ -1210,16 +1211,33 @@ template <typename T, int W, bool CK> struct Feed {
       }
   }
   __device__ __forceinline__ void issue(int s) {
-    const uint32_t o = next;
+    vectors(s, next);
+    if constexpr (CK) bytes_of_x(s, next);
     next += step;
+  }
+  __device__ __forceinline__ void vectors(int s, uint32_t o) {
     dys.template fetch<W>(s, from.dy + o, left);
-    if constexpr (CK) {
-      if constexpr (W == kWhole) copy8_async(codes + s * kThreads, from.codes + o); else codes[s * kThreads] = load_codes<kCodeWidth<T, W>>(from.codes + o, left);
-    } else {
-      xs.template fetch<W>(s, from.x + o, left);
-    }
+    if constexpr (!CK) xs.template fetch<W>(s, from.x + o, left);
     if (slope == SLOPE_MASK) masks.template fetch<W>(s, from.mask + o, left);
     if (res) ress.template fetch<W>(s, res + o, left);
+  }
+  __device__ __forceinline__ void bytes_of_x(int s, uint32_t o) {           // 8 of them: there is no copy of that size past L1
+    if constexpr (W == kWhole) copy8_async(codes + s * kThreads, from.codes + o); else codes[s * kThreads] = load_codes<kCodeWidth<T, W>>(from.codes + o, left);
+  }
+  // Stream::start in two parts: what goes past L1, and what does not (with the first group all of the former).
+  __device__ __forceinline__ void start_past_l1() {
+#pragma unroll
+    for (int k = 0; k < kBatch * kAhead; ++k)
+      if (k < n) vectors(k, next + (uint32_t)k * step);
+  }
+  __device__ __forceinline__ void start_rest() {
+#pragma unroll
+    for (int k = 0; k < kBatch * kAhead; ++k) {
+      if constexpr (CK)
+        if (k < n) bytes_of_x(k, next + (uint32_t)k * step);
+      if (k % kBatch == kBatch - 1) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    next += (uint32_t)(kBatch * kAhead) * step;
   }
   __device__ __forceinline__ Held<T, CK> get(int slot, int u) const {
     Held<T, CK> h;
@@ -1593,11 +1611,11 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_apply_kerne
   const int c_last = min(g.C, c_first + g.cols * 8) - 1;
   const int g_first = c_first / g.Cg, sets = c_last / g.Cg - g_first + 1, c_base = g_first * g.Cg;
   Feed<T, W, CK> feed(p, at, sh, slope, p.res, true, smem);
-  if constexpr (kEarly<T, W>) Stream<kBatch>::start(sh.mine, [&](int slot) { feed.issue(slot); });
+  if constexpr (kEarly<T, W>) feed.start_past_l1();
   grid_dependency_wait();
   grid_dependency_release();
   auto issue = [&](int slot) { feed.issue(slot); };
-  if constexpr (!kEarly<T, W>) Stream<kBatch>::start(sh.mine, issue);
+  if constexpr (kEarly<T, W>) feed.start_rest(); else Stream<kBatch>::start(sh.mine, issue);
   feed.start_bytes();
   Channels ch;
   float rstd[8];

@@ -17,8 +17,10 @@ namespace fdg {
 // backward apply) are launched with programmatic stream serialisation: the next kernel of the stream may be
 // scheduled while this one still runs, does the part of its start-up that needs nothing from global
 // memory (barriers, tensor-memory allocation, descriptor prefetch), and then blocks in grid_dependency_wait()
-// until the preceding kernel has completed and its writes are visible.  Nothing may be read from or written
-// to global memory before that wait.  grid_dependency_release() tells the scheduler that, as far as this
+// until the preceding kernel has completed and its writes are visible.  Nothing may be written to global memory
+// before that wait, and nothing read, but for copies past L1 (cp.async.cg) of what was complete before the
+// preceding kernel released this one: a kernel that releases after its own wait vouches for everything
+// before itself, though not for what it writes (the second passes of group_norm.cuh).  grid_dependency_release() tells the scheduler that, as far as this
 // block is concerned, the next kernel may start being scheduled (it fires once every block has called it or
 // exited).  Both are no-ops in a kernel launched the ordinary way.
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -785,3 +785,38 @@ def test_gradients_of_long_threads_in_every_form(prec_name, act, gate, held, by)
         h = adz * gamma.abs()
         assert ((dx[i].double() - want).abs() <= _half_step(ew.dtype) * want.abs() + 2 * K * r * (h + mean(h) + size * mean(h * size))).all()
     assert ((dgamma.double() - A).abs() <= 2 * K * ma).all() and ((dbeta.double() - B).abs() <= 2 * K * mb).all()
+
+
+def test_buffers_written_anew_for_every_call():
+    """Codes, scales, bits and scratch in the same buffers call after call, with nothing between the calls: each backward pass
+    reads what the forward pass before it left."""
+    B, ew = _ops("bf16")
+    lib, prec, st = ew.lib, ew.precision, torch.cuda.current_stream().cuda_stream
+    for n, p, c, groups in ((8, 1024, 160, 32), (2, 12000, 96, 8), (2000, 4, 64, 4)):
+        s, need, back = B.fdg_gn_shape(n, p, c, groups), C.c_size_t(), C.c_size_t()
+        assert lib.fdg_gn_scratch_bytes(prec, C.byref(s), 0, C.byref(need)) == 0
+        assert lib.fdg_gn_scratch_bytes(prec, C.byref(s), 1, C.byref(back)) == 0
+        gamma, beta = (_f32(a) for a in _params(c, 201))
+        ins = [(_mk((n, p, c), 202 + i, ew.dtype)[0], _mk((n, p, c), 212 + i, ew.dtype)[0]) for i in range(4)]
+        y = torch.empty_like(ins[0][0])
+        stats = torch.empty((2, n, groups), device="cuda")
+        bits, codes, scales, scratch = (torch.empty(k, dtype=torch.uint8, device="cuda") for k in
+                                        (n * p * (c // 8), n * p * c, n * p * -(-c // 32), max(need.value, back.value, 1)))
+        got = []
+        torch.cuda.synchronize()
+        for k in range(12):
+            x, dy = ins[k % 4]
+            dx, dg, db = torch.empty_like(x), torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+            assert lib.fdg_gn_forward(prec, C.byref(s), x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), None, B.FDG_ACT_RELU, EPS, y.data_ptr(),
+                                      stats.data_ptr(), bits.data_ptr(), codes.data_ptr(), scales.data_ptr(), scratch.data_ptr(), need.value, st) == 0
+            assert lib.fdg_gn_backward(prec, C.byref(s), dy.data_ptr(), None, codes.data_ptr(), scales.data_ptr(), stats.data_ptr(), gamma.data_ptr(), None,
+                                       B.FDG_ACT_RELU, None, bits.data_ptr(), None, dx.data_ptr(), dg.data_ptr(), db.data_ptr(), scratch.data_ptr(),
+                                       back.value, st) == 0
+            got.append((dx, dg, db))
+        torch.cuda.synchronize()
+        for k, (x, dy) in enumerate(ins):
+            _, stats1, bits1, held1 = ew.gn_forward(x, groups, gamma, beta, act="relu", gate=True, checkpoint=True)
+            torch.cuda.synchronize()
+            want = ew.gn_backward(dy, held1, stats1, groups, gamma, act="relu", gate=bits1)
+            for j in range(k, 12, 4):
+                assert all(torch.equal(a, b) for a, b in zip(got[j], want)), (k, j)
