@@ -937,16 +937,15 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) moments_kernel(const 
   }
 }
 
-// Streamed, between the passes where an image has many rows: the statistics of group blockIdx.x from the moments of its
-// channels (tiles > 1) or its own in every row, in fp64.
+// Streamed, between the passes where an image has many rows: the statistics of every gridDim.x-th group from blockIdx.x on, from the
+// moments of its channels (tiles > 1) or its own in every row, in fp64.
 template <typename T>
 __global__ void __launch_bounds__(1024) combine_kernel(const __grid_constant__ Forward<T> p) {
   __shared__ double part[32];
   __shared__ double total;
   const Geom& g = p.g;
-  const int n = blockIdx.x / g.G, s = blockIdx.x % g.G, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   const int width = g.tiles == 1 ? g.G : g.C, size = g.tiles == 1 ? 1 : g.Cg;      // of a row, of the group's share of it
-  const float* src = p.partial + (size_t)n * g.parts * 2 * width + (size_t)s * size;
   grid_dependency_wait();
   grid_dependency_release();
   auto sum = [&](double v) {
@@ -962,27 +961,31 @@ __global__ void __launch_bounds__(1024) combine_kernel(const __grid_constant__ F
     __syncthreads();
     return total;
   };
-  auto each = [&](auto take) {
-    const int step = blockDim.x / size, over = blockDim.x - step * size;
-    int j = threadIdx.x / size, c = threadIdx.x - j * size;
-    while (j < g.parts) {
-      const float* row = src + (size_t)j * 2 * width + c;
-      take((double)min(g.pix, g.P - j * g.pix), (double)row[0], row + width);
-      j += step; c += over;
-      if (c >= size) { c -= size; ++j; }
-    }
-  };
   const double values = (double)g.P * size;
-  double a = 0.0;
-  each([&](double cnt, double mu, const float*) { a += cnt * mu; });
-  const double mean = sum(a) / values;
-  a = 0.0;
   const double per = g.tiles == 1 ? (double)g.Cg : 1.0;                            // values behind a pixel of a row's entry
-  each([&](double cnt, double mu, const float* m2) { a += (double)*m2 + cnt * per * (mu - mean) * (mu - mean); });
-  const double var = sum(a) / ((double)g.P * g.Cg);
-  if (threadIdx.x == 0) {
-    p.stats[(size_t)n * g.G + s] = (float)mean;
-    p.stats[(size_t)(g.N + n) * g.G + s] = (float)(1.0 / sqrt(var + (double)p.eps));
+  for (size_t item = blockIdx.x; item < (size_t)g.N * g.G; item += gridDim.x) {
+    const int n = (int)(item / g.G), s = (int)(item - (size_t)n * g.G);
+    const float* src = p.partial + (size_t)n * g.parts * 2 * width + (size_t)s * size;
+    auto each = [&](auto take) {
+      const int step = blockDim.x / size, over = blockDim.x - step * size;
+      int j = threadIdx.x / size, c = threadIdx.x - j * size;
+      while (j < g.parts) {
+        const float* row = src + (size_t)j * 2 * width + c;
+        take((double)min(g.pix, g.P - j * g.pix), (double)row[0], row + width);
+        j += step; c += over;
+        if (c >= size) { c -= size; ++j; }
+      }
+    };
+    double a = 0.0;
+    each([&](double cnt, double mu, const float*) { a += cnt * mu; });
+    const double mean = sum(a) / values;
+    a = 0.0;
+    each([&](double cnt, double mu, const float* m2) { a += (double)*m2 + cnt * per * (mu - mean) * (mu - mean); });
+    const double var = sum(a) / ((double)g.P * g.Cg);
+    if (threadIdx.x == 0) {
+      p.stats[(size_t)n * g.G + s] = (float)mean;
+      p.stats[(size_t)(g.N + n) * g.G + s] = (float)(1.0 / sqrt(var + (double)p.eps));
+    }
   }
 }
 
@@ -1406,14 +1409,18 @@ __device__ __forceinline__ void add_rows(const float* __restrict__ in, int rows,
   }
   __syncthreads();
 }
-// Between the passes where an image has many rows: totals[n][i] = the sum of the image's rows of sums, n = blockIdx.x / blocks.
-__global__ void __launch_bounds__(1024) totals_kernel(const float* __restrict__ partial, int rows, int width, float* __restrict__ totals) {
+// Between the passes where an image has many rows: totals[n][i] = the sum of image n's rows of sums, 32 of `width` at a time, every
+// gridDim.x-th of them from blockIdx.x on.
+__global__ void __launch_bounds__(1024) totals_kernel(const float* __restrict__ partial, int images, int rows, int width, float* __restrict__ totals) {
   __shared__ double fin[32][33];
-  const int blocks = (width + 31) / 32, n = blockIdx.x / blocks;
+  const int blocks = (width + 31) / 32;
   grid_dependency_wait();
   grid_dependency_release();
-  add_rows(partial + (size_t)n * rows * width, rows, width, (blockIdx.x - n * blocks) * 32, fin,
-           [&](int i, float v) { totals[(size_t)n * width + i] = v; });
+  for (size_t item = blockIdx.x; item < (size_t)images * blocks; item += gridDim.x) {
+    const int n = (int)(item / blocks);
+    add_rows(partial + (size_t)n * rows * width, rows, width, (int)(item - (size_t)n * blocks) * 32, fin,
+             [&](int i, float v) { totals[(size_t)n * width + i] = v; });
+  }
 }
 
 // The team form of the backward pass: both passes over an image from shared memory.  A team adds its images' A and B up in registers (at
@@ -1808,11 +1815,9 @@ inline size_t partial_floats(const Plan& pl) { return (size_t)pl.rows * 2 * pl.g
 // many images of one row each took 5 of 5.8 ms for 4096 of 4096 channels.)
 inline bool merges(const Geom& g) { return g.tiles == 1 && g.parts <= kMergeParts; }
 inline bool merges_backward(const Geom& g) { return g.parts <= kMergeParts; }
-// Whether every launch's grid can be given (with many images a plan has one share of each).
-inline bool grid_ok(const Plan& pl) {
-  const Geom& g = pl.g;
-  return pl.resident || merges(g) || ((int64_t)g.N * g.G <= INT32_MAX && (int64_t)g.N * ((2 * (int64_t)g.C + 31) / 32) <= INT32_MAX);
-}
+// CTAs of a launch whose items are as many as groups or images times blocks of channels, more than a grid may have.
+constexpr size_t kItemCtas = 16 * kSms;
+inline unsigned item_ctas(size_t items) { return (unsigned)std::min(items, kItemCtas); }
 
 // ---- host side: launches ---------------------------------------------------------------------------------------
 template <typename Kernel, typename Params>
@@ -1852,7 +1857,7 @@ template <typename T, int W, int ACT, int EXTRA> inline cudaError_t launch_forwa
   p.combined = !merges(g);
   if (e == cudaSuccess && p.combined) {
     const int64_t entries = (int64_t)g.parts * (g.tiles == 1 ? 1 : g.Cg);
-    e = launch_chained(combine_kernel<T>, dim3((unsigned)(g.N * g.G)), dim3(32 * pow2_up_to(entries / 64, 32)), 0, st, p);
+    e = launch_chained(combine_kernel<T>, dim3(item_ctas((size_t)g.N * g.G)), dim3(32 * pow2_up_to(entries / 64, 32)), 0, st, p);
   }
   if (e == cudaSuccess)
     e = launch_chained(apply_kernel<T, W, ACT, EXTRA>, grid, dim3(kThreads), (p.res ? 2 : 1) * ring + (p.combined ? 0 : 8 * (size_t)g.G), st, p);
@@ -1903,7 +1908,7 @@ inline cudaError_t launch_backward_as(cudaStream_t st, const Plan& pl, Backward<
                      rings(false) + (kClosedInRegisters<SLOPE> || g.iters < kClosedFrom<T> ? 0 : kClosedBytes), st, p);
   if (merges_backward(g)) p.totals = nullptr;
   else if (e == cudaSuccess)
-    e = launch_chained(totals_kernel, dim3((unsigned)(g.N * blocks)), dim3(1024), 0, st, (const float*)p.partial, g.parts, width, p.totals);
+    e = launch_chained(totals_kernel, dim3(item_ctas((size_t)g.N * blocks)), dim3(1024), 0, st, (const float*)p.partial, g.N, g.parts, width, p.totals);
   // coefficients of the tile's groups; with one tile also the channels' sums
   const size_t own = 8 * (size_t)std::min(g.G, g.cols * 8) + (g.tiles == 1 ? 8 * (size_t)g.C : 0);
   p.extra = (blocks + g.parts - 1) / g.parts;

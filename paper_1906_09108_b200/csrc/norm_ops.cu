@@ -71,12 +71,10 @@ fdg_status fdg_gn_scratch_bytes(int precision, const fdg_gn_shape* s, int backwa
   const int b = (int)elem_bytes(precision);
   if (!backward) {
     const gn::Plan pl = gn::plan_forward(b, s->N, s->HW, s->C, s->groups);
-    if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
     *bytes = forward_need(pl);
     return FDG_OK;
   }
   const gn::Plan pl = gn::plan_backward(b, s->N, s->HW, s->C, s->groups);
-  if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
   *bytes = backward_need(pl);
   return FDG_OK;
 }
@@ -90,7 +88,6 @@ fdg_status fdg_gn_forward(int precision, const fdg_gn_shape* s, const void* x, c
   const unsigned b = elem_bytes(precision);
   if (!aligned_to(x, b) || !aligned_to(y, b) || !aligned_to(res, b) || !aligned_to(scratch, 256)) return FDG_ERR_INVALID_ARG;
   const gn::Plan pl = gn::plan_forward((int)b, s->N, s->HW, s->C, s->groups);
-  if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
   const size_t need = forward_need(pl);
   if (need > 0 && (!scratch || scratch_bytes < need)) return FDG_ERR_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -109,7 +106,6 @@ fdg_status fdg_gn_backward(int precision, const fdg_gn_shape* s, const void* dy,
   if (!aligned_to(dy, b) || !aligned_to(x, b) || !aligned_to(mask, b) || !aligned_to(res, b) || !aligned_to(dx, b) || !aligned_to(scratch, 256))
     return FDG_ERR_INVALID_ARG;
   const gn::Plan pl = gn::plan_backward((int)b, s->N, s->HW, s->C, s->groups);
-  if (!gn::grid_ok(pl)) return FDG_ERR_INVALID_ARG;
   if (!scratch || scratch_bytes < backward_need(pl)) return FDG_ERR_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return status_of(precision == FDG_BF16_TC

@@ -820,3 +820,12 @@ def test_buffers_written_anew_for_every_call():
             want = ew.gn_backward(dy, held1, stats1, groups, gamma, act="relu", gate=bits1)
             for j in range(k, 12, 4):
                 assert all(torch.equal(a, b) for a, b in zip(got[j], want)), (k, j)
+
+
+def test_more_groups_and_totals_than_a_grid_has_ctas():
+    """The statistics of many groups and the totals of many images, each formed by a launch of its own of bounded size."""
+    _, ew = _ops("bf16")
+    for shape in ((12, 40, 4104, 1026), (16, 70, 4104, 4104), (3, 300, 2064, 2064)):
+        n, p, c, groups = shape
+        x, xo, y, stats, bits, _ = _check_forward(ew, shape, "relu", False, seed=220, gate=True)
+        _check_backward(ew, shape, "relu", 220, xo, x, stats, y, bits, True, False)

@@ -101,3 +101,14 @@ def test_ckpt_refusals(lib):
             assert lib.fdg_ckpt_decode(prec, *args, None) == INVALID
     assert lib.fdg_ckpt_encode(2, P, 4, 8, P, P, None) == INVALID
     assert lib.fdg_ckpt_decode(2, P, P, 4, 8, P, None) == INVALID
+
+
+@pytest.mark.parametrize("prec", [B.FDG_FP32_CUDACORE, B.FDG_BF16_TC])
+def test_shapes_up_to_the_limits_that_are_named(lib, prec):
+    """2^36 values, 2^30 images, 65536 channels: nothing within these is refused for the size of a grid."""
+    for shape in ((1 << 20, 1, 4104, 4104), (1 << 20, 1, 65536, 65536), (1 << 20, 1, 65536, 1), (1 << 30, 1, 64, 64), (1 << 30, 64, 1, 1), (1, 2 ** 31 - 1, 32, 4),
+                  (1 << 19, 2, 65536, 65536), (16, 1 << 16, 65536, 65536), (1 << 14, 100, 4104, 8)):
+        assert shape[0] * shape[1] * shape[2] <= 1 << 36
+        for backward in (0, 1):
+            rc, need = _scratch(lib, prec, *shape, backward=backward)
+            assert rc == 0 and need % 256 == 0, (shape, backward)
