@@ -183,7 +183,7 @@ fdg_status fdg_ckpt_decode(int precision, const int8_t* codes, const uint8_t* sc
  * The normalisation that does not depend on which images share a batch.  x [N][HW][C]; group g of an image is channels
  * [g*C/groups, (g+1)*C/groups) at all of its pixels (groups = 1: layer norm over an image, groups = C: instance norm).
  * `groups` divides C; any C up to 65536, at most 2^30 images and 2^36 values, any alignment that the storage type has (multiples of 8 channels on 16-byte aligned tensors are
- * fastest).  gamma, beta, dgamma, dbeta [C], stats [2][N][groups] (mean, then 1/sqrt(var + eps), biased variance) are fp32.
+ * fastest).  gamma, beta, dgamma, dbeta [C], stats [2][N][groups] (mean, then 1/sqrt(var + eps), biased variance) are fp32, 4-byte aligned.
  * `scratch`: fdg_gn_scratch_bytes bytes of device memory for that pass (0 for a forward pass that needs none: scratch may then
  * be NULL), 256-byte aligned, any contents; not to be shared by calls that may run at the same time.  The result of a call does not depend on scheduling.  No output
  * overlaps an input or another output.  Errors: FDG_ERR_INVALID_ARG (null pointer, bad shape, precision or activation, a

@@ -17,6 +17,11 @@ static bool gn_shape_ok(int precision, const fdg_gn_shape* s) {
   return s && precision_ok(precision) && s->N >= 1 && s->N <= 1 << 30 && s->HW >= 1 && s->C >= 1 && s->groups >= 1 && s->C % s->groups == 0 &&
          s->C <= 1 << 16 && rows_ok((size_t)s->N * (size_t)s->HW, s->C);
 }
+static bool floats_ok(std::initializer_list<const float*> arrays) {
+  for (const float* a : arrays)
+    if (!aligned_to(a, sizeof(float))) return false;
+  return true;
+}
 static size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Scratch: the forward pass's rows of sums; the backward pass's per-image totals [N][2][C], where it forms them, and its rows of sums.
@@ -86,7 +91,8 @@ fdg_status fdg_gn_forward(int precision, const fdg_gn_shape* s, const void* x, c
   if (act != FDG_ACT_NONE && act != FDG_ACT_RELU && act != FDG_ACT_SILU) return FDG_ERR_INVALID_ARG;
   if ((act == FDG_ACT_SILU && res) || (gate && act != FDG_ACT_RELU) || (codes != nullptr) != (scales != nullptr)) return FDG_ERR_INVALID_ARG;
   const unsigned b = elem_bytes(precision);
-  if (!aligned_to(x, b) || !aligned_to(y, b) || !aligned_to(res, b) || !aligned_to(scratch, 256)) return FDG_ERR_INVALID_ARG;
+  if (!aligned_to(x, b) || !aligned_to(y, b) || !aligned_to(res, b) || !aligned_to(scratch, 256) || !floats_ok({gamma, beta, stats}))
+    return FDG_ERR_INVALID_ARG;
   const gn::Plan pl = gn::plan_forward((int)b, s->N, s->HW, s->C, s->groups);
   const size_t need = forward_need(pl);
   if (need > 0 && (!scratch || scratch_bytes < need)) return FDG_ERR_WORKSPACE_TOO_SMALL;
@@ -103,7 +109,8 @@ fdg_status fdg_gn_backward(int precision, const fdg_gn_shape* s, const void* dy,
   if ((codes != nullptr) != (scales != nullptr) || (x != nullptr) == (codes != nullptr)) return FDG_ERR_INVALID_ARG;
   if ((mask != nullptr) + (gate != nullptr) != (act == FDG_ACT_RELU ? 1 : 0) || (act == FDG_ACT_SILU && !beta)) return FDG_ERR_INVALID_ARG;
   const unsigned b = elem_bytes(precision);
-  if (!aligned_to(dy, b) || !aligned_to(x, b) || !aligned_to(mask, b) || !aligned_to(res, b) || !aligned_to(dx, b) || !aligned_to(scratch, 256))
+  if (!aligned_to(dy, b) || !aligned_to(x, b) || !aligned_to(mask, b) || !aligned_to(res, b) || !aligned_to(dx, b) ||
+      !aligned_to(scratch, 256) || !floats_ok({stats, gamma, beta, dgamma, dbeta}))
     return FDG_ERR_INVALID_ARG;
   const gn::Plan pl = gn::plan_backward((int)b, s->N, s->HW, s->C, s->groups);
   if (!scratch || scratch_bytes < backward_need(pl)) return FDG_ERR_WORKSPACE_TOO_SMALL;

@@ -112,3 +112,18 @@ def test_shapes_up_to_the_limits_that_are_named(lib, prec):
         for backward in (0, 1):
             rc, need = _scratch(lib, prec, *shape, backward=backward)
             assert rc == 0 and need % 256 == 0, (shape, backward)
+
+
+def test_gn_refuses_fp32_arrays_off_their_alignment(lib):
+    """A kernel reads and writes them as floats: an address that is no multiple of 4 must not reach one."""
+    s = B.fdg_gn_shape(8, 256, 8, 4)
+    need = _scratch(lib, B.FDG_BF16_TC, 8, 256, 8, 4)[1]
+    for off in (1, 2, 3):
+        odd = C.c_void_p(4096 + off)
+        for name in ("gamma", "beta", "stats"):
+            a = dict(x=P, gamma=P, beta=P, res=None, act=B.FDG_ACT_SILU, eps=1e-5, y=P, stats=P, gate=None, codes=None, scales=None, scratch=P)
+            assert lib.fdg_gn_forward(B.FDG_BF16_TC, C.byref(s), *dict(a, **{name: odd}).values(), need, None) == INVALID, name
+        for name in ("stats", "gamma", "beta", "dgamma", "dbeta"):
+            a = dict(dy=P, x=P, codes=None, scales=None, stats=P, gamma=P, beta=P, act=B.FDG_ACT_SILU, mask=None, gate=None, res=None, dx=P, dgamma=P, dbeta=P,
+                     scratch=P)
+            assert lib.fdg_gn_backward(B.FDG_BF16_TC, C.byref(s), *dict(a, **{name: odd}).values(), need, None) == INVALID, name
