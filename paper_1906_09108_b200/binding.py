@@ -647,11 +647,13 @@ class EwOps:
 
     def _gn(self, shape, groups, backward):
         """(shape structure, scratch bytes, layouts of the statistics and of the gate) of a group norm of tensors [N, pixels.., C]."""
+        if not isinstance(groups, int):                      # 4.0 == 4 as a key
+            raise FDGError(1, "group norm: expected a number of groups, got %r" % (groups,))
         key = (shape, groups, backward)
         got = self._gn_shapes.get(key)
         if got is None:
-            if len(shape) < 2 or not isinstance(groups, int):
-                raise FDGError(1, "group norm: expected [N, pixels.., C] and a number of groups, got %s and %r" % (tuple(shape), groups))
+            if len(shape) < 2:
+                raise FDGError(1, "group norm: expected [N, pixels.., C], got %s" % (tuple(shape),))
             hw = 1
             for v in shape[1:-1]:
                 hw *= v

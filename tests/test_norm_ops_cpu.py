@@ -127,3 +127,17 @@ def test_gn_refuses_fp32_arrays_off_their_alignment(lib):
             a = dict(dy=P, x=P, codes=None, scales=None, stats=P, gamma=P, beta=P, act=B.FDG_ACT_SILU, mask=None, gate=None, res=None, dx=P, dgamma=P, dbeta=P,
                      scratch=P)
             assert lib.fdg_gn_backward(B.FDG_BF16_TC, C.byref(s), *dict(a, **{name: odd}).values(), need, None) == INVALID, name
+
+
+def test_the_binding_takes_whole_numbers_of_groups_only(lib):
+    """Also where the same shape was taken before with a number that compares equal."""
+    import torch
+    ew = B.EwOps(B.FDG_BF16_TC)
+    shape = torch.Size((2, 4, 16))
+    for groups in (4.0, "4", None):
+        with pytest.raises(B.FDGError):
+            ew._gn(shape, groups, 0)
+    ew._gn(shape, 4, 0)
+    for groups in (4.0, torch.tensor(4)):
+        with pytest.raises(B.FDGError):
+            ew._gn(shape, groups, 0)
