@@ -829,3 +829,59 @@ def test_more_groups_and_totals_than_a_grid_has_ctas():
         n, p, c, groups = shape
         x, xo, y, stats, bits, _ = _check_forward(ew, shape, "relu", False, seed=220, gate=True)
         _check_backward(ew, shape, "relu", 220, xo, x, stats, y, bits, True, False)
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("shape", [(8, 256, 8, 4), (2, 1024, 160, 32), (3, 65, 33, 11), (1, 16384, 64, 8), (2, 9001, 160, 32), (1, 20011, 30, 1),
+                                   (2, 5, 4104, 27), (2000, 4, 64, 4), (1100, 25, 96, 4), (601, 21, 30, 6), (300, 1, 4096, 32)], ids=str)
+def test_the_options_of_the_backward_pass_together(prec_name, shape):
+    """The stored y and a gradient added to dx, with x and with its codes; x with bits, with and without the added gradient."""
+    _, ew = _ops(prec_name)
+    n, p, c, groups = shape
+    x, xo, y, stats, bits, _ = _check_forward(ew, shape, "relu", True, seed=180, gate=True)
+    held = ew.ckpt_encode(x)
+    heldo = L.ckpt_decode(held[0].cpu().numpy().reshape(-1, c), held[1].cpu().numpy().reshape(n * p, -1)).reshape(n, p, c)
+    for xo_, x_ in ((xo, x), (heldo, held)):
+        for with_res in (False, True):
+            a = _check_backward(ew, shape, "relu", 180, xo_, x_, stats, y, bits, with_res, False)
+            b = _check_backward(ew, shape, "relu", 180, xo_, x_, stats, y, bits, with_res, True)
+            assert all(torch.equal(s, t) for s, t in zip(a, b))          # the gate is the same, so is everything
+
+
+@pytest.mark.parametrize("prec_name", PRECISIONS)
+@pytest.mark.parametrize("by", [0, 1, 2, 4])
+@pytest.mark.parametrize("shape", LARGE + [(1, 20000, 36, 4), (2, 12000, 96, 8), (1, 70001, 16, 2), (1, 50000, 8, 1), (2, 3000, 2112, 33)], ids=str)
+def test_codes_of_streamed_calls_are_those_of_the_encoder(prec_name, shape, by):
+    _, ew = _ops(prec_name)
+    n, p, c, groups = shape
+    buf = torch.empty(n * p * c + by, dtype=ew.dtype, device="cuda")
+    x = buf[by:].view(n, p, c)
+    x.copy_(torch.randn((n, p, c), generator=torch.Generator(device="cuda").manual_seed(19), device="cuda") * 2 + 0.5)
+    x[0, 17, :3], x[-1, p - 1, c - 1] = 0.0, float("inf")
+    want = ew.ckpt_encode(x)
+    gamma, beta = (_f32(a) for a in _params(c, 191))
+    for act, kw in (("relu", dict(gate=True)), ("none", dict(res=x)), ("silu", {})):
+        held = ew.gn_forward(x, groups, gamma, beta, act=act, checkpoint=True, **kw)[3]
+        assert torch.equal(held[0], want[0]) and torch.equal(held[1], want[1])
+
+
+def test_sums_of_parameters_past_32_bits():
+    """More than 2^31 values: dgamma and dbeta, against float64 sums image by image."""
+    _, ew = _ops("bf16")
+    n, p, c, groups = 17, 1 << 20, 128, 8
+    x = torch.empty((n, p, c), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(6)
+    for i in range(n):
+        x[i] = torch.randn((p, c), generator=g, device="cuda")
+    one = torch.ones(c, device="cuda")
+    y, stats, _, _ = ew.gn_forward(x, groups, one, torch.zeros_like(one), act="relu")
+    dx, dgamma, dbeta = ew.gn_backward(y, x, stats, groups, one, act="relu", mask=y)
+    A, B, mag = (torch.zeros(c, dtype=torch.float64, device="cuda") for _ in range(3))
+    for i in range(n):
+        for first in range(0, p, 1 << 18):
+            v, dz = x[i, first:first + (1 << 18)].double(), y[i, first:first + (1 << 18)].double()
+            m, r = (stats[k, i].double().repeat_interleave(c // groups) for k in range(2))
+            A += (dz * (v - m) * r).sum(0)
+            B += dz.sum(0)
+            mag += (dz * (v.abs() + m.abs()) * r).sum(0)
+    assert ((dgamma.double() - A).abs() <= 2 * K * mag).all() and ((dbeta.double() - B).abs() <= 2 * K * B).all()
