@@ -182,11 +182,11 @@ fdg_status fdg_ckpt_decode(int precision, const int8_t* codes, const uint8_t* sc
 /* ---- group normalisation with an activation -------------------------------------------------------------------------
  * The normalisation that does not depend on which images share a batch.  x [N][HW][C]; group g of an image is channels
  * [g*C/groups, (g+1)*C/groups) at all of its pixels (groups = 1: layer norm over an image, groups = C: instance norm).
- * `groups` divides C; any C up to 65536, at most 2^30 images and 2^36 values, any alignment that the storage type has (multiples of 8 channels on 16-byte aligned tensors are
- * fastest).  gamma, beta, dgamma, dbeta [C], stats [2][N][groups] (mean, then 1/sqrt(var + eps), biased variance) are fp32, 4-byte aligned.
+ * `groups` divides C; any C up to 65536, at most 2^30 images and 2^36 values, any alignment that the storage type has (multiples
+ * of 8 channels on tensors aligned to 8 values are fastest).  gamma, beta, dgamma, dbeta [C], stats [2][N][groups] (mean, then 1/sqrt(var + eps), biased variance) are fp32, 4-byte aligned.
  * `scratch`: fdg_gn_scratch_bytes bytes of device memory for that pass (0 for a forward pass that needs none: scratch may then
- * be NULL), 256-byte aligned, any contents; not to be shared by calls that may run at the same time.  The result of a call does not depend on scheduling.  No output
- * overlaps an input or another output.  Errors: FDG_ERR_INVALID_ARG (null pointer, bad shape, precision or activation, a
+ * be NULL), 256-byte aligned, any contents; not to be shared by calls that may run at the same time.  The result of a call does
+ * not depend on scheduling.  In a group without spread x - mean is 0 exactly.  No output overlaps an input or another output.  Errors: FDG_ERR_INVALID_ARG (null pointer, bad shape, precision or activation, a
  * combination named below), FDG_ERR_WORKSPACE_TOO_SMALL, FDG_ERR_CUDA; nothing is launched after the first two. */
 typedef struct {
   int N;        /* images */
@@ -209,7 +209,8 @@ fdg_status fdg_gn_forward(int precision, const fdg_gn_shape* shape, const void* 
  * xhat = (x - mean)*rstd from `stats` and either `x` or the checkpoint (`codes`, `scales`); exactly one of the two is given.
  * FDG_ACT_RELU: dz = dy * [y > 0] from exactly one of `mask` (y, or any tensor that is positive where y is) and `gate`; the other
  * activations take neither.  FDG_ACT_SILU recomputes z from xhat, gamma and beta (beta nullable otherwise).  Where the
- * forward added `res`, the gradient of that summand is dz. */
+ * forward added `res`, the gradient of that summand is dz, which no call of this library forms from bits: a program that adds a
+ * shortcut keeps y, or multiplies dy by the bits itself. */
 fdg_status fdg_gn_backward(int precision, const fdg_gn_shape* shape, const void* dy, const void* x, const int8_t* codes,
                            const uint8_t* scales, const float* stats, const float* gamma, const float* beta, int act,
                            const void* mask, const uint8_t* gate, const void* res, void* dx, float* dgamma, float* dbeta,

@@ -679,9 +679,10 @@ __global__ void __launch_bounds__(kThreads, kForwardPerSm) forward_kernel(const 
 // for, each team one after the other with the next one's copy under way; a team waits for nobody else.  An image is in shared
 // memory, so its mean comes first and the squares of what is left of it after, from sums over groups (a value per thread where
 // columns lie in one group each).  What a CTA per image spends on starting, on exchanging sums and on its end is the time of these
-// calls: us, with the other forms / with this one, 16-bit storage: 4096x2x2x64 54 / 4.9, 4096x4x4x256 66 / 14, 1024x8x8x160 23 / 10,
-// 20000x1x512 284 / 26, 128x8x8x160 6.4 / 4.6, one image of 8x8x64 4.9 / 3.2.  Bound by issue slots at one pixel per image (a quarter of the
-// copy rate), by memory from a few kilobytes per image on (60 to 72 %).  A pixel at a time: two cost spilled registers (14.3 against 16.4).
+// calls: us, with the other forms / with this one, 16-bit storage: 4096x2x2x64 54 / 5.0, 4096x4x4x256 66 / 15, 1024x8x8x160 23 / 11,
+// 20000x1x512 284 / 28, 128x8x8x160 6.4 / 4.3, one image of 8x8x64 4.9 / 3.0.  Bound by issue slots at one pixel per image (a quarter of the
+// copy rate), by memory from a few kilobytes per image on (60 to 72 %).  A pixel at a time: two cost more spilled registers (14.3 against
+// 16.4).  At 80 registers the forms with a residual, gate or codes, and those for rows that are no whole vectors, spill 16 to 88 bytes.
 struct Team {
   int first, tid, size;       // its first thread, this thread's number in it
   int sub, set, r0, j0;       // which of a group's lanes, of which of the first groups; where that lane's terms start
@@ -1426,8 +1427,8 @@ __global__ void __launch_bounds__(1024) totals_kernel(const float* __restrict__ 
 // The team form of the backward pass: both passes over an image from shared memory.  A team adds its images' A and B up in registers (at
 // most kTeamImages of them, so that sums stay short), a CTA leaves one row of its teams' in scratch for parameters_kernel.  What ReLU
 // passes of dy replaces it in shared memory, so that the mask or its bits are read once.  us, streamed / this form, 16-bit storage, no
-// activation: 4096x2x2x64 62 / 9, 4096x4x4x256 74 / 28, 2000x7x7x128 39 / 34, 20000x1x512 365 / 37; from codes and bits 75 / 10, 90 / 40,
-// 48 / 42, 437 / 45.  Bound by issue slots, at one pixel per image by what an image costs beside its values.
+// activation: 4096x2x2x64 62 / 9, 4096x4x4x256 74 / 28, 2000x7x7x128 39 / 35, 20000x1x512 365 / 37; from codes and bits 75 / 10, 90 / 39,
+// 48 / 42, 437 / 44.  Bound by issue slots, at one pixel per image by what an image costs beside its values.
 constexpr int kTeamImages = 128;
 template <typename T, int W, bool CK, int SLOPE>
 __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_teams_kernel(const __grid_constant__ Backward<T> p) {
@@ -1646,7 +1647,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardPerSm) backward_apply_kerne
     for (int c = threadIdx.x; c < g.C; c += kThreads) chan[c] = weighted(c);
     __syncthreads();
     group_sums(sets, g.Cg, g.lanes_g, [&](int c) { return chan[c]; }, done);
-  } else if (rows == 1) {             // loads that do not wait for one another (4096x1x4096, one group: 477 us for 2576)
+  } else if (rows == 1) {             // loads that do not wait for one another (4096x1x4096, one group: 505 us for 2576)
     group_sums(sets, g.Cg, g.lanes_g, [&](int c) {
       const float w = p.gamma[c_base + c];
       return make_float2(w * src[g.C + c_base + c], w * src[c_base + c]);
@@ -1721,7 +1722,7 @@ inline Plan plan_streamed(int N, int P, int C, int G, int per_sm) {
 // (rounds of images per team) * (pixels per thread + 4, the fixed part of a round, in pixels), the fewest slices and the largest team
 // where some are alike; none where an image does not fit.  vec_bytes: of a thread's pixel in shared memory; shared, per_group: bytes of
 // a CTA, of a team's group beside them.
-// Slices are for rows wider than a CTA (us, streamed / sliced: 4096x1x4096 263 / 48, 512x4x4x4096 63 / 28) and, forward, for images that
+// Slices are for rows wider than a CTA (us, streamed / sliced: 4096x1x4096 263 / 49, 512x4x4x4096 63 / 29) and, forward, for images that
 // all run at once then (16x16x16x256 6.8 / 3.4, 64x7x7x512 7.1 / 4.5, 128x8x8x640 8.7 / 7.2; in rounds 512x8x8x640 30 / 28 and with codes
 // 38 / 44; backward 512x16x16x64 16.5 / 20.3).
 // Forward (`most` = 12): teams smaller than a CTA only where they leave no SM without one (37x28x28x30 on 19 SMs: 12 us for 8.4); with
